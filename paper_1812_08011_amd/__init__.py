@@ -1,4 +1,4 @@
-"""Python binding of libfp8train (include/fp8train.h).
+"""Python binding of libfp8train (include/fp8train.h, include/fp8train_lm.h).
 
 Argument marshalling only: every step runs in the HIP library.  Arrays are
 torch tensors on the GPU (uint8 for FP8 codes, uint16 for FP16 codes, float32
@@ -15,6 +15,8 @@ LIB_PATH = os.path.join(PKG, "libfp8train.so")
 OK, EINVAL, EWORKSPACE, EHIP = 0, -1, -2, -3
 SRC_F32, SRC_FP16 = 0, 1
 EXACT, FAST = 0, 1
+FMT_F32, FMT_FP16, FMT_FP8, FMT_HALF = 0, 1, 2, 3
+ATTN_MAX_D = 128
 
 _lib = None
 
@@ -84,6 +86,24 @@ def lib():
                                   u64, vp]
         L.sr_weight_update.restype = i32
         L.sr_weight_update.argtypes = [vp, vp, vp, vp, i64, f32, f32, f32, u64, u64, vp]
+        L.fp16_dequantize.restype = i32
+        L.fp16_dequantize.argtypes = [vp, f32, vp, i32, i64, vp]
+        L.rotary_embed.restype = i32
+        L.rotary_embed.argtypes = [vp, i32, i64, i64, vp, vp, i64, i64, i64, i64, i32, i32, f32,
+                                   f32, vp, i32, i64, i64, vp]
+        rows, sizes = [vp, i64, i64], [i64] * 8 + [i32]
+        L.attn_fwd_fp8.restype = i32
+        L.attn_fwd_fp8.argtypes = (rows * 3 + [vp, vp] + sizes + [f32] + rows * 2 +
+                                   [f32, vp, vp, sz, vp])
+        L.attn_bwd_fp8.restype = i32
+        L.attn_bwd_fp8.argtypes = (rows * 3 + [vp, vp] + sizes + [f32] + rows * 2 + [vp] +
+                                   rows * 3 + [i32, f32, vp, sz, vp])
+        for f in (L.attn_fwd_fp8_workspace_size, L.attn_bwd_fp8_workspace_size):
+            f.restype = sz
+            f.argtypes = sizes
+        L.distill_loss.restype = i32
+        L.distill_loss.argtypes = [vp, i32, i64, vp, vp, i32, i64, vp, i64, i64, f32, f32, vp, vp,
+                                   i32, i64, vp]
         L.fp8t_status_string.restype = ctypes.c_char_p
         L.fp8t_status_string.argtypes = [i32]
         _lib = L
@@ -289,3 +309,153 @@ def col2im_fp16(cols, N, H, W, C, KH, KW, pad, stride, dX, stream=None):
            lib().col2im_fp16(_ptr(cols), int(N), int(H), int(W), int(C), int(KH), int(KW),
                              int(pad), int(stride), _ptr(dX), _stream(stream)))
     return dX
+
+
+# ---- language-model operators (include/fp8train_lm.h) ------------------------------
+#
+# Tensors carry their sizes and strides here: T x H x D arrays may be any views
+# whose last dimension is contiguous.
+
+def _format(fn, t, allowed):
+    import torch
+    fmt = {torch.float32: FMT_F32, torch.uint16: FMT_FP16, torch.uint8: FMT_FP8,
+           torch.float16: FMT_HALF}.get(t.dtype)
+    if fmt not in allowed:
+        raise TypeError(f"{fn}: a tensor of type {t.dtype} is not taken here")
+    return fmt
+
+
+def _rows(fn, t, shape, dtype=None):
+    """(address, token stride, head stride) of a T x H x D tensor."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{fn}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{fn}: {t.dtype} where {dtype} is needed")
+    ts, hs, ds = t.stride()
+    if ds != 1 and shape[2] > 1:
+        raise ValueError(f"{fn}: the last dimension must be contiguous")
+    return t.data_ptr(), ts, hs
+
+
+def _dense(fn, t, shape, dtype):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{fn}: a contiguous {dtype} tensor of shape {tuple(shape)} is needed")
+    return t.data_ptr()
+
+
+def fp16_dequantize(src, dst, scale=1.0, stream=None):
+    """dst (float32 or float16) = value of the FP16 codes src, times scale."""
+    import torch
+    fmt = _format("fp16_dequantize", dst, (FMT_F32, FMT_HALF))
+    if src.dtype != torch.uint16 or dst.numel() != src.numel():
+        raise TypeError("fp16_dequantize: uint16 src, dst of the same size")
+    if not (src.is_contiguous() and dst.is_contiguous()):
+        raise ValueError("fp16_dequantize: tensors must be contiguous")
+    _check("fp16_dequantize", lib().fp16_dequantize(_ptr(src), float(scale), _ptr(dst), fmt,
+                                                    src.numel(), _stream(stream)))
+    return dst
+
+
+def rotary_embed(x, positions, freqs, y, interleaved=False, inverse=False, mscale=1.0, scale=1.0,
+                 stream=None):
+    """y = x with the first 2 * len(freqs) entries of every head turned by
+    positions * freqs; x, y: T x H x D (float32, FP16 or FP8 codes), positions:
+    T int64, freqs: R/2 float64.  y may be x."""
+    import torch
+    fn, any_fmt = "rotary_embed", (FMT_F32, FMT_FP16, FMT_FP8)
+    T, H, D = x.shape
+    _check(fn, lib().rotary_embed(
+        *_with_format(_rows(fn, x, x.shape), _format(fn, x, any_fmt)),
+        _dense(fn, positions, (T,), torch.int64), _dense(fn, freqs, freqs.shape[:1], torch.float64),
+        T, H, D, 2 * freqs.numel(), int(interleaved), int(inverse), float(mscale), float(scale),
+        *_with_format(_rows(fn, y, x.shape), _format(fn, y, any_fmt)), _stream(stream)))
+    return y
+
+
+def _with_format(rows, fmt):
+    return (rows[0], fmt) + rows[1:]
+
+
+def _attn_sizes(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal):
+    import torch
+    Tq, Hq, D = q.shape
+    Tk, Hkv, _ = k.shape
+    S = cu_q.numel() - 1
+    if D != k.shape[2]:
+        raise ValueError(f"{fn}: q and k have different head dimensions")
+    return ((*_rows(fn, q, (Tq, Hq, D), torch.uint8), *_rows(fn, k, (Tk, Hkv, D), torch.uint8),
+             *_rows(fn, v, (Tk, Hkv, D), torch.uint8), _dense(fn, cu_q, (S + 1,), torch.int64),
+             _dense(fn, cu_k, (S + 1,), torch.int64)),
+            (S, Tq, Tk, int(max_q), int(max_k), Hq, Hkv, D, int(causal)))
+
+
+def attn_fwd_fp8_workspace_size(q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale):
+    return int(lib().attn_fwd_fp8_workspace_size(
+        cu_q.numel() - 1, q.shape[0], k.shape[0], int(max_q), int(max_k), q.shape[1], k.shape[1],
+        q.shape[2], int(causal)))
+
+
+def attn_bwd_fp8_workspace_size(q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale):
+    return int(lib().attn_bwd_fp8_workspace_size(
+        cu_q.numel() - 1, q.shape[0], k.shape[0], int(max_q), int(max_k), q.shape[1], k.shape[1],
+        q.shape[2], int(causal)))
+
+
+def attn_fwd_fp8(q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale, o, o8, o8_scale=1.0,
+                 lse=None, workspace=None, workspace_bytes=0, stream=None):
+    """Attention of FP8 codes q (Tq x Hq x D) over k, v (Tk x Hkv x D), packed
+    by the int64 offsets cu_q, cu_k; o (FP16 codes), o8 (FP8 codes) and lse
+    (float32, Hq x Tq) are each optional."""
+    import torch
+    fn = "attn_fwd_fp8"
+    ins, sizes = _attn_sizes(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal)
+    none = (None, 0, 0)
+    _check(fn, lib().attn_fwd_fp8(
+        *ins, *sizes, float(sm_scale),
+        *(none if o is None else _rows(fn, o, q.shape, torch.uint16)),
+        *(none if o8 is None else _rows(fn, o8, q.shape, torch.uint8)), float(o8_scale),
+        None if lse is None else _dense(fn, lse, (q.shape[1], q.shape[0]), torch.float32),
+        _ptr(workspace), int(workspace_bytes), _stream(stream)))
+    return o8 if o is None else o
+
+
+def attn_bwd_fp8(q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale, o, d_o, lse, dq, dk, dv,
+                 grad_scale=1.0, workspace=None, workspace_bytes=0, stream=None):
+    """Gradients dq, dk, dv (all FP16 or all FP8 codes) from attn_fwd_fp8's o
+    (FP16 codes) and lse and the error d_o of o (FP8 codes)."""
+    import torch
+    fn = "attn_bwd_fp8"
+    ins, sizes = _attn_sizes(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal)
+    fmt = _format(fn, dq, (FMT_FP16, FMT_FP8))
+    _check(fn, lib().attn_bwd_fp8(
+        *ins, *sizes, float(sm_scale), *_rows(fn, o, q.shape, torch.uint16),
+        *_rows(fn, d_o, q.shape, torch.uint8),
+        _dense(fn, lse, (q.shape[1], q.shape[0]), torch.float32),
+        *_rows(fn, dq, q.shape, dq.dtype), *_rows(fn, dk, k.shape, dq.dtype),
+        *_rows(fn, dv, k.shape, dq.dtype), fmt, float(grad_scale), _ptr(workspace),
+        int(workspace_bytes), _stream(stream)))
+    return dq, dk, dv
+
+
+def distill_loss(z, idx, t, w, tau, grad_scale, loss, g, stream=None):
+    """Distillation loss of logits z (N x V, float32 or FP16 codes) against a
+    teacher's entries idx, t (N x k): loss (float32, N) and the gradient g
+    (N x V: float32, FP16 or FP8 codes; may be z); either may be None, and w
+    (float32 row weights) too."""
+    import torch
+    fn = "distill_loss"
+    N, V = z.shape
+    k = idx.shape[1]
+
+    def matrix(m, allowed):
+        if tuple(m.shape) != (N, V) or (N > 0 and V > 1 and m.stride(1) != 1):
+            raise ValueError(f"{fn}: an N x V tensor with contiguous rows is needed")
+        return m.data_ptr(), _format(fn, m, allowed), max(m.stride(0), V if N <= 1 else 0)
+    _check(fn, lib().distill_loss(
+        *matrix(z, (FMT_F32, FMT_FP16)), _dense(fn, idx, (N, k), torch.int64),
+        _dense(fn, t, (N, k), t.dtype), _format(fn, t, (FMT_F32, FMT_FP16)), k,
+        None if w is None else _dense(fn, w, (N,), torch.float32), N, V, float(tau),
+        float(grad_scale), None if loss is None else _dense(fn, loss, (N,), torch.float32),
+        *((None, FMT_F32, 0) if g is None else matrix(g, (FMT_F32, FMT_FP16, FMT_FP8))),
+        _stream(stream)))
+    return g
