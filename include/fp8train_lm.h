@@ -110,8 +110,8 @@ int rotary_embed(const void* x, int x_format, int64_t x_ts, int64_t x_hs, const 
  * multiple of Hkv, S, Tq, Tk, Hq above 2^31 - 4097, a flag not 0/1, sm_scale
  * not positive and finite, negative input stride, an output stride that
  * makes rows overlap, NULL pointer for non-empty data, no output, NULL
- * workspace with workspace_bytes > 0); FP8T_EWORKSPACE (0 < workspace_bytes <
- * the query); FP8T_EHIP.
+ * workspace with workspace_bytes > 0, or one that is not 16-byte aligned where
+ * it is used); FP8T_EWORKSPACE (0 < workspace_bytes < the query); FP8T_EHIP.
  */
 int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const uint8_t* k, int64_t k_ts,
                  int64_t k_hs, const uint8_t* v, int64_t v_ts, int64_t v_hs, const int64_t* cu_q,

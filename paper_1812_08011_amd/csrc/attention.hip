@@ -1,5 +1,5 @@
 // Attention over packed sequences (attn_fwd_fp8, attn_bwd_fp8): host side.
-#include "attn.h"
+#include "attn_fwd.h"
 
 namespace fp8t {
 namespace {
@@ -12,63 +12,6 @@ __device__ __forceinline__ float dot_row(const float* row, const uint8_t* p, int
     float s = 0.0f;
     for (int d = 0; d < D; ++d) s = __builtin_fmaf(row[d], fp8_to_f32<0>(p[d]), s);
     return s;
-}
-
-// Forward, a wave per (query, head).
-__global__ __launch_bounds__(kThreads) void attn_fwd_rows(AttnArgs a) {
-    __shared__ float qs[kWaves][FP8T_ATTN_MAX_D];
-    __shared__ float ps[kWaves][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = blockIdx.y;
-    int local;
-    const int s = slot_owner(a.cu_q, a.S, a.Tq, 1, kWaves, blockIdx.x, local);
-    const Seq sq = load_seq(a, s);
-    if ((int64_t)local * kWaves >= sq.nq) return;
-    const int i = local * kWaves + wave;
-    const bool live = i < sq.nq;
-    const int64_t t = sq.q0 + (live ? i : 0);
-    const int hk = h / (a.Hq / a.Hkv);
-    const uint8_t* q = a.q.p + t * a.q.ts + h * a.q.hs;
-    for (int d = lane; d < a.D; d += 64) qs[wave][d] = fp8_to_f32<0>(q[d]);
-    __syncthreads();
-    if (!live) return;
-    const int64_t lim = a.causal ? (int64_t)i + 1 + sq.nk - sq.nq : sq.nk;
-    const int seen = lim < 0 ? 0 : (int)lim;
-    float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
-    for (int j0 = 0; j0 < seen; j0 += 64) {
-        const int j = j0 + lane;
-        float x = -INFINITY;
-        if (j < seen)
-            x = a.c2 * dot_row(qs[wave], a.k.p + (sq.k0 + j) * a.k.ts + hk * a.k.hs, a.D);
-        float mb = x;
-        for (int d = 32; d; d >>= 1) mb = fmaxf(mb, __shfl_xor(mb, d));
-        const float mn = fmaxf(m, mb);
-        const float r = m == -INFINITY ? 0.0f : exp2f(m - mn);
-        const float p = j < seen && mn != -INFINITY ? exp2f(x - mn) : (j < seen ? x - mn : 0.0f);
-        float pl = p;
-        for (int d = 32; d; d >>= 1) pl += __shfl_xor(pl, d);
-        l = l * r + pl;
-        m = mn;
-        ps[wave][lane] = p;
-        __builtin_amdgcn_wave_barrier();
-        for (int u = 0; u < 2; ++u) {
-            const int d = lane + 64 * u;
-            o[u] *= r;
-            if (d < a.D)
-                for (int jj = 0; jj < 64 && j0 + jj < seen; ++jj)
-                    o[u] += ps[wave][jj] *
-                            fp8_to_f32<0>(a.v.p[(sq.k0 + j0 + jj) * a.v.ts + hk * a.v.hs + d]);
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
-    for (int u = 0; u < 2; ++u) {
-        const int d = lane + 64 * u;
-        if (d >= a.D) continue;
-        const float x = seen ? o[u] / l : 0.0f;
-        if (a.o) a.o[t * a.o_ts + h * a.o_hs + d] = f32_to_fp16_rn(x);
-        if (a.o8) a.o8[t * a.o8_ts + h * a.o8_hs + d] = (uint8_t)f32_to_fp8(x * a.o8_scale);
-    }
-    if (a.lse && lane == 0)
-        a.lse[(int64_t)h * a.Tq + t] = seen ? kAttnLn2 * (m + log2f(l)) : -INFINITY;
 }
 
 // delta = <e, o>, a wave per (query, head).
@@ -206,6 +149,10 @@ bool rows_ok(const void* p, int64_t ts, int64_t hs, int64_t T, int64_t H) {
     return ts >= 0 && hs >= 0 && (p || T == 0 || H == 0);
 }
 
+bool rows16(const AttnRows& r) {
+    return aligned(r.p, 16) && r.ts % 16 == 0 && r.hs % 16 == 0;
+}
+
 }  // namespace
 }  // namespace fp8t
 
@@ -215,7 +162,8 @@ extern "C" size_t attn_fwd_fp8_workspace_size(int64_t S, int64_t Tq, int64_t Tk,
                                               int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D,
                                               int causal) {
     if (!sizes_ok(S, Tq, Tk, max_q, max_k, Hq, Hkv, D, causal)) return 0;
-    return 0;
+    if (S == 0 || Tq == 0 || Hq == 0) return 0;
+    return attn_fwd_plan(S, Tq, max_q, max_k, Hq, Hkv, D).bytes;
 }
 
 extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const uint8_t* k,
@@ -235,9 +183,10 @@ extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     if (!cu_q || !cu_k || (!o && !o8 && !lse)) return FP8T_EINVAL;
     if ((o && !rows_apart(Tq, Hq, D, o_ts, o_hs)) || (o8 && !rows_apart(Tq, Hq, D, o8_ts, o8_hs)))
         return FP8T_EINVAL;
-    if (workspace_bytes && workspace_bytes < attn_fwd_fp8_workspace_size(S, Tq, Tk, max_q, max_k,
-                                                                         Hq, Hkv, D, causal))
-        return FP8T_EWORKSPACE;
+    AttnFwdPlan p = attn_fwd_plan(S, Tq, max_q, max_k, Hq, Hkv, D);
+    if (workspace_bytes && workspace_bytes < p.bytes) return FP8T_EWORKSPACE;
+    if (p.bytes && !workspace_bytes) p.splits = 1;
+    if (p.splits > 1 && !aligned(workspace, 16)) return FP8T_EINVAL;
     AttnArgs a = {};
     a.q = {q, q_ts, q_hs};
     a.k = {k, k_ts, k_hs};
@@ -261,8 +210,8 @@ extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     a.o8_hs = o8_hs;
     a.o8_scale = o8_scale;
     a.lse = lse;
-    hipLaunchKernelGGL(attn_fwd_rows, dim3((unsigned)slots(S, Tq, 1, kWaves), (unsigned)Hq),
-                       dim3(kThreads), 0, stream, a);
+    const bool vec = D % 16 == 0 && rows16(a.q) && rows16(a.k) && rows16(a.v);
+    attn_fwd_launch(a, p, vec, workspace, stream);
     return launch_status();
 }
 

@@ -1,0 +1,471 @@
+// Attention forward on the matrix cores.
+//
+// A workgroup owns a tile of rows -- (query, query head of a group) pairs, the
+// heads of a group beside each other, so that one pass over a key head's keys
+// and values serves them all -- and streams key tiles through LDS.
+#include "attn_mfma.h"
+#include "attn_fwd.h"
+
+namespace fp8t {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kBase = 7.0f;         // p is held times 2^7 (relative to the row's reference)
+constexpr float kRoom = 15.0f;        // and may grow to 2^15 before the reference moves
+
+struct Fmax { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct Add { __device__ float operator()(float a, float b) const { return a + b; } };
+
+// Key tile in flight: the registers between global memory and LDS.
+template <int DP, int NT>
+struct Stage {
+    static constexpr int kBN = attn_keys(DP);
+    static constexpr int kK = CodeTile<kBN, DP>::template units<NT>();
+    static constexpr int kV = HalfTile<kBN, DP>::template units<NT>();
+    uint4 k[kK];
+    uint2 v[kV][4];
+};
+
+template <int DP, bool VEC, int NT>
+__device__ __forceinline__ void load_k(Stage<DP, NT>& s, const uint8_t* k, int64_t ts, int j0, int nk,
+                                       int D, int tid) {
+#pragma unroll
+    for (int u = 0; u < Stage<DP, NT>::kK; ++u) {
+        const int id = tid + u * NT, row = id / (DP / 16), col = id % (DP / 16) * 16;
+        s.k[u] = load_codes16<VEC>(k + (int64_t)(j0 + row) * ts, col, D, j0 + row < nk);
+    }
+}
+template <int DP, bool VEC, int NT>
+__device__ __forceinline__ void load_v(Stage<DP, NT>& s, const uint8_t* v, int64_t ts, int j0, int nk,
+                                       int D, int tid) {
+    constexpr int kBN = attn_keys(DP);
+    using HT = HalfTile<kBN, DP>;
+#pragma unroll
+    for (int u = 0; u < Stage<DP, NT>::kV; ++u) {
+        const int id = tid + u * NT, row = j0 + HT::unit_row(id), col = HT::unit_col(id);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            s.v[u][r] = load_codes8<VEC>(v + (int64_t)(row + r) * ts, col, D, row + r < nk);
+    }
+}
+template <int DP, int NT>
+__device__ __forceinline__ void store_k(const Stage<DP, NT>& s, uint8_t* lds, int tid) {
+    constexpr int kBN = attn_keys(DP);
+#pragma unroll
+    for (int u = 0; u < Stage<DP, NT>::kK; ++u) {
+        const int id = tid + u * NT, row = id / (DP / 16), col = id % (DP / 16) * 16;
+        *reinterpret_cast<uint4*>(lds + row * CodeTile<kBN, DP>::kRow + col) = s.k[u];
+    }
+}
+// partial: some row does not see some key of the tile.  Values that are not
+// finite are then taken out (a matrix product would let 0 x NaN into rows that
+// do not see the key) and their keys noted in `bad`.
+template <int DP, int NT>
+__device__ __forceinline__ void store_v(Stage<DP, NT>& s, uint8_t* lds, int tid, bool partial,
+                                        uint32_t* bad) {
+    constexpr int kBN = attn_keys(DP);
+    using HT = HalfTile<kBN, DP>;
+#pragma unroll
+    for (int u = 0; u < Stage<DP, NT>::kV; ++u) {
+        const int id = tid + u * NT;
+        if (partial) {
+            const int row = HT::unit_row(id);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t nx = nonfinite_bytes(s.v[u][r].x), ny = nonfinite_bytes(s.v[u][r].y);
+                if (nx | ny) {
+                    atomicOr(bad + (row + r) / 32, 1u << ((row + r) % 32));
+                    s.v[u][r].x &= ~nx;
+                    s.v[u][r].y &= ~ny;
+                }
+            }
+        }
+        HT::store(lds, id, s.v[u]);
+    }
+}
+
+// KW = 1: 128 rows, 32 per wave, every wave walks all key tiles (shared in
+// LDS, double-buffered).  KW = 4: 32 rows, each wave walks every fourth key
+// tile by itself and the waves' results are joined in LDS -- for calls with
+// few rows, where the keys are what there is to share out.
+// SPLIT: the key tiles are shared out over gridDim.y workgroups, whose partial
+// results go to the workspace.
+template <int DP, int KW, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnSplit sp) {
+    constexpr int NT = kThreads / KW, BM = 128 / KW;
+    constexpr int NB = KW == 1 ? 2 : 4;                     // LDS buffers: double, or one per wave
+    constexpr int kBN = attn_keys(DP);
+    constexpr int NC = DP / 32, ND = DP / 32, NK = kBN / 32;
+    using CT = CodeTile<kBN, DP>;
+    using HT = HalfTile<kBN, DP>;
+    __shared__ __attribute__((aligned(16))) uint8_t ks[KW == 1 ? NB * CT::kBytes : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t vs[NB * HT::kBytes];
+    __shared__ uint32_t bad[4][NK];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+    const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
+    int tile;
+    const int s = slot_owner(a.cu_q, a.S, a.Tq, G, BM, blockIdx.x / a.Hkv, tile);
+    const Seq sq = load_seq(a, s);
+    const int64_t nrows = (int64_t)sq.nq * G;
+    const int ntiles = (int)((nrows + BM - 1) / BM);
+    if (tile >= ntiles) return;
+    tile = ntiles - 1 - tile;                               // the longest first
+    const int64_t row0 = (int64_t)tile * BM, row = row0 + (KW == 1 ? 32 * wave : 0) + l31;
+    const bool live = row < nrows;
+    const int i = live ? (int)(row / G) : 0, g = live ? (int)(row % G) : 0;
+    const int off = sq.nk - sq.nq;
+    // keys [0, lim) are seen by this lane's row; the tile's first and last row
+    auto limit = [&](int64_t r) {
+        const int64_t n = a.causal ? r / G + 1 + off : sq.nk;
+        return (int)(n < 0 ? 0 : n);
+    };
+    const int lim = live ? limit(row) : 0;
+    const int64_t last = row0 + BM < nrows ? row0 + BM - 1 : nrows - 1;
+    const int lim_lo = limit(row0), lim_hi = limit(last);
+    int wave_hi = lim_hi;
+    if (KW == 1) {
+        const int64_t wl = row0 + 32 * wave + 31 < nrows ? row0 + 32 * wave + 31 : nrows - 1;
+        wave_hi = row0 + 32 * wave < nrows ? limit(wl) : 0;
+    }
+    int t0 = 0, t1 = (lim_hi + kBN - 1) / kBN;
+    if (SPLIT) {
+        t0 = blockIdx.y * sp.per;
+        if (blockIdx.y + 1 < gridDim.y && t0 + sp.per < t1) t1 = t0 + sp.per;
+    }
+
+    const int64_t tq = sq.q0 + i;
+    const int hq = hk * G + g;
+    const uint8_t* qp = a.q.p + tq * a.q.ts + (int64_t)hq * a.q.hs;
+    const uint8_t* kp = a.k.p + sq.k0 * a.k.ts + (int64_t)hk * a.k.hs;
+    const uint8_t* vp = a.v.p + sq.k0 * a.v.ts + (int64_t)hk * a.v.hs;
+    const Widen widen;
+    const float c2 = __uint_as_float(in_vgpr(__float_as_uint(a.c2)));
+    v8h qf[NC][2];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const uint4 w = load_codes16<VEC>(qp, 32 * c + 16 * h, a.D, live);
+        qf[c][0] = widen(w.x, w.y);
+        qf[c][1] = widen(w.z, w.w);
+    }
+
+    v16f o[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    float ref = -INFINITY, mu = 0.0f, l = 0.0f;             // reference; the same, 0 before the first key
+    const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+
+    // One key tile: kf(kt, c) gives the key operand, vl the values in LDS; next()
+    // runs once the key operands are used up.
+    auto step = [&](auto kf, const uint8_t* vl, int j0, bool partial, const uint32_t* badw,
+                    auto next) {
+        v16f st[NK];
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt) {
+            st[kt] = zero;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const uint4 w = kf(kt, c);
+                st[kt] = mfma_half(widen(w.x, w.y), qf[c][0], st[kt]);
+                st[kt] = mfma_half(widen(w.z, w.w), qf[c][1], st[kt]);
+            }
+        }
+        next();
+        if (partial) {
+            const int rel = lim - j0 - 4 * h;
+#pragma unroll
+            for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (32 * kt + 8 * (r / 4) + r % 4 >= rel) st[kt][r] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kt][r]);
+        mx = both_halves(mx, Fmax()) * c2;
+        if (__any(mx - ref > kRoom)) {
+            const float nref = fmaxf(ref, mx - kBase);
+            const float f = nref == ref ? 1.0f : exp2f(ref - nref);
+            ref = nref;
+            mu = ref == -INFINITY ? 0.0f : ref;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= f;
+        }
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt) {
+            float p[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][r], c2, -mu));
+                l += p[r];
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const v8h pf = to_half8(p + 8 * t);
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    o[d] = mfma_half(HT::frag(vl, 32 * d + l31, 2 * kt + t, h), pf, o[d]);
+            }
+        }
+        if (partial) {
+            // keys whose values are not finite, for the rows that see them
+#pragma unroll
+            for (int kt = 0; kt < NK; ++kt) {
+                uint32_t b = badw[kt];
+                while (b) {
+                    const int key = j0 + 32 * kt + __builtin_ctz(b);
+                    b &= b - 1;
+                    const uint8_t* vr = vp + (int64_t)key * a.v.ts;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int col = 32 * d + 8 * (r / 4) + 4 * h + r % 4;
+                            const uint32_t c = key < lim && col < a.D ? vr[col] : 0u;
+                            if ((c & 0x7Cu) == 0x7Cu) o[d][r] += fp8_to_f32<0>(c);
+                        }
+                }
+            }
+        }
+    };
+
+    Stage<DP, NT> sg;
+    if constexpr (KW == 1) {
+        if (tid < 4 * NK) bad[tid / NK][tid % NK] = 0u;
+        __syncthreads();
+        auto is_partial = [&](int t) { return (t + 1) * kBN > lim_lo || (t + 1) * kBN > sq.nk; };
+        if (t0 < t1) {
+            load_k<DP, VEC>(sg, kp, a.k.ts, t0 * kBN, sq.nk, a.D, tid);
+            load_v<DP, VEC>(sg, vp, a.v.ts, t0 * kBN, sq.nk, a.D, tid);
+            store_k(sg, ks, tid);
+            store_v(sg, vs, tid, is_partial(t0), bad[0]);
+        }
+        __syncthreads();
+        for (int t = t0; t < t1; ++t) {
+            const int b = (t - t0) & 1, q = (t - t0) % 3;
+            if (t + 1 < t1) {
+                load_k<DP, VEC>(sg, kp, a.k.ts, (t + 1) * kBN, sq.nk, a.D, tid);
+                load_v<DP, VEC>(sg, vp, a.v.ts, (t + 1) * kBN, sq.nk, a.D, tid);
+            }
+            if (t * kBN < wave_hi) {
+                const uint8_t* kl = ks + b * CT::kBytes;
+                step([&](int kt, int c) { return CT::frag(kl, 32 * kt + l31, c, h); },
+                     vs + b * HT::kBytes, t * kBN, is_partial(t), bad[q], []() {});
+            }
+            // noted keys: slot q is read here, the next one written, the one
+            // read in the last step cleared
+            if (tid < NK) bad[(q + 2) % 3][tid] = 0u;
+            if (t + 1 < t1) {
+                store_k(sg, ks + (b ^ 1) * CT::kBytes, tid);
+                store_v(sg, vs + (b ^ 1) * HT::kBytes, tid, is_partial(t + 1), bad[(q + 1) % 3]);
+            }
+            __syncthreads();
+        }
+    } else {
+        uint8_t* vl = vs + wave * HT::kBytes;
+        uint4 kf[NK][NC];
+        auto load = [&](int t) {
+#pragma unroll
+            for (int kt = 0; kt < NK; ++kt) {
+                const int j = t * kBN + 32 * kt + l31;
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                    kf[kt][c] = load_codes16<VEC>(kp + (int64_t)j * a.k.ts, 32 * c + 16 * h, a.D, j < sq.nk);
+            }
+            load_v<DP, VEC>(sg, vp, a.v.ts, t * kBN, sq.nk, a.D, lane);
+        };
+        // a wave works by itself here: its LDS accesses are ordered
+        auto fence = [&]() {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        if (t0 + wave < t1) load(t0 + wave);
+        for (int t = t0 + wave; t < t1; t += KW) {
+            const bool partial = (t + 1) * kBN > lim_lo || (t + 1) * kBN > sq.nk;
+            fence();
+            if (lane < NK) bad[wave][lane] = 0u;
+            fence();
+            store_v(sg, vl, lane, partial, bad[wave]);
+            fence();
+            step([&](int kt, int c) { return kf[kt][c]; }, vl, t * kBN, partial, bad[wave], [&]() {
+                if (t + KW < t1) load(t + KW);
+            });
+        }
+    }
+    l = both_halves(l, Add());
+
+    if constexpr (KW > 1) {
+        // join the waves: references first, then the scaled sums
+        __shared__ float refs[KW][32], ls[KW][32];
+        __syncthreads();
+        if (h == 0) {
+            refs[wave][l31] = ref;
+            ls[wave][l31] = l;
+        }
+        __syncthreads();
+        float m = refs[0][l31];
+#pragma unroll
+        for (int w = 1; w < KW; ++w) m = fmaxf(m, refs[w][l31]);
+        l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < KW; ++w)
+            l += refs[w][l31] == m ? ls[w][l31] : ls[w][l31] * exp2f(refs[w][l31] - m);
+        const float f = ref == m ? 1.0f : exp2f(ref - m);
+        // wave w's sums go through LDS as [d][lane] floats, 64 lanes at a time
+        float* xs = reinterpret_cast<float*>(vs);
+        static_assert(NB * HT::kBytes >= 3 * ND * 16 * 64 * 4, "the joined waves' sums fit");
+        if (wave) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    xs[(((wave - 1) * ND + d) * 16 + r) * 64 + lane] = o[d][r] * f;
+        }
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float x = o[d][r] * f;
+                for (int w = 0; w < KW - 1; ++w) x += xs[((w * ND + d) * 16 + r) * 64 + lane];
+                o[d][r] = x;
+            }
+        ref = m;
+    }
+
+    if (!live) return;
+    if constexpr (SPLIT) {
+        const int64_t part = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+        const int64_t pr = part * BM + (row - row0);
+        float* po = sp.o + pr * DP;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<float4*>(po + 32 * d + 8 * q + 4 * h) =
+                    make_float4(o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]);
+        if (h == 0) sp.ml[pr] = make_float2(ref, l);
+    } else {
+        attn_write_row<DP>(a, tq, hq, lim, ref, l, h, [&](int d, int r) { return o[d][r]; });
+    }
+}
+
+// Joins the partial results of a tile's key ranges, in their order: a wave per
+// row, a lane for every 64th entry.
+template <int DP>
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSplit sp) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
+    int tile;
+    const int s = slot_owner(a.cu_q, a.S, a.Tq, G, sp.BM, blockIdx.x / a.Hkv, tile);
+    const Seq sq = load_seq(a, s);
+    const int64_t nrows = (int64_t)sq.nq * G;
+    const int ntiles = (int)((nrows + sp.BM - 1) / sp.BM);
+    if (tile >= ntiles) return;
+    tile = ntiles - 1 - tile;
+    const int rr = blockIdx.y * (kThreads / 64) + wave;
+    const int64_t row = (int64_t)tile * sp.BM + rr;
+    if (rr >= sp.BM || row >= nrows) return;
+    const int64_t lim = a.causal ? row / G + 1 + sq.nk - sq.nq : sq.nk;
+    float m = -INFINITY;
+    auto at = [&](int z) {
+        return ((int64_t)z * gridDim.x + blockIdx.x) * sp.BM + rr;
+    };
+    for (int z = 0; z < sp.n; ++z) m = fmaxf(m, sp.ml[at(z)].x);
+    float l = 0.0f, o[2] = {0.0f, 0.0f};
+    for (int z = 0; z < sp.n; ++z) {
+        const float2 ml = sp.ml[at(z)];
+        if (ml.x == -INFINITY) continue;                    // no key in this range
+        const float f = ml.x == m ? 1.0f : exp2f(ml.x - m);
+        l += ml.y * f;
+#pragma unroll
+        for (int u = 0; u < DP / 64; ++u) o[u] += sp.o[at(z) * DP + 64 * u + lane] * f;
+    }
+    const int64_t t = sq.q0 + row / G;
+    const int hq = hk * G + (int)(row % G);
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int u = 0; u < DP / 64; ++u) {
+        const int d = 64 * u + lane;
+        const float x = lim > 0 ? o[u] * inv : 0.0f;
+        if (d >= a.D) continue;
+        if (a.o) a.o[t * a.o_ts + hq * a.o_hs + d] = f32_to_fp16_rn(x);
+        if (a.o8) a.o8[t * a.o8_ts + hq * a.o8_hs + d] = (uint8_t)f32_to_fp8(x * a.o8_scale);
+    }
+    if (a.lse && lane == 0)
+        a.lse[(int64_t)hq * a.Tq + t] = lim > 0 ? kAttnLn2 * (m + log2f(l)) : -INFINITY;
+}
+
+template <int DP, int KW, bool VEC>
+void launch(const AttnArgs& a, const AttnFwdPlan& p, const AttnSplit& sp, hipStream_t stream) {
+    const dim3 grid((unsigned)(a.Hkv * p.slots), (unsigned)p.splits), block(kThreads);
+    if (p.splits > 1) {
+        hipLaunchKernelGGL((attn_fwd_kernel<DP, KW, VEC, true>), grid, block, 0, stream, a, sp);
+        const unsigned rows = (unsigned)((p.max_rows + 3) / 4);
+        hipLaunchKernelGGL(attn_join_kernel<DP>, dim3(grid.x, rows), block, 0, stream, a, sp);
+    } else {
+        hipLaunchKernelGGL((attn_fwd_kernel<DP, KW, VEC, false>), grid, block, 0, stream, a, sp);
+    }
+}
+template <int DP>
+void launch_dp(const AttnArgs& a, const AttnFwdPlan& p, const AttnSplit& sp, bool vec,
+               hipStream_t stream) {
+    if (p.BM == 32) {
+        if (vec) launch<DP, 4, true>(a, p, sp, stream);
+        else launch<DP, 4, false>(a, p, sp, stream);
+    } else {
+        if (vec) launch<DP, 1, true>(a, p, sp, stream);
+        else launch<DP, 1, false>(a, p, sp, stream);
+    }
+}
+
+}  // namespace
+
+// Rows of 32 take the kernel that shares out the keys inside a workgroup; the
+// keys are shared out over workgroups where the rows alone leave CUs idle.
+AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t max_q, int64_t max_k, int64_t Hq,
+                          int64_t Hkv, int64_t D) {
+    AttnFwdPlan p = {};
+    const int64_t G = Hkv ? Hq / Hkv : 1;
+    p.DP = D <= 64 ? 64 : 128;
+    p.BM = max_q * G <= 32 ? 32 : 128;
+    p.slots = slots(S, Tq, G, p.BM);
+    p.max_rows = p.BM;
+    const int64_t tiles_q = (max_q * G + p.BM - 1) / p.BM;
+    int64_t groups = p.slots < S * tiles_q ? p.slots : S * tiles_q;
+    groups *= Hkv;
+    const int kBN = attn_keys(p.DP);
+    const int64_t tiles_k = (max_k + kBN - 1) / kBN;
+    const int64_t want = 4 * (int64_t)device_cus(), least = p.BM == 32 ? 8 : 16;
+    int64_t n = groups > 0 && groups * 2 <= want ? want / groups : 1;
+    if (n > tiles_k / least) n = tiles_k / least;
+    if (n > 64) n = 64;
+    p.splits = n > 1 ? (int)n : 1;
+    p.per = (int)((tiles_k + p.splits - 1) / p.splits);
+    p.bytes = p.splits > 1 ? (size_t)p.splits * p.slots * Hkv * p.BM * (p.DP * 4 + 8) : 0;
+    return p;
+}
+
+void attn_fwd_launch(const AttnArgs& a, const AttnFwdPlan& p, bool vec, void* workspace,
+                     hipStream_t stream) {
+    AttnSplit sp = {};
+    if (p.splits > 1) {
+        const int64_t rows = (int64_t)p.splits * p.slots * a.Hkv * p.BM;
+        sp.o = static_cast<float*>(workspace);
+        sp.ml = reinterpret_cast<float2*>(sp.o + rows * p.DP);
+        sp.n = p.splits;
+        sp.per = p.per;
+        sp.BM = p.BM;
+    }
+    if (p.DP == 64) launch_dp<64>(a, p, sp, vec, stream);
+    else launch_dp<128>(a, p, sp, vec, stream);
+}
+
+}  // namespace fp8t

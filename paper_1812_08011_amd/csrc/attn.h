@@ -53,6 +53,10 @@ __device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s) {
     return r;
 }
 
+__device__ __forceinline__ bool aligned_to(const void* p, uintptr_t n) {
+    return ((uintptr_t)p & (n - 1)) == 0;
+}
+
 // Work of sequences of unknown lengths laid out without a scan: with
 // `len(s) = (cu[s+1] - cu[s]) * mult` rows in tiles of `tile`, sequence s owns
 // the slots from floor(cu[s] mult / tile) + s on -- at least ceil(len / tile)
