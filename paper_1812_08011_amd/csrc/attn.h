@@ -30,6 +30,8 @@ struct AttnArgs {
     int64_t dq_ts, dq_hs, dk_ts, dk_hs, dv_ts, dv_hs;
     float grad_scale;
     float* delta;            // Hq x Tq
+    float* norms;            // the largest squared row norms of e and v, per workgroup
+    int norm_count;
 };
 
 constexpr float kAttnLog2e = 1.44269504088896340736f;
