@@ -31,7 +31,7 @@ extern "C" size_t attn_fwd_fp8_workspace_size(int64_t S, int64_t Tq, int64_t Tk,
                                               int causal) {
     if (!sizes_ok(S, Tq, Tk, max_q, max_k, Hq, Hkv, D, causal)) return 0;
     if (S == 0 || Tq == 0 || Hq == 0) return 0;
-    return attn_fwd_plan(S, Tq, max_q, max_k, Hq, Hkv, D).bytes;
+    return attn_fwd_plan(S, Tq, Tk, max_q, max_k, Hq, Hkv, D).bytes;
 }
 
 extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const uint8_t* k,
@@ -51,10 +51,13 @@ extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     if (!cu_q || !cu_k || (!o && !o8 && !lse)) return FP8T_EINVAL;
     if ((o && !rows_apart(Tq, Hq, D, o_ts, o_hs)) || (o8 && !rows_apart(Tq, Hq, D, o8_ts, o8_hs)))
         return FP8T_EINVAL;
-    AttnFwdPlan p = attn_fwd_plan(S, Tq, max_q, max_k, Hq, Hkv, D);
+    AttnFwdPlan p = attn_fwd_plan(S, Tq, Tk, max_q, max_k, Hq, Hkv, D);
     if (workspace_bytes && workspace_bytes < p.bytes) return FP8T_EWORKSPACE;
-    if (p.bytes && !workspace_bytes) p.splits = 1;
-    if (p.splits > 1 && !aligned(workspace, 16)) return FP8T_EINVAL;
+    if (p.bytes && !workspace_bytes) {
+        p.splits = 1;
+        p.image = false;
+    }
+    if (p.bytes && workspace_bytes && !aligned(workspace, 16)) return FP8T_EINVAL;
     AttnArgs a = {};
     a.q = {q, q_ts, q_hs};
     a.k = {k, k_ts, k_hs};
@@ -88,7 +91,7 @@ extern "C" size_t attn_bwd_fp8_workspace_size(int64_t S, int64_t Tq, int64_t Tk,
                                               int causal) {
     if (!sizes_ok(S, Tq, Tk, max_q, max_k, Hq, Hkv, D, causal)) return 0;
     if (S == 0 || Hq == 0 || (Tq == 0 && Tk == 0)) return 0;
-    return attn_bwd_bytes(Hq, Tq);
+    return attn_bwd_plan(S, Tq, Tk, max_q, max_k, Hq, Hkv, D).bytes;
 }
 
 extern "C" int attn_bwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const uint8_t* k,
@@ -116,9 +119,8 @@ extern "C" int attn_bwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     if (!rows_apart(Tq, Hq, D, dq_ts, dq_hs) || !rows_apart(Tk, Hkv, D, dk_ts, dk_hs) ||
         !rows_apart(Tk, Hkv, D, dv_ts, dv_hs) || !aligned(workspace, 16))
         return FP8T_EINVAL;
-    if (workspace_bytes <
-        attn_bwd_fp8_workspace_size(S, Tq, Tk, max_q, max_k, Hq, Hkv, D, causal))
-        return FP8T_EWORKSPACE;
+    const AttnBwdPlan p = attn_bwd_plan(S, Tq, Tk, max_q, max_k, Hq, Hkv, D);
+    if (workspace_bytes < p.bytes) return FP8T_EWORKSPACE;
     AttnArgs a = {};
     a.q = {q, q_ts, q_hs};
     a.k = {k, k_ts, k_hs};
@@ -149,10 +151,7 @@ extern "C" int attn_bwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     a.dv_ts = dv_ts;
     a.dv_hs = dv_hs;
     a.grad_scale = grad_scale;
-    a.delta = static_cast<float*>(workspace);
-    a.norms = reinterpret_cast<float*>(static_cast<char*>(workspace) + attn_delta_bytes(Hq, Tq));
-    const bool vec = D % 16 == 0 && rows16(a.q) && rows16(a.k) && rows16(a.v) && rows16(a.e) &&
-                     aligned(o, 16) && o_ts % 8 == 0 && o_hs % 8 == 0;
-    attn_bwd_launch(a, grad_format, vec, stream);
+    const bool vec = D % 16 == 0 && rows16(a.q) && rows16(a.k) && rows16(a.v) && rows16(a.e);
+    attn_bwd_launch(a, p, grad_format, vec, workspace, stream);
     return launch_status();
 }

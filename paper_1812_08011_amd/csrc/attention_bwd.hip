@@ -1,19 +1,17 @@
-// Attention backward on the matrix cores, in three kernels:
-//   prepare: delta = <e, o> of every row, and the largest row norms of e and v;
+// Attention backward on the matrix cores, from the images that attn_image.hip
+// builds first:
 //   dq:      a wave owns rows (queries) and streams the keys;
 //   dk, dv:  a wave owns keys and streams the queries of every head that
 //            shares them.
-// Scores are computed twice (7 products instead of 5), which needs no atomics
-// and no partial sums: the same bits on every run.
+// Scores are computed twice (7 products instead of 5), which needs no atomics:
+// the same bits on every run.
 #include "attn_bwd.h"
-#include "attn_mfma.h"
+#include "attn_image.h"
 
 namespace fp8t {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kN = 64;                // rows per streamed tile
-constexpr int kPUp = 15;              // p enters its product times 2^15
 
 // Four entries of a gradient from column col on.
 template <int FG>
@@ -36,157 +34,56 @@ __device__ __forceinline__ void write4(void* base, int64_t at, int col, int D, c
     }
 }
 
-// ---- delta and the norms ------------------------------------------------------------
-
-// 16 lanes per row, 8 entries each.  Norms: the largest squared norm among the
-// finite rows of e, then of v, per workgroup.
-template <bool VEC>
-__global__ __launch_bounds__(kThreads) void attn_prepare_kernel(AttnArgs a) {
-    __shared__ float red[kThreads / 64];
-    const int lane = threadIdx.x & 15, d0 = lane * 8;
-    const int64_t rows_e = a.Tq * a.Hq, rows_v = a.Tk * a.Hkv;
-    const int64_t step = (int64_t)gridDim.x * (kThreads / 16);
-    const int64_t first = (int64_t)blockIdx.x * (kThreads / 16) + threadIdx.x / 16;
-    float top[2] = {0.0f, 0.0f};
-    for (int64_t r = first; r < rows_e; r += step) {
-        const int64_t t = r / a.Hq, hq = r % a.Hq;
-        const uint2 w = load_codes8<VEC>(a.e.p + t * a.e.ts + hq * a.e.hs, d0, a.D, true);
-        const uint16_t* o = a.o + t * a.o_ts + hq * a.o_hs;
-        uint32_t oc[4] = {0, 0, 0, 0};
-        if (VEC) {
-            if (d0 < a.D) {
-                const uint4 q = *reinterpret_cast<const uint4*>(o + d0);
-                oc[0] = q.x;
-                oc[1] = q.y;
-                oc[2] = q.z;
-                oc[3] = q.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (d0 + i < a.D) oc[i / 2] |= (uint32_t)o[d0 + i] << (16 * (i % 2));
-        }
-        float s = 0.0f, n = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float e = fp8_to_f32<0>(((i < 4 ? w.x : w.y) >> (8 * (i % 4))) & 0xFFu);
-            s = __builtin_fmaf(e, fp16_to_f32((oc[i / 2] >> (16 * (i % 2))) & 0xFFFFu), s);
-            n = __builtin_fmaf(e, e, n);
-        }
-#pragma unroll
-        for (int d = 8; d; d >>= 1) {
-            s += __shfl_xor(s, d);
-            n += __shfl_xor(n, d);
-        }
-        if (lane == 0) a.delta[hq * a.Tq + t] = s;
-        if (n < INFINITY) top[0] = fmaxf(top[0], n);
-    }
-    for (int64_t r = first; r < rows_v; r += step) {
-        const int64_t t = r / a.Hkv, hk = r % a.Hkv;
-        const uint2 w = load_codes8<VEC>(a.v.p + t * a.v.ts + hk * a.v.hs, d0, a.D, true);
-        float n = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float v = fp8_to_f32<0>(((i < 4 ? w.x : w.y) >> (8 * (i % 4))) & 0xFFu);
-            n = __builtin_fmaf(v, v, n);
-        }
-#pragma unroll
-        for (int d = 8; d; d >>= 1) n += __shfl_xor(n, d);
-        if (n < INFINITY) top[1] = fmaxf(top[1], n);
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        float x = top[k];
-        for (int d = 32; d >= 16; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-        __syncthreads();
-        if (threadIdx.x == 0)
-            a.norms[k * kAttnNorms + blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    }
-}
-
 // The power of two that dS = p (<e, v> - delta) is held times.  Both terms are
 // at most |e| |v| (delta is a mean of such products), so with the largest norms
 // the scaled dS stays below 2^15, and a dS down to 2^-29 of that bound keeps
-// all 11 bits of a half.  Every thread of the workgroup calls this.
-__device__ __forceinline__ float ds_scale(const AttnArgs& a, float* red) {
-    float x[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        x[k] = 0.0f;
-        for (int i = threadIdx.x; i < a.norm_count; i += kThreads)
-            x[k] = fmaxf(x[k], a.norms[k * kAttnNorms + i]);
-        for (int d = 32; d; d >>= 1) x[k] = fmaxf(x[k], __shfl_xor(x[k], d));
-        if ((threadIdx.x & 63) == 0) red[k * 4 + (threadIdx.x >> 6)] = x[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-        x[k] = fmaxf(fmaxf(red[4 * k], red[4 * k + 1]), fmaxf(red[4 * k + 2], red[4 * k + 3]));
-    const float bound = __builtin_sqrtf(x[0]) * __builtin_sqrtf(x[1]);
+// all 11 bits of a half.
+__device__ __forceinline__ float ds_scale(const AttnArgs& a) {
+    const float bound = __builtin_sqrtf(a.norms[0]) * __builtin_sqrtf(a.norms[1]);
     if (!(bound > 0.0f)) return 1.0f;
     int e;
     (void)__builtin_frexpf(bound, &e);                      // bound < 2^e
     return __builtin_ldexpf(1.0f, 13 - e);
 }
 
-// ---- staging ----------------------------------------------------------------------------
-
-template <int DP>
-using CT = CodeTile<kN, DP>;
-template <int DP>
-using HT = HalfTile<kN, DP>;
-
-// Four rows x eight columns of a tile that starts at row t0, rows below n.
-template <int DP, bool VEC>
-__device__ __forceinline__ void load_unit(uint2* w, const uint8_t* p, int64_t ts, int t0, int n, int D,
-                                          int u) {
-    const int row = t0 + HT<DP>::unit_row(u), col = HT<DP>::unit_col(u);
+// Entries that are not finite, of the rows noted in `bits` (row 0 of them is
+// token t0 of `src`), for the columns that see the row: f(d, r, code).
+template <int ND, typename SEES, typename F>
+__device__ __forceinline__ void add_noted(uint32_t bits, const uint8_t* src, int64_t ts, int t0, int D,
+                                          int h, SEES sees, F f) {
+    bits = __builtin_amdgcn_readfirstlane(bits);
+    while (__builtin_expect(bits != 0, 0)) {
+        int hh = h;
+        asm volatile("" : "+v"(hh));                        // nothing of this is hoisted
+        const int t = t0 + __builtin_ctz(bits);
+        bits &= bits - 1;
+        if (!sees(t)) continue;
+        const uint8_t* p = src + (int64_t)t * ts;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        w[r] = load_codes8<VEC>(p + (int64_t)(row + r) * ts, col, D, row + r < n);
-}
-// A unit as codes and transposed as halves; on partial tiles values that are
-// not finite leave the halves (0 x NaN must not reach a masked place) and
-// their rows are noted.
-template <int DP>
-__device__ __forceinline__ void store_unit(uint2* w, uint8_t* codes, uint8_t* halves, int u,
-                                           bool partial, uint32_t* bad) {
-    const int row = HT<DP>::unit_row(u), col = HT<DP>::unit_col(u);
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        *reinterpret_cast<uint2*>(codes + (row + r) * CT<DP>::kRow + col) = w[r];
-        if (partial) {
-            const uint32_t nx = nonfinite_bytes(w[r].x), ny = nonfinite_bytes(w[r].y);
-            if (nx | ny) {
-                atomicOr(bad + (row + r) / 32, 1u << ((row + r) % 32));
-                w[r].x &= ~nx;
-                w[r].y &= ~ny;
+            for (int r = 0; r < 16; ++r) {
+                const int col = 32 * d + 8 * (r / 4) + 4 * hh + r % 4;
+                const uint32_t c = col < D ? p[col] : 0u;
+                if ((c & 0x7Cu) == 0x7Cu) f(d, r, c);
             }
-        }
     }
-    HT<DP>::store(halves, u, w);
 }
 
 // ---- dq ------------------------------------------------------------------------------------
 
-// 128 rows (query, head of the group), 32 per wave; keys and values in LDS,
-// double-buffered.  dQ^T = K^T dS^T with dS^T's registers as the operand.
+// 128 rows (query, head of the group), 32 per wave; key tiles one ahead in
+// LDS.  dQ^T = K^T dS^T with dS^T's registers as the operand.
 template <int DP, bool VEC, int FG>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
-    constexpr int BM = 128, NC = DP / 32, ND = DP / 32;
-    constexpr int U = (kN / 4) * (DP / 8), KU = (U + kThreads - 1) / kThreads;
-    constexpr int VU = kN * (DP / 16) / kThreads;
-    constexpr int kBuf = 2 * CT<DP>::kBytes + HT<DP>::kBytes;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuf];
-    __shared__ uint32_t bad[3][2];
-    __shared__ float red[8];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+    using I = KeyImage<DP>;
+    constexpr int BM = 128, N = I::N, NC = DP / 32, ND = DP / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int l31 = lane & 31, h = lane >> 5;
     const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
     int tile;
-    const int s = slot_owner(a.cu_q, a.S, a.Tq, G, BM, blockIdx.x / a.Hkv, tile);
-    const Seq sq = load_seq(a, s);
+    const Seq sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, G, BM, blockIdx.x / a.Hkv, tile));
     const int64_t nrows = (int64_t)sq.nq * G;
     const int ntiles = (int)((nrows + BM - 1) / BM);
     if (tile >= ntiles) return;
@@ -200,18 +97,19 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
         return (int)(n < 0 ? 0 : n);
     };
     const int lim = live ? limit(row) : 0;
-    const int64_t last = row0 + BM < nrows ? row0 + BM - 1 : nrows - 1;
-    const int lim_lo = limit(row0), lim_hi = limit(last);
-    const int64_t wl = row0 + 32 * wave + 31 < nrows ? row0 + 32 * wave + 31 : nrows - 1;
-    const int wave_hi = row0 + 32 * wave < nrows ? limit(wl) : 0;
-    const int t1 = (lim_hi + kN - 1) / kN;
+    const int lim_lo = limit(row0), lim_hi = limit(row0 + BM < nrows ? row0 + BM - 1 : nrows - 1);
+    const int64_t w0 = row0 + 32 * wave;
+    const int wave_hi = w0 < nrows ? limit(w0 + 31 < nrows ? w0 + 31 : nrows - 1) : 0;
+    const int first = (int)(sq.k0 / N), j00 = (int)((int64_t)first * N - sq.k0);
+    const int t1 = lim_hi > 0 ? (lim_hi - j00 + N - 1) / N : 0;
+    const uint8_t* image = a.key_image + ((int64_t)hk * a.key_tiles + first) * I::kBytes;
+    if (t1 > 0) image_to_lds<I::kBytes, 4>(image, lds, wave, lane);
 
     const int64_t tq = sq.q0 + i;
     const int hq = hk * G + g;
     const uint8_t* qp = a.q.p + tq * a.q.ts + (int64_t)hq * a.q.hs;
     const uint8_t* ep = a.e.p + tq * a.e.ts + (int64_t)hq * a.e.hs;
     const uint8_t* kp = a.k.p + sq.k0 * a.k.ts + (int64_t)hk * a.k.hs;
-    const uint8_t* vp = a.v.p + sq.k0 * a.v.ts + (int64_t)hk * a.v.hs;
     const Widen widen;
     const float c2 = __uint_as_float(in_vgpr(__float_as_uint(a.c2)));
     v8h qf[NC][2], ef[NC][2];
@@ -224,7 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
         ef[c][0] = widen(w.x, w.y);
         ef[c][1] = widen(w.z, w.w);
     }
-    const float sigma = ds_scale(a, red);
+    const float sigma = ds_scale(a);
     float lse2 = INFINITY, delta = 0.0f;                    // a row that sees nothing: p = 0
     if (lim > 0) {
         lse2 = a.lse[(int64_t)hq * a.Tq + tq] * kAttnLog2e;
@@ -238,102 +136,51 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-
-    uint2 ku[KU][4];
-    uint4 vu[VU];
-    auto load = [&](int t) {
-#pragma unroll
-        for (int u = 0; u < KU; ++u)
-            if (U % kThreads == 0 || tid + u * kThreads < U)
-                load_unit<DP, VEC>(ku[u], kp, a.k.ts, t * kN, sq.nk, a.D, tid + u * kThreads);
-#pragma unroll
-        for (int u = 0; u < VU; ++u) {
-            const int id = tid + u * kThreads, r = t * kN + id / (DP / 16), col = id % (DP / 16) * 16;
-            vu[u] = load_codes16<VEC>(vp + (int64_t)r * a.v.ts, col, a.D, r < sq.nk);
-        }
-    };
-    auto is_partial = [&](int t) { return (t + 1) * kN > lim_lo || (t + 1) * kN > sq.nk; };
-    auto store = [&](int t, uint8_t* buf, uint32_t* badw) {
-        const bool partial = is_partial(t);
-#pragma unroll
-        for (int u = 0; u < KU; ++u)
-            if (U % kThreads == 0 || tid + u * kThreads < U)
-                store_unit<DP>(ku[u], buf, buf + 2 * CT<DP>::kBytes, tid + u * kThreads, partial, badw);
-#pragma unroll
-        for (int u = 0; u < VU; ++u) {
-            const int id = tid + u * kThreads, r = id / (DP / 16), col = id % (DP / 16) * 16;
-            *reinterpret_cast<uint4*>(buf + CT<DP>::kBytes + r * CT<DP>::kRow + col) = vu[u];
-        }
-    };
-
-    if (tid < 6) bad[tid / 2][tid % 2] = 0u;
-    __syncthreads();
-    if (t1 > 0) {
-        load(0);
-        store(0, lds, bad[0]);
-    }
-    __syncthreads();
     for (int t = 0; t < t1; ++t) {
-        const int b = t & 1, q = t % 3, j0 = t * kN;
-        if (t + 1 < t1) load(t + 1);
-        if (j0 < wave_hi) {
-            const uint8_t* kl = lds + b * kBuf;
-            const uint8_t* vl = kl + CT<DP>::kBytes;
-            const uint8_t* kt_ = vl + CT<DP>::kBytes;
-            const bool partial = is_partial(t);
+        const uint8_t* buf = lds + (t & 1) * I::kBytes;
+        image_barrier();
+        if (t + 1 < t1)
+            image_to_lds<I::kBytes, 4>(image + (int64_t)(t + 1) * I::kBytes,
+                                       lds + ((t + 1) & 1) * I::kBytes, wave, lane);
+        const int j0 = j00 + t * N;
+        if (j0 >= wave_hi) continue;
+        const bool partial = j0 < 0 || j0 + N > lim_lo;
 #pragma unroll
-            for (int kt = 0; kt < kN / 32; ++kt) {
-                v16f st = zero, dp = zero;
+        for (int kt = 0; kt < N / 32; ++kt) {
+            v16f st = zero, dp = zero;
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    uint4 w = CT<DP>::frag(kl, 32 * kt + l31, c, h);
-                    st = mfma_half(widen(w.x, w.y), qf[c][0], st);
-                    st = mfma_half(widen(w.z, w.w), qf[c][1], st);
-                    w = CT<DP>::frag(vl, 32 * kt + l31, c, h);
-                    dp = mfma_half(widen(w.x, w.y), ef[c][0], dp);
-                    dp = mfma_half(widen(w.z, w.w), ef[c][1], dp);
-                }
-                float ds[16];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r], c2, -lse2));
-                    ds[r] = p * __builtin_fmaf(dp[r], sg, -delta);
-                }
-                if (partial) {
-                    const int rel = lim - j0 - 32 * kt - 4 * h;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (8 * (r / 4) + r % 4 >= rel) ds[r] = 0.0f;
-                }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const v8h f = to_half8(ds + 8 * u);
-#pragma unroll
-                    for (int d = 0; d < ND; ++d)
-                        o[d] = mfma_half(HT<DP>::frag(kt_, 32 * d + l31, 2 * kt + u, h), f, o[d]);
-                }
-                if (partial) {
-                    // keys that are not finite, for the rows that see them
-                    uint32_t bw = bad[q][kt];
-                    while (bw) {
-                        const int key = j0 + 32 * kt + __builtin_ctz(bw);
-                        bw &= bw - 1;
-                        const uint8_t* kr = kp + (int64_t)key * a.k.ts;
-#pragma unroll
-                        for (int d = 0; d < ND; ++d)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) {
-                                const int col = 32 * d + 8 * (r / 4) + 4 * h + r % 4;
-                                const uint32_t c = key < lim && col < a.D ? kr[col] : 0u;
-                                if ((c & 0x7Cu) == 0x7Cu) o[d][r] = __uint_as_float(kF32NaN);
-                            }
-                    }
-                }
+            for (int c = 0; c < NC; ++c) {
+                uint4 w = I::CT::frag(buf, 32 * kt + l31, c, h);
+                st = mfma_half(widen(w.x, w.y), qf[c][0], st);
+                st = mfma_half(widen(w.z, w.w), qf[c][1], st);
+                w = I::CT::frag(buf + I::kV, 32 * kt + l31, c, h);
+                dp = mfma_half(widen(w.x, w.y), ef[c][0], dp);
+                dp = mfma_half(widen(w.z, w.w), ef[c][1], dp);
             }
+            float ds[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r], c2, -lse2));
+                ds[r] = p * __builtin_fmaf(dp[r], sg, -delta);
+            }
+            if (partial) {
+                int key = j0 + 32 * kt + 4 * h;
+                asm volatile("" : "+v"(key));               // a branch: no selects on whole tiles
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if ((uint32_t)(key + 8 * (r / 4) + r % 4) >= (uint32_t)lim) ds[r] = 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const v8h f = to_half8(ds + 8 * u);
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    o[d] = mfma_half(I::HT::frag(buf + I::kT, 32 * d + l31, 2 * kt + u, h), f, o[d]);
+            }
+            add_noted<ND>(reinterpret_cast<const uint32_t*>(buf + I::kNoted)[kt], kp, a.k.ts, j0 + 32 * kt,
+                          a.D, h, [&](int key) { return (uint32_t)key < (uint32_t)lim; },
+                          [&](int d, int r, uint32_t) { o[d][r] = __uint_as_float(kF32NaN); });
         }
-        if (tid < 2) bad[(q + 2) % 3][tid] = 0u;
-        if (t + 1 < t1) store(t + 1, lds + (b ^ 1) * kBuf, bad[(q + 1) % 3]);
-        __syncthreads();
     }
     if (!live) return;
     const float f = a.sm_scale / sigma * a.grad_scale;
@@ -351,239 +198,196 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
 
 // ---- dk and dv --------------------------------------------------------------------------------
 
-// 32 KT keys per wave; the queries and errors of the group's heads stream
-// through LDS.  dV^T = E^T P and dK^T = Q^T dS with P's and dS's registers as
-// the operands.
-template <int DP, int KT, bool VEC, int FG>
-__global__ __launch_bounds__(kThreads, KT == 1 ? 2 : 1) void attn_dkv_kernel(AttnArgs a) {
-    constexpr int BN = 128 * KT, NC = DP / 32, ND = DP / 32;
-    constexpr int U = (kN / 4) * (DP / 8), NU = 2 * U / kThreads;
-    constexpr int kBuf = 2 * CT<DP>::kBytes + 2 * HT<DP>::kBytes;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuf];
-    __shared__ __attribute__((aligned(16))) float rows[2][2][kN];   // lse and delta of a tile
-    __shared__ uint32_t bad[3][2][2];
-    __shared__ float red[8];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+// 128 keys of a sequence, 32 per wave; the queries and errors of the group's
+// heads stream through LDS in tiles of 32.  dV^T = E^T P and dK^T = Q^T dS with
+// P's and dS's registers as the operands.  SPLIT: gridDim.y workgroups share a
+// tile's steps (every gridDim.y-th each) and leave FP32 sums in the workspace.
+template <int DP, bool VEC, int FG, bool SPLIT>
+__global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
+    using I = QueryImage<DP>;
+    constexpr int BN = 128, N = I::N, NC = DP / 32, ND = DP / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int l31 = lane & 31, h = lane >> 5;
     const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
     int tile;
-    const int s = slot_owner(a.cu_k, a.S, a.Tk, 1, BN, blockIdx.x / a.Hkv, tile);
-    const Seq sq = load_seq(a, s);
+    const Seq sq = load_seq(a, slot_owner(a.cu_k, a.S, a.Tk, 1, BN, blockIdx.x / a.Hkv, tile));
     if ((int64_t)tile * BN >= sq.nk) return;
-    const int off = sq.nk - sq.nq, key0 = tile * BN;
-    const int wave0 = key0 + 32 * KT * wave;
+    const int off = sq.nk - sq.nq, key0 = tile * BN, wave0 = key0 + 32 * wave, j = wave0 + l31;
     const int key_hi = key0 + BN < sq.nk ? key0 + BN - 1 : sq.nk - 1;
-    // query i sees key j iff i >= j - off
+    // query i sees key j iff i >= j - off; [lo, nq) see this lane's key
     const int first = a.causal && key0 - off > 0 ? key0 - off : 0;
-    const int tq0 = first / kN, ntq = (sq.nq + kN - 1) / kN - tq0, steps = ntq > 0 ? ntq * G : 0;
+    const int lo = a.causal && j - off > 0 ? j - off : 0;
+    const uint32_t seen_by = sq.nq > lo ? (uint32_t)(sq.nq - lo) : 0u;
     const int wave_lo = a.causal ? wave0 - off : 0;         // the wave's first key's first query
-    const int wg_all = a.causal ? key_hi - off : 0;         // from here on every key is seen
+    const int all_lo = a.causal && key_hi - off > 0 ? key_hi - off : 0;   // from here on every key is seen
+    // tiles of the packed queries that hold some of [q0 + first, q0 + nq)
+    const int ta = (int)((sq.q0 + first) / N), tb = (int)((sq.q0 + sq.nq + N - 1) / N);
+    const int ntq = first < sq.nq ? tb - ta : 0, steps = ntq * G;
+    const int n0 = SPLIT ? blockIdx.y : 0, dn = SPLIT ? gridDim.y : 1;
+    auto issue = [&](int n, int b) {
+        const int hq = hk * G + n / ntq, t = ta + n % ntq;
+        image_to_lds<I::kBytes, 4>(a.query_image + ((int64_t)hq * a.query_tiles + t) * I::kBytes,
+                                   lds + b * I::kBytes, wave, lane);
+    };
+    if (n0 < steps) issue(n0, 0);
 
-    const uint8_t* kp = a.k.p + sq.k0 * a.k.ts + (int64_t)hk * a.k.hs;
-    const uint8_t* vp = a.v.p + sq.k0 * a.v.ts + (int64_t)hk * a.v.hs;
+    const uint8_t* kp = a.k.p + (sq.k0 + j) * a.k.ts + (int64_t)hk * a.k.hs;
+    const uint8_t* vp = a.v.p + (sq.k0 + j) * a.v.ts + (int64_t)hk * a.v.hs;
     const Widen widen;
     const float c2 = __uint_as_float(in_vgpr(__float_as_uint(a.c2)));
-    v8h kf[KT][NC][2], vf[KT][NC][2];
+    v8h kf[NC][2];
+    uint4 vf[NC];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-        const int j = wave0 + 32 * kt + l31;
+    for (int c = 0; c < NC; ++c) {
+        const uint4 w = load_codes16<VEC>(kp, 32 * c + 16 * h, a.D, j < sq.nk);
+        kf[c][0] = widen(w.x, w.y);
+        kf[c][1] = widen(w.z, w.w);
+        vf[c] = load_codes16<VEC>(vp, 32 * c + 16 * h, a.D, j < sq.nk);
+    }
+    const float sigma = ds_scale(a);
+    // p is held times 2^15, dS times sigma: p (dP - delta) sigma 2^-15
+    const float sg = __uint_as_float(in_vgpr(__float_as_uint(__builtin_ldexpf(sigma, -kAttnPUp))));
+
+    v16f dk[ND], dv[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
+    const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    int b = 0;
+    for (int n = n0; n < steps; n += dn, b ^= 1) {
+        image_barrier();
+        if (n + dn < steps) issue(n + dn, b ^ 1);
+        const int i0 = (int)((int64_t)(ta + n % ntq) * N - sq.q0);
+        if (i0 + N - 1 < wave_lo) continue;                 // no row sees a key of the wave
+        const bool partial = i0 < all_lo || i0 + N > sq.nq;
+        // opaque in every step: the compiler otherwise hoists the widened values
+        // out of the loop, past the register budget
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            asm volatile("" : "+v"(vf[c].x), "+v"(vf[c].y), "+v"(vf[c].z), "+v"(vf[c].w));
+        const uint8_t* buf = lds + b * I::kBytes;
+        // dp starts from -delta
+        v16f st = zero, dp;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float4 x = *reinterpret_cast<const float4*>(buf + I::delta(2 * q + h));
+            dp[4 * q] = x.x;
+            dp[4 * q + 1] = x.y;
+            dp[4 * q + 2] = x.z;
+            dp[4 * q + 3] = x.w;
+        }
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            uint4 w = load_codes16<VEC>(kp + (int64_t)j * a.k.ts, 32 * c + 16 * h, a.D, j < sq.nk);
-            kf[kt][c][0] = widen(w.x, w.y);
-            kf[kt][c][1] = widen(w.z, w.w);
-            w = load_codes16<VEC>(vp + (int64_t)j * a.v.ts, 32 * c + 16 * h, a.D, j < sq.nk);
-            vf[kt][c][0] = widen(w.x, w.y);
-            vf[kt][c][1] = widen(w.z, w.w);
+            uint4 w = I::CT::frag(buf, l31, c, h);
+            st = mfma_half(widen(w.x, w.y), kf[c][0], st);
+            st = mfma_half(widen(w.z, w.w), kf[c][1], st);
+            w = I::CT::frag(buf + I::kE, l31, c, h);
+            dp = mfma_half(widen(w.x, w.y), widen(vf[c].x, vf[c].y), dp);
+            dp = mfma_half(widen(w.z, w.w), widen(vf[c].z, vf[c].w), dp);
         }
-    }
-    const float sigma = ds_scale(a, red);
-    // p is held times 2^15, dS times sigma: p (dP - delta) sigma 2^-15
-    const float sg = __uint_as_float(in_vgpr(__float_as_uint(__builtin_ldexpf(sigma, -kPUp))));
-
-    v16f dk[KT][ND], dv[KT][ND];
+        float p[16], ds[16];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+        for (int q = 0; q < 4; ++q) {
+            const float4 x = *reinterpret_cast<const float4*>(buf + I::lse(2 * q + h));
+            const float l[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dk[kt][d][r] = dv[kt][d][r] = 0.0f;
-    const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-
-    uint2 st_[NU][4];
-    float rowv = 0.0f;
-    // step n: head n / ntq of the group, query tile tq0 + n % ntq
-    auto head = [&](int n) { return hk * G + n / ntq; };
-    auto tile_of = [&](int n) { return tq0 + n % ntq; };
-    auto load = [&](int n) {
-        const int hq = head(n), t0 = tile_of(n) * kN;
-#pragma unroll
-        for (int k = 0; k < NU; ++k) {
-            const int u = (tid + k * kThreads) % U;
-            const bool is_e = tid + k * kThreads >= U;      // uniform in a wave
-            const uint8_t* p = is_e ? a.e.p + sq.q0 * a.e.ts + (int64_t)hq * a.e.hs
-                                    : a.q.p + sq.q0 * a.q.ts + (int64_t)hq * a.q.hs;
-            load_unit<DP, VEC>(st_[k], p, is_e ? a.e.ts : a.q.ts, t0, sq.nq, a.D, u);
-        }
-        if (tid < 2 * kN) {
-            // rows that see no key, or past the last one: p = 0
-            const int i = t0 + tid % kN;
-            const bool ok = i < sq.nq && (!a.causal || i + off >= 0);
-            const float* src = (tid < kN ? a.lse : a.delta) + (int64_t)hq * a.Tq + sq.q0 + i;
-            rowv = ok ? *src : tid < kN ? INFINITY : 0.0f;
-        }
-    };
-    auto is_partial = [&](int n) { return tile_of(n) * kN < wg_all; };
-    auto store = [&](int n, int b, uint32_t(*badw)[2]) {
-        uint8_t* buf = lds + b * kBuf;
-        const bool partial = is_partial(n);
-#pragma unroll
-        for (int k = 0; k < NU; ++k) {
-            const int u = (tid + k * kThreads) % U, is_e = tid + k * kThreads >= U;
-            store_unit<DP>(st_[k], buf + is_e * CT<DP>::kBytes,
-                           buf + 2 * CT<DP>::kBytes + is_e * HT<DP>::kBytes, u, partial, badw[is_e]);
-        }
-        if (tid < kN) rows[b][0][tid] = rowv * kAttnLog2e - (float)kPUp;
-        else if (tid < 2 * kN) rows[b][1][tid - kN] = rowv * sg;
-    };
-
-    if (tid < 12) bad[tid / 4][tid / 2 % 2][tid % 2] = 0u;
-    __syncthreads();
-    if (steps > 0) {
-        load(0);
-        store(0, 0, bad[0]);
-    }
-    __syncthreads();
-    for (int n = 0; n < steps; ++n) {
-        const int b = n & 1, q = n % 3, i0 = tile_of(n) * kN;
-        if (n + 1 < steps) load(n + 1);
-        const uint8_t* ql = lds + b * kBuf;
-        const uint8_t* el = ql + CT<DP>::kBytes;
-        const uint8_t* qt = el + CT<DP>::kBytes;
-        const uint8_t* et = qt + HT<DP>::kBytes;
-        const bool partial = is_partial(n);
-#pragma unroll
-        for (int u = 0; u < kN / 32; ++u) {
-            if (i0 + 32 * u + 31 < wave_lo) continue;       // no row sees a key of the wave
-            v16f st[KT], dp[KT];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) st[kt] = dp[kt] = zero;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const uint4 w = CT<DP>::frag(ql, 32 * u + l31, c, h);
-                const uint4 x = CT<DP>::frag(el, 32 * u + l31, c, h);
-                const v8h w0 = widen(w.x, w.y), w1 = widen(w.z, w.w);
-                const v8h x0 = widen(x.x, x.y), x1 = widen(x.z, x.w);
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    st[kt] = mfma_half(w0, kf[kt][c][0], st[kt]);
-                    st[kt] = mfma_half(w1, kf[kt][c][1], st[kt]);
-                    dp[kt] = mfma_half(x0, vf[kt][c][0], dp[kt]);
-                    dp[kt] = mfma_half(x1, vf[kt][c][1], dp[kt]);
-                }
-            }
-            const float* lr = rows[b][0] + 32 * u + 4 * h;
-            const float* dr = rows[b][1] + 32 * u + 4 * h;
-            v8h pf[KT][2], sf[KT][2];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                float p[16], ds[16];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    p[r] = __builtin_amdgcn_exp2f(
-                        __builtin_fmaf(st[kt][r], c2, -lr[8 * (r / 4) + r % 4]));
-                    ds[r] = p[r] * __builtin_fmaf(dp[kt][r], sg, -dr[8 * (r / 4) + r % 4]);
-                }
-                if (partial) {
-                    // row i0 + 32 u + 4 h + x is seen iff that >= key - off
-                    const int rel = wave0 + 32 * kt + l31 - off - i0 - 32 * u - 4 * h;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (8 * (r / 4) + r % 4 < rel) p[r] = ds[r] = 0.0f;
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    pf[kt][t] = to_half8(p + 8 * t);
-                    sf[kt][t] = to_half8(ds + 8 * t);
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const v8h ef = HT<DP>::frag(et, 32 * d + l31, 2 * u + t, h);
-                    const v8h qf = HT<DP>::frag(qt, 32 * d + l31, 2 * u + t, h);
-#pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) {
-                        dv[kt][d] = mfma_half(ef, pf[kt][t], dv[kt][d]);
-                        dk[kt][d] = mfma_half(qf, sf[kt][t], dk[kt][d]);
-                    }
-                }
-            if (partial) {
-                // queries (0) and errors (1) that are not finite, for the keys they see
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    uint32_t bw = bad[q][w][u];
-                    while (bw) {
-                        const int i = i0 + 32 * u + __builtin_ctz(bw);
-                        bw &= bw - 1;
-                        const AttnRows& src = w ? a.e : a.q;
-                        const uint8_t* r_ = src.p + (sq.q0 + i) * src.ts + (int64_t)head(n) * src.hs;
-#pragma unroll
-                        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                                for (int r = 0; r < 16; ++r) {
-                                    const int col = 32 * d + 8 * (r / 4) + 4 * h + r % 4;
-                                    const bool sees = wave0 + 32 * kt + l31 <= i + off;
-                                    const uint32_t c = sees && col < a.D ? r_[col] : 0u;
-                                    if ((c & 0x7Cu) != 0x7Cu) continue;
-                                    if (w) dv[kt][d][r] += fp8_to_f32<0>(c);
-                                    else dk[kt][d][r] = __uint_as_float(kF32NaN);
-                                }
-                    }
-                }
+            for (int r = 0; r < 4; ++r) {
+                p[4 * q + r] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[4 * q + r], c2, -l[r]));
+                ds[4 * q + r] = p[4 * q + r] * (dp[4 * q + r] * sg);
             }
         }
-        if (tid < 4) bad[(q + 2) % 3][tid / 2][tid % 2] = 0u;
-        if (n + 1 < steps) store(n + 1, b ^ 1, bad[(q + 1) % 3]);
-        __syncthreads();
+        if (partial) {
+            int i = i0 + 4 * h - lo;
+            asm volatile("" : "+v"(i));                     // a branch: no selects on whole tiles
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if ((uint32_t)(i + 8 * (r / 4) + r % 4) >= seen_by) p[r] = ds[r] = 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const v8h pf = to_half8(p + 8 * t), sf = to_half8(ds + 8 * t);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                dv[d] = mfma_half(I::HT::frag(buf + I::kET, 32 * d + l31, t, h), pf, dv[d]);
+                dk[d] = mfma_half(I::HT::frag(buf + I::kQT, 32 * d + l31, t, h), sf, dk[d]);
+            }
+        }
+        const uint32_t* noted = reinterpret_cast<const uint32_t*>(buf + I::kNoted);
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(noted[0] | noted[1]) != 0, 0)) {
+            const int hq = hk * G + n / ntq;
+            auto sees = [&](int i) { return (uint32_t)(i - lo) < seen_by; };
+            add_noted<ND>(noted[0], a.q.p + sq.q0 * a.q.ts + (int64_t)hq * a.q.hs, a.q.ts, i0, a.D, h, sees,
+                          [&](int d, int r, uint32_t) { dk[d][r] = __uint_as_float(kF32NaN); });
+            add_noted<ND>(noted[1], a.e.p + sq.q0 * a.e.ts + (int64_t)hq * a.e.hs, a.e.ts, i0, a.D, h, sees,
+                          [&](int d, int r, uint32_t c) { dv[d][r] += fp8_to_f32<0>(c); });
+        }
     }
-    const float fk = a.sm_scale / sigma * a.grad_scale;
-    const float fv = __builtin_ldexpf(a.grad_scale, -kPUp);
+    if (j >= sq.nk) return;
+    const float fk = a.sm_scale / sigma * a.grad_scale, fv = __builtin_ldexpf(a.grad_scale, -kAttnPUp);
+    const int64_t t = sq.k0 + j;
+    float* part = SPLIT ? a.parts + (((int64_t)blockIdx.y * a.Tk + t) * a.Hkv + hk) * (2 * DP) : nullptr;
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-        const int j = wave0 + 32 * kt + l31;
-        if (j >= sq.nk) continue;
-        const int64_t t = sq.k0 + j;
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+        for (int q = 0; q < 4; ++q) {
+            float x[4], y[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float x[4], y[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[r] = dk[kt][d][4 * q + r] * fk;
-                    y[r] = dv[kt][d][4 * q + r] * fv;
-                }
-                const int col = 32 * d + 8 * q + 4 * h;
+            for (int r = 0; r < 4; ++r) {
+                x[r] = dk[d][4 * q + r] * fk;
+                y[r] = dv[d][4 * q + r] * fv;
+            }
+            const int col = 32 * d + 8 * q + 4 * h;
+            if constexpr (SPLIT) {
+                *reinterpret_cast<float4*>(part + col) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4*>(part + DP + col) = make_float4(y[0], y[1], y[2], y[3]);
+            } else {
                 write4<FG>(a.dk, t * a.dk_ts + (int64_t)hk * a.dk_hs, col, a.D, x);
                 write4<FG>(a.dv, t * a.dv_ts + (int64_t)hk * a.dv_hs, col, a.D, y);
             }
+        }
+}
+
+// Sums the partial dk and dv in their order: four entries a thread.  A token of
+// no sequence is not written.
+template <int DP, int FG>
+__global__ __launch_bounds__(kThreads) void attn_dkv_join_kernel(AttnArgs a) {
+    constexpr int kPer = 2 * DP / 4;                        // threads per (token, head)
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, rows = a.Tk * a.Hkv;
+    const int64_t row = id / kPer;
+    const int c = (int)(id % kPer) * 4, col = c % DP;
+    if (row >= rows || col >= a.D) return;
+    const int64_t t = row / a.Hkv, hk = row % a.Hkv;
+    if (t < clamp_to(a.cu_k[0], a.Tk) || t >= clamp_to(a.cu_k[a.S], a.Tk)) return;
+    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int z = 0; z < a.splits; ++z) {
+        const float4 p = *reinterpret_cast<const float4*>(a.parts + (z * rows + row) * (2 * DP) + c);
+        x[0] += p.x;
+        x[1] += p.y;
+        x[2] += p.z;
+        x[3] += p.w;
     }
+    if (c < DP) write4<FG>(a.dk, t * a.dk_ts + hk * a.dk_hs, col, a.D, x);
+    else write4<FG>(a.dv, t * a.dv_ts + hk * a.dv_hs, col, a.D, x);
 }
 
 template <int DP, bool VEC, int FG>
 void launch(const AttnArgs& a, hipStream_t stream) {
-    const int G = a.Hq / a.Hkv;
     const dim3 block(kThreads);
     if (a.Tq > 0)
         hipLaunchKernelGGL((attn_dq_kernel<DP, VEC, FG>),
-                           dim3((unsigned)(a.Hkv * slots(a.S, a.Tq, G, 128))), block, 0, stream, a);
-    if (a.Tk > 0) {
-        constexpr int KT = 1;
-        hipLaunchKernelGGL((attn_dkv_kernel<DP, KT, VEC, FG>),
-                           dim3((unsigned)(a.Hkv * slots(a.S, a.Tk, 1, 128 * KT))), block, 0, stream, a);
+                           dim3((unsigned)(a.Hkv * slots(a.S, a.Tq, a.Hq / a.Hkv, 128))), block, 0,
+                           stream, a);
+    if (a.Tk == 0) return;
+    const dim3 grid((unsigned)(a.Hkv * slots(a.S, a.Tk, 1, 128)), (unsigned)a.splits);
+    if (a.splits > 1) {
+        hipLaunchKernelGGL((attn_dkv_kernel<DP, VEC, FG, true>), grid, block, 0, stream, a);
+        const int64_t items = a.Tk * a.Hkv * (2 * DP / 4);
+        hipLaunchKernelGGL((attn_dkv_join_kernel<DP, FG>), dim3((unsigned)((items + kThreads - 1) / kThreads)),
+                           block, 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((attn_dkv_kernel<DP, VEC, FG, false>), grid, block, 0, stream, a);
     }
 }
 template <int DP, bool VEC>
@@ -594,13 +398,45 @@ void launch_fmt(const AttnArgs& a, int grad_format, hipStream_t stream) {
 
 }  // namespace
 
-void attn_bwd_launch(AttnArgs a, int grad_format, bool vec, hipStream_t stream) {
-    const int64_t rows = a.Tq * a.Hq + a.Tk * a.Hkv, blocks = (rows + 63) / 64;
-    a.norm_count = (int)(blocks < kAttnNorms ? blocks : kAttnNorms);
-    const dim3 grid((unsigned)a.norm_count), block(kThreads);
-    if (vec) hipLaunchKernelGGL(attn_prepare_kernel<true>, grid, block, 0, stream, a);
-    else hipLaunchKernelGGL(attn_prepare_kernel<false>, grid, block, 0, stream, a);
-    if (a.D <= 64) {
+AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int64_t max_k, int64_t Hq,
+                          int64_t Hkv, int64_t D) {
+    AttnBwdPlan p = {};
+    p.DP = D <= 64 ? 64 : 128;
+    const auto up = [](int64_t n) { return (size_t)((n + 15) / 16 * 16); };
+    p.key_tiles = image_tiles(Tk, 64);
+    p.query_tiles = image_tiles(Tq, 32);
+    p.norms = 0;
+    p.delta = up((4 + p.key_tiles * Hkv) * 4);
+    p.key_image = p.delta + up(Hq * Tq * 4);
+    p.query_image = p.key_image + (size_t)(p.key_tiles * Hkv) *
+                                      (p.DP == 64 ? KeyImage<64>::kBytes : KeyImage<128>::kBytes);
+    p.parts = p.query_image + (size_t)(p.query_tiles * Hq) *
+                                  (p.DP == 64 ? QueryImage<64>::kBytes : QueryImage<128>::kBytes);
+    // the steps of a key tile are shared out where the tiles leave CUs idle
+    const int64_t G = Hkv ? Hq / Hkv : 1, tiles = slots(S, Tk, 1, 128);
+    const int64_t some = S * ((max_k + 127) / 128), groups = (tiles < some ? tiles : some) * Hkv;
+    const int64_t steps = (max_q + 31) / 32 * G, want = 4 * (int64_t)device_cus();
+    int64_t n = groups > 0 && 2 * groups <= want ? want / groups : 1;
+    if (n > steps / 16) n = steps / 16;
+    if (n > 16) n = 16;
+    p.splits = n > 1 ? (int)n : 1;
+    p.bytes = p.parts + (p.splits > 1 ? (size_t)p.splits * Tk * Hkv * 2 * p.DP * 4 : 0);
+    return p;
+}
+
+void attn_bwd_launch(AttnArgs a, const AttnBwdPlan& p, int grad_format, bool vec, void* workspace,
+                     hipStream_t stream) {
+    uint8_t* w = static_cast<uint8_t*>(workspace);
+    a.norms = reinterpret_cast<float*>(w + p.norms);
+    a.delta = reinterpret_cast<float*>(w + p.delta);
+    a.key_image = w + p.key_image;
+    a.query_image = w + p.query_image;
+    a.parts = reinterpret_cast<float*>(w + p.parts);
+    a.key_tiles = p.key_tiles;
+    a.query_tiles = p.query_tiles;
+    a.splits = p.splits;
+    attn_bwd_image_launch(a, vec, p.DP, stream);
+    if (p.DP == 64) {
         if (vec) launch_fmt<64, true>(a, grad_format, stream);
         else launch_fmt<64, false>(a, grad_format, stream);
     } else {

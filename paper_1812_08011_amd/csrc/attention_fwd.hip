@@ -3,8 +3,8 @@
 // A workgroup owns a tile of rows -- (query, query head of a group) pairs, the
 // heads of a group beside each other, so that one pass over a key head's keys
 // and values serves them all -- and streams key tiles through LDS.
-#include "attn_mfma.h"
 #include "attn_fwd.h"
+#include "attn_image.h"
 
 namespace fp8t {
 namespace {
@@ -84,82 +84,44 @@ __device__ __forceinline__ void store_v(Stage<DP, NT>& s, uint8_t* lds, int tid,
     }
 }
 
-// KW = 1: 128 rows, 32 per wave, every wave walks all key tiles (shared in
-// LDS, double-buffered).  KW = 4: 32 rows, each wave walks every fourth key
-// tile by itself and the waves' results are joined in LDS -- for calls with
-// few rows, where the keys are what there is to share out.
-// SPLIT: the key tiles are shared out over gridDim.y workgroups, whose partial
-// results go to the workspace.
-template <int DP, int KW, bool VEC, bool SPLIT>
-__global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnSplit sp) {
-    constexpr int NT = kThreads / KW, BM = 128 / KW;
-    constexpr int NB = KW == 1 ? 2 : 4;                     // LDS buffers: double, or one per wave
-    constexpr int kBN = attn_keys(DP);
-    constexpr int NC = DP / 32, ND = DP / 32, NK = kBN / 32;
-    using CT = CodeTile<kBN, DP>;
-    using HT = HalfTile<kBN, DP>;
-    __shared__ __attribute__((aligned(16))) uint8_t ks[KW == 1 ? NB * CT::kBytes : 16];
-    __shared__ __attribute__((aligned(16))) uint8_t vs[NB * HT::kBytes];
-    __shared__ uint32_t bad[4][NK];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
-    const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
-    int tile;
-    const int s = slot_owner(a.cu_q, a.S, a.Tq, G, BM, blockIdx.x / a.Hkv, tile);
-    const Seq sq = load_seq(a, s);
-    const int64_t nrows = (int64_t)sq.nq * G;
-    const int ntiles = (int)((nrows + BM - 1) / BM);
-    if (tile >= ntiles) return;
-    tile = ntiles - 1 - tile;                               // the longest first
-    const int64_t row0 = (int64_t)tile * BM, row = row0 + (KW == 1 ? 32 * wave : 0) + l31;
-    const bool live = row < nrows;
-    const int i = live ? (int)(row / G) : 0, g = live ? (int)(row % G) : 0;
-    const int off = sq.nk - sq.nq;
-    // keys [0, lim) are seen by this lane's row; the tile's first and last row
-    auto limit = [&](int64_t r) {
-        const int64_t n = a.causal ? r / G + 1 + off : sq.nk;
-        return (int)(n < 0 ? 0 : n);
-    };
-    const int lim = live ? limit(row) : 0;
-    const int64_t last = row0 + BM < nrows ? row0 + BM - 1 : nrows - 1;
-    const int lim_lo = limit(row0), lim_hi = limit(last);
-    int wave_hi = lim_hi;
-    if (KW == 1) {
-        const int64_t wl = row0 + 32 * wave + 31 < nrows ? row0 + 32 * wave + 31 : nrows - 1;
-        wave_hi = row0 + 32 * wave < nrows ? limit(wl) : 0;
-    }
-    int t0 = 0, t1 = (lim_hi + kBN - 1) / kBN;
-    if (SPLIT) {
-        t0 = blockIdx.y * sp.per;
-        if (blockIdx.y + 1 < gridDim.y && t0 + sp.per < t1) t1 = t0 + sp.per;
-    }
-
-    const int64_t tq = sq.q0 + i;
-    const int hq = hk * G + g;
-    const uint8_t* qp = a.q.p + tq * a.q.ts + (int64_t)hq * a.q.hs;
-    const uint8_t* kp = a.k.p + sq.k0 * a.k.ts + (int64_t)hk * a.k.hs;
-    const uint8_t* vp = a.v.p + sq.k0 * a.v.ts + (int64_t)hk * a.v.hs;
-    const Widen widen;
-    const float c2 = __uint_as_float(in_vgpr(__float_as_uint(a.c2)));
+// What a wave holds of its 32 rows: queries, running sums, statistics.  Lane
+// half h of column l % 32 holds rows 8 g + 4 h + r of every result.
+template <int DP>
+struct FwdRows {
+    static constexpr int N = attn_keys(DP), NC = DP / 32, ND = DP / 32, NK = N / 32;
+    using HT = HalfTile<N, DP>;
+    Widen widen;
     v8h qf[NC][2];
+    v16f o[ND];
+    float ref, mu, l, c2;              // reference; the same, 0 before the first key; sum; scale
+
+    template <bool VEC>
+    __device__ __forceinline__ void init(const AttnArgs& a, const uint8_t* q, int h, bool live) {
+        c2 = __uint_as_float(in_vgpr(__float_as_uint(a.c2)));
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const uint4 w = load_codes16<VEC>(qp, 32 * c + 16 * h, a.D, live);
-        qf[c][0] = widen(w.x, w.y);
-        qf[c][1] = widen(w.z, w.w);
+        for (int c = 0; c < NC; ++c) {
+            const uint4 w = load_codes16<VEC>(q, 32 * c + 16 * h, a.D, live);
+            qf[c][0] = widen(w.x, w.y);
+            qf[c][1] = widen(w.z, w.w);
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+        ref = -INFINITY;
+        mu = l = 0.0f;
     }
 
-    v16f o[ND];
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-    float ref = -INFINITY, mu = 0.0f, l = 0.0f;             // reference; the same, 0 before the first key
-    const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-
-    // One key tile: kf(kt, c) gives the key operand, vl the values in LDS; next()
-    // runs once the key operands are used up.
-    auto step = [&](auto kf, const uint8_t* vl, int j0, bool partial, const uint32_t* badw,
-                    auto next) {
+    // One key tile whose first key is j0 (negative: keys of another sequence
+    // first): kf(kt, c) gives the key operand, vl the values in LDS; next() runs
+    // once the key operands are used up.  partial: some row does not see some
+    // key; a row sees keys [0, lim).  noted: the keys whose values are not
+    // finite, v their sequence's first value.
+    template <typename KF, typename NEXT>
+    __device__ __forceinline__ void step(KF kf, const uint8_t* vl, int j0, int lim, bool partial, int h,
+                                         int l31, const uint32_t* noted, const uint8_t* v, int64_t v_ts,
+                                         int D, NEXT next) {
+        const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
         v16f st[NK];
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt) {
@@ -173,12 +135,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
         }
         next();
         if (partial) {
-            const int rel = lim - j0 - 4 * h;
+            int key = j0 + 4 * h;
+            asm volatile("" : "+v"(key));                   // a branch: no selects on whole tiles
 #pragma unroll
             for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (32 * kt + 8 * (r / 4) + r % 4 >= rel) st[kt][r] = -INFINITY;
+                    if ((uint32_t)(key + 32 * kt + 8 * (r / 4) + r % 4) >= (uint32_t)lim)
+                        st[kt][r] = -INFINITY;
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -213,33 +177,160 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
                     o[d] = mfma_half(HT::frag(vl, 32 * d + l31, 2 * kt + t, h), pf, o[d]);
             }
         }
-        if (partial) {
-            // keys whose values are not finite, for the rows that see them
 #pragma unroll
-            for (int kt = 0; kt < NK; ++kt) {
-                uint32_t b = badw[kt];
-                while (b) {
-                    const int key = j0 + 32 * kt + __builtin_ctz(b);
-                    b &= b - 1;
-                    const uint8_t* vr = vp + (int64_t)key * a.v.ts;
+        for (int kt = 0; kt < NK; ++kt) {
+            uint32_t b = __builtin_amdgcn_readfirstlane(noted[kt]);
+            while (__builtin_expect(b != 0, 0)) {
+                int hh = h;
+                asm volatile("" : "+v"(hh));                // nothing of this is hoisted
+                const int key = j0 + 32 * kt + __builtin_ctz(b);
+                b &= b - 1;
+                if ((uint32_t)key >= (uint32_t)lim) continue;
+                const uint8_t* vr = v + (int64_t)key * v_ts;
 #pragma unroll
-                    for (int d = 0; d < ND; ++d)
+                for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int col = 32 * d + 8 * (r / 4) + 4 * h + r % 4;
-                            const uint32_t c = key < lim && col < a.D ? vr[col] : 0u;
-                            if ((c & 0x7Cu) == 0x7Cu) o[d][r] += fp8_to_f32<0>(c);
-                        }
-                }
+                    for (int r = 0; r < 16; ++r) {
+                        const int col = 32 * d + 8 * (r / 4) + 4 * hh + r % 4;
+                        const uint32_t c = col < D ? vr[col] : 0u;
+                        if ((c & 0x7Cu) == 0x7Cu) o[d][r] += fp8_to_f32<0>(c);
+                    }
             }
         }
-    };
+    }
+};
+
+// A workgroup's tile of rows and this lane's row in it.
+template <int BM, int RW>              // rows, rows from one wave to the next (0: the same rows)
+struct FwdTile {
+    Seq sq;
+    int64_t row0, row, nrows, tq;
+    int hk, hq, lim, lim_lo, lim_hi, wave_hi;
+    bool live;
+    // false: nothing to do.  Row r sees keys [0, limit(r)); the longest tiles
+    // come first.
+    __device__ __forceinline__ bool init(const AttnArgs& a, int wave, int l31) {
+        hk = blockIdx.x % a.Hkv;
+        const int G = a.Hq / a.Hkv;
+        int tile;
+        sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, G, BM, blockIdx.x / a.Hkv, tile));
+        nrows = (int64_t)sq.nq * G;
+        const int ntiles = (int)((nrows + BM - 1) / BM);
+        if (tile >= ntiles) return false;
+        row0 = (int64_t)(ntiles - 1 - tile) * BM;
+        row = row0 + RW * wave + l31;
+        live = row < nrows;
+        const int i = live ? (int)(row / G) : 0, off = sq.nk - sq.nq;
+        auto limit = [&](int64_t r) {
+            const int64_t n = a.causal ? r / G + 1 + off : sq.nk;
+            return (int)(n < 0 ? 0 : n);
+        };
+        lim = live ? limit(row) : 0;
+        lim_lo = limit(row0);
+        lim_hi = limit(row0 + BM < nrows ? row0 + BM - 1 : nrows - 1);
+        const int64_t w0 = row0 + RW * wave;
+        wave_hi = w0 < nrows ? limit(w0 + 31 < nrows ? w0 + 31 : nrows - 1) : 0;
+        tq = sq.q0 + i;
+        hq = hk * G + (live ? (int)(row % G) : 0);
+        return true;
+    }
+};
+
+template <int DP, int BM, bool SPLIT>
+__device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& sp,
+                                            const FwdTile<BM, BM == 128 ? 32 : 0>& t,
+                                            const FwdRows<DP>& x, float ref, float l, int h) {
+    if (!t.live) return;
+    if constexpr (SPLIT) {
+        const int64_t part = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+        const int64_t pr = part * BM + (t.row - t.row0);
+        float* po = sp.o + pr * DP;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<float4*>(po + 32 * d + 8 * q + 4 * h) = make_float4(
+                    x.o[d][4 * q], x.o[d][4 * q + 1], x.o[d][4 * q + 2], x.o[d][4 * q + 3]);
+        if (h == 0) sp.ml[pr] = make_float2(ref, l);
+    } else {
+        attn_write_row<DP>(a, t.tq, t.hq, t.lim, ref, l, h, [&](int d, int r) { return x.o[d][r]; });
+    }
+}
+
+// 128 rows, 32 per wave; key tiles come from their image by direct loads into
+// LDS, one tile ahead.
+template <int DP, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(kThreads, 2) void attn_fwd_image_kernel(AttnArgs a, AttnSplit sp) {
+    using I = FwdImage<DP>;
+    constexpr int N = I::N;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int l31 = lane & 31, h = lane >> 5;
+    FwdTile<128, 32> t;
+    if (!t.init(a, wave, l31)) return;
+    // tiles of the packed keys that hold some of [k0, k0 + lim_hi)
+    const int first = (int)(t.sq.k0 / N), j00 = (int)((int64_t)first * N - t.sq.k0);
+    int t0 = 0, t1 = t.lim_hi > 0 ? (t.lim_hi - j00 + N - 1) / N : 0;
+    if (SPLIT) {
+        t0 = blockIdx.y * sp.per;
+        if (blockIdx.y + 1 < gridDim.y && t0 + sp.per < t1) t1 = t0 + sp.per;
+    }
+    const uint8_t* image = a.key_image + ((int64_t)t.hk * a.key_tiles + first) * I::kBytes;
+    const uint8_t* vp = a.v.p + t.sq.k0 * a.v.ts + (int64_t)t.hk * a.v.hs;
+    if (t0 < t1) image_to_lds<I::kBytes, 4>(image + (int64_t)t0 * I::kBytes, lds, wave, lane);
+    FwdRows<DP> x;
+    x.template init<VEC>(a, a.q.p + t.tq * a.q.ts + (int64_t)t.hq * a.q.hs, h, t.live);
+    for (int n = t0; n < t1; ++n) {
+        const uint8_t* buf = lds + ((n - t0) & 1) * I::kBytes;
+        image_barrier();
+        if (n + 1 < t1)
+            image_to_lds<I::kBytes, 4>(image + (int64_t)(n + 1) * I::kBytes,
+                                       lds + ((n + 1 - t0) & 1) * I::kBytes, wave, lane);
+        const int j0 = j00 + n * N;
+        if (j0 >= t.wave_hi) continue;
+        x.step([&](int kt, int c) { return I::CT::frag(buf, 32 * kt + l31, c, h); }, buf + I::kV, j0, t.lim,
+               j0 < 0 || j0 + N > t.lim_lo, h, l31, reinterpret_cast<const uint32_t*>(buf + I::kNoted), vp,
+               a.v.ts, a.D, []() {});
+    }
+    const float l = both_halves(x.l, Add());
+    finish_rows<DP, 128, SPLIT>(a, sp, t, x, x.ref, l, h);
+}
+
+// KW = 1: 128 rows, 32 per wave, every wave walks all key tiles (shared in
+// LDS, double-buffered).  KW = 4: 32 rows, each wave walks every fourth key
+// tile by itself and the waves' results are joined in LDS -- for calls with
+// few rows, where the keys are what there is to share out.
+// SPLIT: the key tiles are shared out over gridDim.y workgroups, whose partial
+// results go to the workspace.
+template <int DP, int KW, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnSplit sp) {
+    constexpr int NT = kThreads / KW, BM = 128 / KW, kBN = attn_keys(DP);
+    constexpr int NB = KW == 1 ? 2 : 4;                     // LDS buffers: double, or one per wave
+    constexpr int NC = DP / 32, ND = DP / 32, NK = kBN / 32;
+    using CT = CodeTile<kBN, DP>;
+    using HT = HalfTile<kBN, DP>;
+    __shared__ __attribute__((aligned(16))) uint8_t ks[KW == 1 ? NB * CT::kBytes : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t vs[NB * HT::kBytes];
+    __shared__ uint32_t bad[4][NK];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
+    FwdTile<BM, KW == 1 ? 32 : 0> w;
+    if (!w.init(a, wave, l31)) return;
+    const Seq& sq = w.sq;
+    int t0 = 0, t1 = (w.lim_hi + kBN - 1) / kBN;
+    if (SPLIT) {
+        t0 = blockIdx.y * sp.per;
+        if (blockIdx.y + 1 < gridDim.y && t0 + sp.per < t1) t1 = t0 + sp.per;
+    }
+    const uint8_t* kp = a.k.p + sq.k0 * a.k.ts + (int64_t)w.hk * a.k.hs;
+    const uint8_t* vp = a.v.p + sq.k0 * a.v.ts + (int64_t)w.hk * a.v.hs;
+    FwdRows<DP> x;
+    x.template init<VEC>(a, a.q.p + w.tq * a.q.ts + (int64_t)w.hq * a.q.hs, h, w.live);
+    auto is_partial = [&](int t) { return (t + 1) * kBN > w.lim_lo; };
 
     Stage<DP, NT> sg;
     if constexpr (KW == 1) {
         if (tid < 4 * NK) bad[tid / NK][tid % NK] = 0u;
         __syncthreads();
-        auto is_partial = [&](int t) { return (t + 1) * kBN > lim_lo || (t + 1) * kBN > sq.nk; };
         if (t0 < t1) {
             load_k<DP, VEC>(sg, kp, a.k.ts, t0 * kBN, sq.nk, a.D, tid);
             load_v<DP, VEC>(sg, vp, a.v.ts, t0 * kBN, sq.nk, a.D, tid);
@@ -253,10 +344,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
                 load_k<DP, VEC>(sg, kp, a.k.ts, (t + 1) * kBN, sq.nk, a.D, tid);
                 load_v<DP, VEC>(sg, vp, a.v.ts, (t + 1) * kBN, sq.nk, a.D, tid);
             }
-            if (t * kBN < wave_hi) {
+            if (t * kBN < w.wave_hi) {
                 const uint8_t* kl = ks + b * CT::kBytes;
-                step([&](int kt, int c) { return CT::frag(kl, 32 * kt + l31, c, h); },
-                     vs + b * HT::kBytes, t * kBN, is_partial(t), bad[q], []() {});
+                x.step([&](int kt, int c) { return CT::frag(kl, 32 * kt + l31, c, h); },
+                       vs + b * HT::kBytes, t * kBN, w.lim, is_partial(t), h, l31, bad[q], vp, a.v.ts,
+                       a.D, []() {});
             }
             // noted keys: slot q is read here, the next one written, the one
             // read in the last step cleared
@@ -276,7 +368,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
                 const int j = t * kBN + 32 * kt + l31;
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
-                    kf[kt][c] = load_codes16<VEC>(kp + (int64_t)j * a.k.ts, 32 * c + 16 * h, a.D, j < sq.nk);
+                    kf[kt][c] = load_codes16<VEC>(kp + (int64_t)j * a.k.ts, 32 * c + 16 * h, a.D,
+                                                  j < sq.nk);
             }
             load_v<DP, VEC>(sg, vp, a.v.ts, t * kBN, sq.nk, a.D, lane);
         };
@@ -287,18 +380,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
         };
         if (t0 + wave < t1) load(t0 + wave);
         for (int t = t0 + wave; t < t1; t += KW) {
-            const bool partial = (t + 1) * kBN > lim_lo || (t + 1) * kBN > sq.nk;
             fence();
             if (lane < NK) bad[wave][lane] = 0u;
             fence();
-            store_v(sg, vl, lane, partial, bad[wave]);
+            store_v(sg, vl, lane, is_partial(t), bad[wave]);
             fence();
-            step([&](int kt, int c) { return kf[kt][c]; }, vl, t * kBN, partial, bad[wave], [&]() {
-                if (t + KW < t1) load(t + KW);
-            });
+            x.step([&](int kt, int c) { return kf[kt][c]; }, vl, t * kBN, w.lim, is_partial(t), h, l31,
+                   bad[wave], vp, a.v.ts, a.D, [&]() {
+                       if (t + KW < t1) load(t + KW);
+                   });
         }
     }
-    l = both_halves(l, Add());
+    float l = both_halves(x.l, Add()), ref = x.ref;
 
     if constexpr (KW > 1) {
         // join the waves: references first, then the scaled sums
@@ -311,21 +404,20 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
         __syncthreads();
         float m = refs[0][l31];
 #pragma unroll
-        for (int w = 1; w < KW; ++w) m = fmaxf(m, refs[w][l31]);
+        for (int v = 1; v < KW; ++v) m = fmaxf(m, refs[v][l31]);
         l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < KW; ++w)
-            l += refs[w][l31] == m ? ls[w][l31] : ls[w][l31] * exp2f(refs[w][l31] - m);
+        for (int v = 0; v < KW; ++v)
+            l += refs[v][l31] == m ? ls[v][l31] : ls[v][l31] * exp2f(refs[v][l31] - m);
         const float f = ref == m ? 1.0f : exp2f(ref - m);
-        // wave w's sums go through LDS as [d][lane] floats, 64 lanes at a time
-        float* xs = reinterpret_cast<float*>(vs);
+        float* xs = reinterpret_cast<float*>(vs);           // [wave - 1][register][lane]
         static_assert(NB * HT::kBytes >= 3 * ND * 16 * 64 * 4, "the joined waves' sums fit");
         if (wave) {
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    xs[(((wave - 1) * ND + d) * 16 + r) * 64 + lane] = o[d][r] * f;
+                    xs[(((wave - 1) * ND + d) * 16 + r) * 64 + lane] = x.o[d][r] * f;
         }
         __syncthreads();
         if (wave) return;
@@ -333,28 +425,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                float x = o[d][r] * f;
-                for (int w = 0; w < KW - 1; ++w) x += xs[((w * ND + d) * 16 + r) * 64 + lane];
-                o[d][r] = x;
+                float y = x.o[d][r] * f;
+                for (int v = 0; v < KW - 1; ++v) y += xs[((v * ND + d) * 16 + r) * 64 + lane];
+                x.o[d][r] = y;
             }
         ref = m;
     }
-
-    if (!live) return;
-    if constexpr (SPLIT) {
-        const int64_t part = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-        const int64_t pr = part * BM + (row - row0);
-        float* po = sp.o + pr * DP;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<float4*>(po + 32 * d + 8 * q + 4 * h) =
-                    make_float4(o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]);
-        if (h == 0) sp.ml[pr] = make_float2(ref, l);
-    } else {
-        attn_write_row<DP>(a, tq, hq, lim, ref, l, h, [&](int d, int r) { return o[d][r]; });
-    }
+    finish_rows<DP, BM, SPLIT>(a, sp, w, x, ref, l, h);
 }
 
 // Joins the partial results of a tile's key ranges, in their order: a wave per
@@ -403,41 +480,42 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSpl
         a.lse[(int64_t)hq * a.Tq + t] = lim > 0 ? kAttnLn2 * (m + log2f(l)) : -INFINITY;
 }
 
-template <int DP, int KW, bool VEC>
+template <int DP, bool VEC>
 void launch(const AttnArgs& a, const AttnFwdPlan& p, const AttnSplit& sp, hipStream_t stream) {
     const dim3 grid((unsigned)(a.Hkv * p.slots), (unsigned)p.splits), block(kThreads);
-    if (p.splits > 1) {
-        hipLaunchKernelGGL((attn_fwd_kernel<DP, KW, VEC, true>), grid, block, 0, stream, a, sp);
-        const unsigned rows = (unsigned)((p.max_rows + 3) / 4);
-        hipLaunchKernelGGL(attn_join_kernel<DP>, dim3(grid.x, rows), block, 0, stream, a, sp);
+    const bool split = p.splits > 1;
+    if (p.image) {
+        attn_fwd_image_launch(a, VEC, DP, stream);
+        if (split) hipLaunchKernelGGL((attn_fwd_image_kernel<DP, VEC, true>), grid, block, 0, stream, a, sp);
+        else hipLaunchKernelGGL((attn_fwd_image_kernel<DP, VEC, false>), grid, block, 0, stream, a, sp);
+    } else if (p.BM == 32) {
+        if (split) hipLaunchKernelGGL((attn_fwd_kernel<DP, 4, VEC, true>), grid, block, 0, stream, a, sp);
+        else hipLaunchKernelGGL((attn_fwd_kernel<DP, 4, VEC, false>), grid, block, 0, stream, a, sp);
     } else {
-        hipLaunchKernelGGL((attn_fwd_kernel<DP, KW, VEC, false>), grid, block, 0, stream, a, sp);
+        if (split) hipLaunchKernelGGL((attn_fwd_kernel<DP, 1, VEC, true>), grid, block, 0, stream, a, sp);
+        else hipLaunchKernelGGL((attn_fwd_kernel<DP, 1, VEC, false>), grid, block, 0, stream, a, sp);
     }
-}
-template <int DP>
-void launch_dp(const AttnArgs& a, const AttnFwdPlan& p, const AttnSplit& sp, bool vec,
-               hipStream_t stream) {
-    if (p.BM == 32) {
-        if (vec) launch<DP, 4, true>(a, p, sp, stream);
-        else launch<DP, 4, false>(a, p, sp, stream);
-    } else {
-        if (vec) launch<DP, 1, true>(a, p, sp, stream);
-        else launch<DP, 1, false>(a, p, sp, stream);
-    }
+    if (split)
+        hipLaunchKernelGGL(attn_join_kernel<DP>, dim3(grid.x, (unsigned)((p.BM + 3) / 4)), block, 0,
+                           stream, a, sp);
 }
 
 }  // namespace
 
 // Rows of 32 take the kernel that shares out the keys inside a workgroup; the
 // keys are shared out over workgroups where the rows alone leave CUs idle.
-AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t max_q, int64_t max_k, int64_t Hq,
+AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int64_t max_k, int64_t Hq,
                           int64_t Hkv, int64_t D) {
     AttnFwdPlan p = {};
     const int64_t G = Hkv ? Hq / Hkv : 1;
     p.DP = D <= 64 ? 64 : 128;
     p.BM = max_q * G <= 32 ? 32 : 128;
     p.slots = slots(S, Tq, G, p.BM);
-    p.max_rows = p.BM;
+    // images pay where many row tiles read them (measured below)
+    p.image = p.BM == 128 && max_q * G >= 1024;
+    const int64_t image = p.image ? image_tiles(Tk, attn_keys(p.DP)) * Hkv *
+                                        (p.DP == 64 ? FwdImage<64>::kBytes : FwdImage<128>::kBytes)
+                                  : 0;
     const int64_t tiles_q = (max_q * G + p.BM - 1) / p.BM;
     int64_t groups = p.slots < S * tiles_q ? p.slots : S * tiles_q;
     groups *= Hkv;
@@ -449,23 +527,31 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t max_q, int64_t max_k, i
     if (n > 64) n = 64;
     p.splits = n > 1 ? (int)n : 1;
     p.per = (int)((tiles_k + p.splits - 1) / p.splits);
-    p.bytes = p.splits > 1 ? (size_t)p.splits * p.slots * Hkv * p.BM * (p.DP * 4 + 8) : 0;
+    p.image_bytes = (size_t)image;
+    p.bytes = p.image_bytes +
+              (p.splits > 1 ? (size_t)p.splits * p.slots * Hkv * p.BM * (p.DP * 4 + 8) : 0);
     return p;
 }
 
-void attn_fwd_launch(const AttnArgs& a, const AttnFwdPlan& p, bool vec, void* workspace,
-                     hipStream_t stream) {
+void attn_fwd_launch(AttnArgs a, const AttnFwdPlan& p, bool vec, void* workspace, hipStream_t stream) {
     AttnSplit sp = {};
+    a.key_image = static_cast<uint8_t*>(workspace);
+    a.key_tiles = image_tiles(a.Tk, attn_keys(p.DP));
     if (p.splits > 1) {
         const int64_t rows = (int64_t)p.splits * p.slots * a.Hkv * p.BM;
-        sp.o = static_cast<float*>(workspace);
+        sp.o = reinterpret_cast<float*>(a.key_image + p.image_bytes);
         sp.ml = reinterpret_cast<float2*>(sp.o + rows * p.DP);
         sp.n = p.splits;
         sp.per = p.per;
         sp.BM = p.BM;
     }
-    if (p.DP == 64) launch_dp<64>(a, p, sp, vec, stream);
-    else launch_dp<128>(a, p, sp, vec, stream);
+    if (p.DP == 64) {
+        if (vec) launch<64, true>(a, p, sp, stream);
+        else launch<64, false>(a, p, sp, stream);
+    } else {
+        if (vec) launch<128, true>(a, p, sp, stream);
+        else launch<128, false>(a, p, sp, stream);
+    }
 }
 
 }  // namespace fp8t

@@ -1,18 +1,20 @@
-// The backward kernels' host side.
+// The backward kernels' plan.
 #pragma once
 
 #include "attn.h"
 
 namespace fp8t {
 
-// Workgroups of the kernel that takes the norms, each with a place for two.
-constexpr int kAttnNorms = 1024;
+struct AttnBwdPlan {
+    int DP, splits;                    // padded D; workgroups that share a key tile's queries
+    int64_t key_tiles, query_tiles;    // of the images
+    // byte offsets into the workspace, and its size
+    size_t norms, delta, key_image, query_image, parts, bytes;
+};
 
-// Workspace: delta (rounded up to 16 bytes), then the norms.
-inline size_t attn_delta_bytes(int64_t Hq, int64_t Tq) { return ((size_t)Hq * Tq * 4 + 15) / 16 * 16; }
-inline size_t attn_bwd_bytes(int64_t Hq, int64_t Tq) {
-    return attn_delta_bytes(Hq, Tq) + 2 * kAttnNorms * sizeof(float);
-}
-void attn_bwd_launch(AttnArgs a, int grad_format, bool vec, hipStream_t stream);
+AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int64_t max_k, int64_t Hq,
+                          int64_t Hkv, int64_t D);
+void attn_bwd_launch(AttnArgs a, const AttnBwdPlan& p, int grad_format, bool vec, void* workspace,
+                     hipStream_t stream);
 
 }  // namespace fp8t

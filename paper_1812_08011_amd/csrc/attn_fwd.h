@@ -5,14 +5,11 @@
 
 namespace fp8t {
 
-// Keys per tile: 256 threads stage a tile's values as one unit of 4 x 8 each.
-constexpr int attn_keys(int DP) { return DP == 64 ? 128 : 64; }
-
 struct AttnFwdPlan {
     int DP, BM, splits, per;           // padded D, rows per workgroup, key ranges and tiles in each
     int64_t slots;                     // row tiles of all sequences, empty ones included
-    int max_rows;
-    size_t bytes;                      // workspace
+    bool image;                        // keys and values through images
+    size_t image_bytes, bytes;         // workspace: images first, then partial results
 };
 
 struct AttnSplit {                     // partial results: rows x DP sums, (reference, sum)
@@ -21,9 +18,9 @@ struct AttnSplit {                     // partial results: rows x DP sums, (refe
     int n, per, BM;
 };
 
-AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t max_q, int64_t max_k, int64_t Hq,
-                          int64_t Hkv, int64_t D);
-void attn_fwd_launch(const AttnArgs& a, const AttnFwdPlan& p, bool vec, void* workspace,
+AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int64_t max_k,
+                          int64_t Hq, int64_t Hkv, int64_t D);
+void attn_fwd_launch(AttnArgs a, const AttnFwdPlan& p, bool vec, void* workspace,
                      hipStream_t stream);
 
 // One row's results from the two lanes that hold it: value(d, r) is entry 32 d

@@ -1,0 +1,237 @@
+// Builds the images (attn_image.h).  A workgroup builds one tile of one head in
+// LDS and writes it out 16 bytes a thread.
+#include "attn_image.h"
+
+namespace fp8t {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Four rows x eight columns of the tile that starts at token t0.
+template <int N, int DP, bool VEC>
+__device__ __forceinline__ void load_unit(uint2* w, const AttnRows& r, int64_t head, int64_t t0, int64_t T,
+                                          int D, int u) {
+    const int row = HalfTile<N, DP>::unit_row(u), col = HalfTile<N, DP>::unit_col(u);
+    const uint8_t* p = r.p + head * r.hs;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = load_codes8<VEC>(p + (t0 + row + i) * r.ts, col, D, t0 + row + i < T);
+}
+template <int N, int DP>
+__device__ __forceinline__ void store_codes(const uint2* w, uint8_t* lds, int u) {
+    const int row = HalfTile<N, DP>::unit_row(u), col = HalfTile<N, DP>::unit_col(u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint2*>(lds + (row + i) * CodeTile<N, DP>::kRow + col) = w[i];
+}
+// Transposed, without the values that are not finite, whose rows are noted.
+template <int N, int DP>
+__device__ __forceinline__ void store_halves(uint2* w, uint8_t* lds, int u, uint32_t* noted) {
+    const int row = HalfTile<N, DP>::unit_row(u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t nx = nonfinite_bytes(w[i].x), ny = nonfinite_bytes(w[i].y);
+        if (nx | ny) {
+            atomicOr(noted + (row + i) / 32, 1u << ((row + i) % 32));
+            w[i].x &= ~nx;
+            w[i].y &= ~ny;
+        }
+    }
+    HalfTile<N, DP>::store(lds, u, w);
+}
+template <int BYTES>
+__device__ __forceinline__ void write_image(const uint8_t* lds, uint8_t* dst) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < BYTES / 16; i += kThreads)
+        reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(lds)[i];
+}
+// Squared norm of 16 codes.
+__device__ __forceinline__ float norm16(uint4 w) {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    float n = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float x = fp8_to_f32<0>((v[i / 4] >> (8 * (i % 4))) & 0xFFu);
+        n = __builtin_fmaf(x, x, n);
+    }
+    return n;
+}
+__device__ __forceinline__ float block_max(float x, float* red) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
+
+template <int DP, bool VEC>
+__global__ __launch_bounds__(kThreads) void fwd_image_kernel(AttnArgs a) {
+    using I = FwdImage<DP>;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[I::kBytes];
+    const int tid = threadIdx.x, hk = blockIdx.x % a.Hkv, t = blockIdx.x / a.Hkv;
+    const int64_t t0 = (int64_t)t * I::N;
+    uint32_t* noted = reinterpret_cast<uint32_t*>(lds + I::kNoted);
+    if (tid < 4) noted[tid] = 0u;
+#pragma unroll
+    for (int u = 0; u < I::N * (DP / 16) / kThreads; ++u) {
+        const int id = tid + u * kThreads, row = id / (DP / 16), col = id % (DP / 16) * 16;
+        *reinterpret_cast<uint4*>(lds + row * I::CT::kRow + col) = load_codes16<VEC>(
+            a.k.p + (t0 + row) * a.k.ts + (int64_t)hk * a.k.hs, col, a.D, t0 + row < a.Tk);
+    }
+    uint2 w[4];
+    load_unit<I::N, DP, VEC>(w, a.v, hk, t0, a.Tk, a.D, tid);
+    __syncthreads();
+    store_halves<I::N, DP>(w, lds + I::kV, tid, noted);
+    write_image<I::kBytes>(lds, a.key_image + ((int64_t)hk * a.key_tiles + t) * I::kBytes);
+}
+
+// Also the largest squared norm of the values' finite rows, per workgroup, and
+// a zero for what the next kernel takes the maximum into.
+template <int DP, bool VEC>
+__global__ __launch_bounds__(kThreads) void key_image_kernel(AttnArgs a) {
+    using I = KeyImage<DP>;
+    constexpr int U = (I::N / 4) * (DP / 8), VU = I::N * (DP / 16) / kThreads;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[I::kBytes];
+    __shared__ float red[kThreads / 64];
+    const int tid = threadIdx.x;
+    if (blockIdx.x == 0 && tid < 2) a.norms[tid] = 0.0f;
+    if (a.key_tiles == 0) return;
+    const int hk = blockIdx.x % a.Hkv, t = blockIdx.x / a.Hkv;
+    const int64_t t0 = (int64_t)t * I::N;
+    uint32_t* noted = reinterpret_cast<uint32_t*>(lds + I::kNoted);
+    if (tid < 4) noted[tid] = 0u;
+    float top = 0.0f;
+#pragma unroll
+    for (int u = 0; u < VU; ++u) {
+        const int id = tid + u * kThreads, row = id / (DP / 16), col = id % (DP / 16) * 16;
+        const uint4 w = load_codes16<VEC>(a.v.p + (t0 + row) * a.v.ts + (int64_t)hk * a.v.hs, col, a.D,
+                                          t0 + row < a.Tk);
+        *reinterpret_cast<uint4*>(lds + I::kV + row * I::CT::kRow + col) = w;
+        float n = norm16(w);
+#pragma unroll
+        for (int d = DP / 32; d; d >>= 1) n += __shfl_xor(n, d);
+        if (n < INFINITY) top = fmaxf(top, n);
+    }
+    top = block_max(top, red);
+    if (tid == 0) a.norms[4 + blockIdx.x] = top;
+    uint2 w[4];
+    if (tid < U) {
+        load_unit<I::N, DP, VEC>(w, a.k, hk, t0, a.Tk, a.D, tid);
+        store_codes<I::N, DP>(w, lds, tid);
+        store_halves<I::N, DP>(w, lds + I::kT, tid, noted);
+    }
+    write_image<I::kBytes>(lds, a.key_image + ((int64_t)hk * a.key_tiles + t) * I::kBytes);
+}
+
+// Also delta = <e, o> of every row, and the largest squared norms of e's and
+// v's finite rows (maxima do not depend on the order of the atomics).
+template <int DP, bool VEC>
+__global__ __launch_bounds__(kThreads) void query_image_kernel(AttnArgs a, int vec_o) {
+    using I = QueryImage<DP>;
+    constexpr int U = (I::N / 4) * (DP / 8);
+    __shared__ __attribute__((aligned(16))) uint8_t lds[I::kBytes];
+    __shared__ float red[kThreads / 64];
+    const int tid = threadIdx.x, hq = blockIdx.x % a.Hq, t = blockIdx.x / a.Hq;
+    const int64_t t0 = (int64_t)t * I::N;
+    uint32_t* noted = reinterpret_cast<uint32_t*>(lds + I::kNoted);
+    if (tid < 4) noted[tid] = 0u;
+    __syncthreads();
+    if (tid < 2 * U) {
+        uint2 w[4];
+        const int is_e = tid >= U, u = tid % U;
+        load_unit<I::N, DP, VEC>(w, is_e ? a.e : a.q, hq, t0, a.Tq, a.D, u);
+        store_codes<I::N, DP>(w, lds + is_e * I::kE, u);
+        store_halves<I::N, DP>(w, lds + (is_e ? I::kET : I::kQT), u, noted + is_e);
+    }
+    __syncthreads();
+    // 16 lanes per row, 8 entries each
+    float top = 0.0f;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+        const int row = pass * 16 + tid / 16, d0 = tid % 16 * 8;
+        const bool live = t0 + row < a.Tq;
+        uint2 w = make_uint2(0, 0);
+        if (d0 < DP) w = *reinterpret_cast<const uint2*>(lds + I::kE + row * I::CT::kRow + d0);
+        const uint16_t* o = a.o + (t0 + row) * a.o_ts + (int64_t)hq * a.o_hs;
+        uint32_t oc[4] = {0, 0, 0, 0};
+        if (live && d0 < a.D) {
+            if (vec_o) {
+                const uint4 x = *reinterpret_cast<const uint4*>(o + d0);
+                oc[0] = x.x;
+                oc[1] = x.y;
+                oc[2] = x.z;
+                oc[3] = x.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (d0 + i < a.D) oc[i / 2] |= (uint32_t)o[d0 + i] << (16 * (i % 2));
+            }
+        }
+        float s = 0.0f, n = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e = fp8_to_f32<0>(((i < 4 ? w.x : w.y) >> (8 * (i % 4))) & 0xFFu);
+            s = __builtin_fmaf(e, fp16_to_f32((oc[i / 2] >> (16 * (i % 2))) & 0xFFFFu), s);
+            n = __builtin_fmaf(e, e, n);
+        }
+#pragma unroll
+        for (int d = 8; d; d >>= 1) {
+            s += __shfl_xor(s, d);
+            n += __shfl_xor(n, d);
+        }
+        if (n < INFINITY) top = fmaxf(top, n);
+        if (tid % 16 == 0) {
+            float l = INFINITY;                             // no such row, or one that sees nothing: p = 0
+            if (live) {
+                a.delta[(int64_t)hq * a.Tq + t0 + row] = s;
+                const float x = a.lse[(int64_t)hq * a.Tq + t0 + row];
+                if (x != -INFINITY) l = x * kAttnLog2e - (float)kAttnPUp;
+            }
+            *reinterpret_cast<float*>(lds + I::lse(row / 4) + 4 * (row % 4)) = l;
+            *reinterpret_cast<float*>(lds + I::delta(row / 4) + 4 * (row % 4)) = live ? -s : 0.0f;
+        }
+    }
+    top = block_max(top, red);
+    // non-negative floats order as their bits
+    if (tid == 0) atomicMax(reinterpret_cast<uint32_t*>(a.norms), __float_as_uint(top));
+    const int64_t nv = a.key_tiles * a.Hkv, i = (int64_t)blockIdx.x * kThreads + tid;
+    for (int64_t j = i; j < nv; j += (int64_t)gridDim.x * kThreads)
+        atomicMax(reinterpret_cast<uint32_t*>(a.norms) + 1, __float_as_uint(a.norms[4 + j]));
+    write_image<I::kBytes>(lds, a.query_image + ((int64_t)hq * a.query_tiles + t) * I::kBytes);
+}
+
+template <int DP, bool VEC>
+void launch_bwd(const AttnArgs& a, bool vec_o, hipStream_t stream) {
+    const int64_t nk = a.key_tiles * a.Hkv;
+    hipLaunchKernelGGL((key_image_kernel<DP, VEC>), dim3((unsigned)(nk ? nk : 1)), dim3(kThreads), 0,
+                       stream, a);
+    if (a.query_tiles)
+        hipLaunchKernelGGL((query_image_kernel<DP, VEC>), dim3((unsigned)(a.query_tiles * a.Hq)),
+                           dim3(kThreads), 0, stream, a, (int)vec_o);
+}
+
+}  // namespace
+
+void attn_fwd_image_launch(const AttnArgs& a, bool vec, int DP, hipStream_t stream) {
+    const dim3 grid((unsigned)(a.key_tiles * a.Hkv)), block(kThreads);
+    if (DP == 64) {
+        if (vec) hipLaunchKernelGGL((fwd_image_kernel<64, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((fwd_image_kernel<64, false>), grid, block, 0, stream, a);
+    } else {
+        if (vec) hipLaunchKernelGGL((fwd_image_kernel<128, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((fwd_image_kernel<128, false>), grid, block, 0, stream, a);
+    }
+}
+
+void attn_bwd_image_launch(const AttnArgs& a, bool vec, int DP, hipStream_t stream) {
+    const bool vec_o = a.D % 8 == 0 && aligned(a.o, 16) && a.o_ts % 8 == 0 && a.o_hs % 8 == 0;
+    if (DP == 64) {
+        if (vec) launch_bwd<64, true>(a, vec_o, stream);
+        else launch_bwd<64, false>(a, vec_o, stream);
+    } else {
+        if (vec) launch_bwd<128, true>(a, vec_o, stream);
+        else launch_bwd<128, false>(a, vec_o, stream);
+    }
+}
+
+}  // namespace fp8t

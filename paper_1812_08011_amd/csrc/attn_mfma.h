@@ -121,11 +121,15 @@ struct CodeTile {
 
 // The same rows transposed as halves: row d holds N values in the k order
 // above, i.e. of every 16 the blocks of four 0, 2, 1, 3; 16-byte blocks are
-// swizzled by the row, so that neither the writers (eight octets of columns by
-// two blocks of four) nor the readers (32 rows) meet bank conflicts.
+// swizzled by the row, so that the readers (32 rows) meet no bank conflicts and
+// the writers (eight octets of columns by two blocks of four) none, or with N =
+// 32, whose rows have four blocks only, two-way ones.
 template <int N, int DP>
 struct HalfTile {
     static constexpr int kRow = 2 * N, kBytes = DP * kRow;
+    static __device__ __forceinline__ int swizzle(int d) {
+        return N == 32 ? ((d >> 1) ^ (d >> 3)) & 3 : (d ^ (d >> 3)) & 7;
+    }
     // units of 4 rows x 8 columns, NT threads
     template <int NT>
     static constexpr int units() { return (N / 4) * (DP / 8) / NT; }
@@ -147,13 +151,13 @@ struct HalfTile {
             uint2 o;
             o.x = __builtin_amdgcn_perm(w1, w0, sel);
             o.y = __builtin_amdgcn_perm(w3, w2, sel);
-            const int swz = block ^ ((d ^ (col >> 3)) & 7);
+            const int swz = block ^ swizzle(col + d);
             *reinterpret_cast<uint2*>(lds + (col + d) * kRow + swz * 16 + eight) = o;
         }
     }
     // Left operand of instruction t (16 rows): column d, lane half h.
     static __device__ __forceinline__ v8h frag(const uint8_t* lds, int d, int t, int h) {
-        const int swz = (2 * t + h) ^ ((d ^ (d >> 3)) & 7);
+        const int swz = (2 * t + h) ^ swizzle(d);
         return *reinterpret_cast<const v8h*>(lds + d * kRow + swz * 16);
     }
 };
