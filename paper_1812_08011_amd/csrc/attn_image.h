@@ -59,21 +59,29 @@ constexpr int kAttnPUp = 15;           // the backward kernels hold p times 2^15
 
 inline int64_t image_tiles(int64_t T, int N) { return (T + N - 1) / N; }
 
-// An image into LDS, shared out over WAVES waves; the caller waits.
-typedef __attribute__((address_space(1))) const void* gptr_t;
-typedef __attribute__((address_space(3))) void* lptr_t;
+// An image into LDS by direct loads, 1024 bytes a wave and instruction, shared
+// out over WAVES waves; the caller waits (image_barrier).  The instruction is
+// written out because the compiler, given its builtin, waits for every such
+// load in flight before any later LDS read -- also of the other buffer.  It
+// has no result register; m0 holds the wave's LDS address.
+typedef __attribute__((address_space(3))) const void* lptr_t;
 template <int BYTES, int WAVES>
-__device__ __forceinline__ void image_to_lds(const uint8_t* src, uint8_t* lds, int wave, int lane) {
-    const uint8_t* s = src + lane * 16;
+__device__ __forceinline__ void image_to_lds(const uint8_t* src, const uint8_t* lds, int wave, int lane) {
+    constexpr int kPieces = BYTES / 1024;
+    const uint32_t to = (uint32_t)(uintptr_t)(lptr_t)lds;
 #pragma unroll
-    for (int c = 0; c < (BYTES / 1024 + WAVES - 1) / WAVES; ++c) {
+    for (int c = 0; c < (kPieces + WAVES - 1) / WAVES; ++c) {
         const int n = c * WAVES + wave;
-        if (BYTES / 1024 % WAVES == 0 || n < BYTES / 1024)
-            __builtin_amdgcn_global_load_lds((gptr_t)(s + n * 1024), (lptr_t)(lds + n * 1024), 16, 0, 0);
+        if ((c + 1) * WAVES <= kPieces || n < kPieces) {
+            const uint8_t* s = src + n * 1024;              // uniform
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                         :
+                         : "s"(to + (uint32_t)n * 1024u), "v"((uint32_t)lane * 16u), "s"(s)
+                         : "memory", "m0");
+        }
     }
 }
-// Waits for this wave's direct loads (the compiler does not see their LDS
-// writes), then for every wave.
+// Waits for this wave's direct loads, then for every wave.
 __device__ __forceinline__ void image_barrier() {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
