@@ -77,13 +77,15 @@ __device__ __forceinline__ void add_noted(uint32_t bits, const uint8_t* src, int
 template <int DP, bool VEC, int FG>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
     using I = KeyImage<DP>;
-    constexpr int BM = 128, N = I::N, NC = DP / 32, ND = DP / 32;
+    constexpr int BM = kAttnRows, N = I::N, NC = DP / 32, ND = DP / 32;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int l31 = lane & 31, h = lane >> 5;
     const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
+    const int slot = ordered_slot(a.row_order, blockIdx.x / a.Hkv);
+    if (slot < 0) return;
     int tile;
-    const Seq sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, G, BM, blockIdx.x / a.Hkv, tile));
+    const Seq sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, G, BM, slot, tile));
     const int64_t nrows = (int64_t)sq.nq * G;
     const int ntiles = (int)((nrows + BM - 1) / BM);
     if (tile >= ntiles) return;
@@ -205,13 +207,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
 template <int DP, bool VEC, int FG, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
     using I = QueryImage<DP>;
-    constexpr int BN = 128, N = I::N, NC = DP / 32, ND = DP / 32;
+    constexpr int BN = kAttnDkvKeys, N = I::N, NC = DP / 32, ND = DP / 32;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int l31 = lane & 31, h = lane >> 5;
     const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
+    const int slot = ordered_slot(a.key_order, blockIdx.x / a.Hkv);
+    if (slot < 0) return;
     int tile;
-    const Seq sq = load_seq(a, slot_owner(a.cu_k, a.S, a.Tk, 1, BN, blockIdx.x / a.Hkv, tile));
+    const Seq sq = load_seq(a, slot_owner(a.cu_k, a.S, a.Tk, 1, BN, slot, tile));
     if ((int64_t)tile * BN >= sq.nk) return;
     const int off = sq.nk - sq.nq, key0 = tile * BN, wave0 = key0 + 32 * wave, j = wave0 + l31;
     const int key_hi = key0 + BN < sq.nk ? key0 + BN - 1 : sq.nk - 1;
@@ -377,10 +381,10 @@ void launch(const AttnArgs& a, hipStream_t stream) {
     const dim3 block(kThreads);
     if (a.Tq > 0)
         hipLaunchKernelGGL((attn_dq_kernel<DP, VEC, FG>),
-                           dim3((unsigned)(a.Hkv * slots(a.S, a.Tq, a.Hq / a.Hkv, 128))), block, 0,
+                           dim3((unsigned)(a.Hkv * slots(a.S, a.Tq, a.Hq / a.Hkv, kAttnRows))), block, 0,
                            stream, a);
     if (a.Tk == 0) return;
-    const dim3 grid((unsigned)(a.Hkv * slots(a.S, a.Tk, 1, 128)), (unsigned)a.splits);
+    const dim3 grid((unsigned)(a.Hkv * slots(a.S, a.Tk, 1, kAttnDkvKeys)), (unsigned)a.splits);
     if (a.splits > 1) {
         hipLaunchKernelGGL((attn_dkv_kernel<DP, VEC, FG, true>), grid, block, 0, stream, a);
         const int64_t items = a.Tk * a.Hkv * (2 * DP / 4);
@@ -410,11 +414,14 @@ AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     p.key_image = p.delta + up(Hq * Tq * 4);
     p.query_image = p.key_image + (size_t)(p.key_tiles * Hkv) *
                                       (p.DP == 64 ? KeyImage<64>::kBytes : KeyImage<128>::kBytes);
-    p.parts = p.query_image + (size_t)(p.query_tiles * Hq) *
+    p.order = p.query_image + (size_t)(p.query_tiles * Hq) *
                                   (p.DP == 64 ? QueryImage<64>::kBytes : QueryImage<128>::kBytes);
+    const int64_t row_slots = slots(S, Tq, Hkv ? Hq / Hkv : 1, kAttnRows);
+    p.key_order = p.order + (S > 1 ? up(row_slots * 4) : 0);
+    p.parts = p.key_order + (S > 1 ? up(slots(S, Tk, 1, kAttnDkvKeys) * 4) : 0);
     // the steps of a key tile are shared out where the tiles leave CUs idle
-    const int64_t G = Hkv ? Hq / Hkv : 1, tiles = slots(S, Tk, 1, 128);
-    const int64_t some = S * ((max_k + 127) / 128), groups = (tiles < some ? tiles : some) * Hkv;
+    const int64_t G = Hkv ? Hq / Hkv : 1, tiles = slots(S, Tk, 1, kAttnDkvKeys);
+    const int64_t some = S * ((max_k + kAttnDkvKeys - 1) / kAttnDkvKeys), groups = (tiles < some ? tiles : some) * Hkv;
     const int64_t steps = (max_q + 31) / 32 * G, want = 4 * (int64_t)device_cus();
     int64_t n = groups > 0 && 2 * groups <= want ? want / groups : 1;
     if (n > steps / 16) n = steps / 16;
@@ -435,6 +442,10 @@ void attn_bwd_launch(AttnArgs a, const AttnBwdPlan& p, int grad_format, bool vec
     a.key_tiles = p.key_tiles;
     a.query_tiles = p.query_tiles;
     a.splits = p.splits;
+    if (a.S > 1) {
+        a.row_order = reinterpret_cast<int*>(w + p.order);
+        a.key_order = reinterpret_cast<int*>(w + p.key_order);
+    }
     attn_bwd_image_launch(a, vec, p.DP, stream);
     if (p.DP == 64) {
         if (vec) launch_fmt<64, true>(a, grad_format, stream);

@@ -205,7 +205,7 @@ template <int BM, int RW>              // rows, rows from one wave to the next (
 struct FwdTile {
     Seq sq;
     int64_t row0, row, nrows, tq;
-    int hk, hq, lim, lim_lo, lim_hi, wave_hi;
+    int hk, hq, slot, lim, lim_lo, lim_hi, wave_hi;
     bool live;
     // false: nothing to do.  Row r sees keys [0, limit(r)); the longest tiles
     // come first.
@@ -213,7 +213,9 @@ struct FwdTile {
         hk = blockIdx.x % a.Hkv;
         const int G = a.Hq / a.Hkv;
         int tile;
-        sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, G, BM, blockIdx.x / a.Hkv, tile));
+        slot = ordered_slot(a.row_order, blockIdx.x / a.Hkv);
+        if (slot < 0) return false;
+        sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, G, BM, slot, tile));
         nrows = (int64_t)sq.nq * G;
         const int ntiles = (int)((nrows + BM - 1) / BM);
         if (tile >= ntiles) return false;
@@ -242,7 +244,7 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
                                             const FwdRows<DP>& x, float ref, float l, int h) {
     if (!t.live) return;
     if constexpr (SPLIT) {
-        const int64_t part = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+        const int64_t part = (int64_t)blockIdx.y * gridDim.x + (int64_t)t.slot * a.Hkv + t.hk;
         const int64_t pr = part * BM + (t.row - t.row0);
         float* po = sp.o + pr * DP;
 #pragma unroll
@@ -260,7 +262,7 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
 // 128 rows, 32 per wave; key tiles come from their image by direct loads into
 // LDS, one tile ahead.
 template <int DP, bool VEC, bool SPLIT>
-__global__ __launch_bounds__(kThreads, 2) void attn_fwd_image_kernel(AttnArgs a, AttnSplit sp) {
+__global__ __launch_bounds__(kThreads, 3) void attn_fwd_image_kernel(AttnArgs a, AttnSplit sp) {
     using I = FwdImage<DP>;
     constexpr int N = I::N;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
@@ -527,7 +529,8 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     if (n > 64) n = 64;
     p.splits = n > 1 ? (int)n : 1;
     p.per = (int)((tiles_k + p.splits - 1) / p.splits);
-    p.image_bytes = (size_t)image;
+    p.order = p.image && S > 1;
+    p.image_bytes = (size_t)image + (p.order ? (p.slots * 4 + 15) / 16 * 16 : 0);
     p.bytes = p.image_bytes +
               (p.splits > 1 ? (size_t)p.splits * p.slots * Hkv * p.BM * (p.DP * 4 + 8) : 0);
     return p;
@@ -537,6 +540,8 @@ void attn_fwd_launch(AttnArgs a, const AttnFwdPlan& p, bool vec, void* workspace
     AttnSplit sp = {};
     a.key_image = static_cast<uint8_t*>(workspace);
     a.key_tiles = image_tiles(a.Tk, attn_keys(p.DP));
+    if (p.image && p.order)
+        a.row_order = reinterpret_cast<int*>(a.key_image + p.image_bytes - (p.slots * 4 + 15) / 16 * 16);
     if (p.splits > 1) {
         const int64_t rows = (int64_t)p.splits * p.slots * a.Hkv * p.BM;
         sp.o = reinterpret_cast<float*>(a.key_image + p.image_bytes);

@@ -35,6 +35,10 @@ struct AttnArgs {
     uint8_t* key_image;
     uint8_t* query_image;
     int64_t key_tiles, query_tiles;
+    // tiles of rows and of keys, the longest first (attn_image.hip), -1 past the
+    // last; null: in the order of their slots
+    int* row_order;
+    int* key_order;
     float* parts;            // partial dk, dv: [part][token][head][2][padded D]
     int splits;
 };
@@ -82,6 +86,8 @@ __device__ __forceinline__ int slot_owner(const int64_t* cu, int S, int64_t T, i
     local = l < 0 ? INT32_MAX : (int)l;     // before the first sequence: empty
     return lo;
 }
+// The tile that a workgroup takes: the slot, and its sequence and place there.
+__device__ __forceinline__ int ordered_slot(const int* order, int n) { return order ? order[n] : n; }
 inline int64_t slots(int64_t S, int64_t T, int64_t mult, int64_t tile) {
     return S > 0 ? T * mult / tile + S : 0;
 }

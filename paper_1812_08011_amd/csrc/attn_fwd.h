@@ -8,8 +8,8 @@ namespace fp8t {
 struct AttnFwdPlan {
     int DP, BM, splits, per;           // padded D, rows per workgroup, key ranges and tiles in each
     int64_t slots;                     // row tiles of all sequences, empty ones included
-    bool image;                        // keys and values through images
-    size_t image_bytes, bytes;         // workspace: images first, then partial results
+    bool image, order;                 // keys and values through images; row tiles in an order
+    size_t image_bytes, bytes;         // workspace: images and order first, then partial results
 };
 
 struct AttnSplit {                     // partial results: rows x DP sums, (reference, sum)

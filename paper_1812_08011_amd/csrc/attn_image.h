@@ -87,6 +87,10 @@ __device__ __forceinline__ void image_barrier() {
     __syncthreads();
 }
 
+// Workgroup 0 or 1 of the kernels that build images writes an order of tiles, if
+// any; rows and keys per tile.
+constexpr int kAttnRows = 128, kAttnDkvKeys = 128;
+
 void attn_fwd_image_launch(const AttnArgs& a, bool vec, int DP, hipStream_t stream);
 void attn_bwd_image_launch(const AttnArgs& a, bool vec, int DP, hipStream_t stream);
 

@@ -64,11 +64,74 @@ __device__ __forceinline__ float block_max(float x, float* red) {
     return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
 }
 
+// Orders the tiles of all sequences by their work, the longest first (a
+// counting sort over 256 classes), so that no long tile starts last: with
+// sequences of many lengths in one batch the order of the slots leaves the
+// card waiting for the last long sequence.  Rows (KEYS false) or keys.  The
+// order inside a class is open; no result depends on it.
+template <bool KEYS>
+__device__ __forceinline__ void order_tiles(const AttnArgs& a, int* order) {
+    constexpr int kTile = KEYS ? kAttnDkvKeys : kAttnRows;
+    __shared__ int count[257];
+    __shared__ int top;
+    const int tid = threadIdx.x, G = a.Hq / a.Hkv;
+    const int64_t* cu = KEYS ? a.cu_k : a.cu_q;
+    const int64_t T = KEYS ? a.Tk : a.Tq, mult = KEYS ? 1 : G;
+    const int n = (int)(T * mult / kTile + a.S);
+    // keys that the tile's last row sees, or queries that see the tile's first
+    // key; -1: an empty slot
+    auto work = [&](int slot) {
+        int tile;
+        const Seq sq = load_seq(a, slot_owner(cu, a.S, T, mult, kTile, slot, tile));
+        const int64_t len = KEYS ? sq.nk : (int64_t)sq.nq * G, first = (int64_t)tile * kTile;
+        if (first >= len) return -1;
+        const int off = sq.nk - sq.nq;
+        if (KEYS) {
+            const int64_t lo = a.causal && first - off > 0 ? first - off : 0;
+            return lo < sq.nq ? (int)(sq.nq - lo) : 0;
+        }
+        // row tiles run backwards in their slots
+        const int64_t ntiles = (len + kTile - 1) / kTile, t = ntiles - 1 - tile;
+        const int64_t last = (t + 1) * kTile < len ? (t + 1) * kTile - 1 : len - 1;
+        const int64_t lim = a.causal ? last / G + 1 + off : sq.nk;
+        return lim > 0 ? (int)lim : 0;
+    };
+    for (int i = tid; i < 257; i += kThreads) count[i] = 0;
+    if (tid == 0) top = 1;
+    __syncthreads();
+    int most = 1;
+    for (int i = tid; i < n; i += kThreads) most = max(most, work(i));
+    atomicMax(&top, most);
+    __syncthreads();
+    const float per = 255.0f / (float)top;
+    auto place = [&](int w) { return w < 0 ? 256 : 255 - (int)((float)w * per); };
+    for (int i = tid; i < n; i += kThreads) atomicAdd(&count[place(work(i))], 1);
+    __syncthreads();
+    if (tid == 0) {
+        int sum = 0;
+        for (int i = 0; i < 257; ++i) {
+            const int c = count[i];
+            count[i] = sum;
+            sum += c;
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += kThreads) {
+        const int w = work(i);
+        order[atomicAdd(&count[place(w)], 1)] = w < 0 ? -1 : i;
+    }
+}
+
 template <int DP, bool VEC>
 __global__ __launch_bounds__(kThreads) void fwd_image_kernel(AttnArgs a) {
+    if (a.row_order && blockIdx.x == 0) {
+        order_tiles<false>(a, a.row_order);
+        return;
+    }
+    const int block = blockIdx.x - (a.row_order ? 1 : 0);
     using I = FwdImage<DP>;
     __shared__ __attribute__((aligned(16))) uint8_t lds[I::kBytes];
-    const int tid = threadIdx.x, hk = blockIdx.x % a.Hkv, t = blockIdx.x / a.Hkv;
+    const int tid = threadIdx.x, hk = block % a.Hkv, t = block / a.Hkv;
     const int64_t t0 = (int64_t)t * I::N;
     uint32_t* noted = reinterpret_cast<uint32_t*>(lds + I::kNoted);
     if (tid < 4) noted[tid] = 0u;
@@ -95,8 +158,14 @@ __global__ __launch_bounds__(kThreads) void key_image_kernel(AttnArgs a) {
     __shared__ float red[kThreads / 64];
     const int tid = threadIdx.x;
     if (blockIdx.x == 0 && tid < 2) a.norms[tid] = 0.0f;
+    if (a.row_order && blockIdx.x < 2) {
+        if (blockIdx.x == 0) order_tiles<false>(a, a.row_order);
+        else order_tiles<true>(a, a.key_order);
+        return;
+    }
     if (a.key_tiles == 0) return;
-    const int hk = blockIdx.x % a.Hkv, t = blockIdx.x / a.Hkv;
+    const int block = blockIdx.x - (a.row_order ? 2 : 0);
+    const int hk = block % a.Hkv, t = block / a.Hkv;
     const int64_t t0 = (int64_t)t * I::N;
     uint32_t* noted = reinterpret_cast<uint32_t*>(lds + I::kNoted);
     if (tid < 4) noted[tid] = 0u;
@@ -113,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void key_image_kernel(AttnArgs a) {
         if (n < INFINITY) top = fmaxf(top, n);
     }
     top = block_max(top, red);
-    if (tid == 0) a.norms[4 + blockIdx.x] = top;
+    if (tid == 0) a.norms[4 + block] = top;
     uint2 w[4];
     if (tid < U) {
         load_unit<I::N, DP, VEC>(w, a.k, hk, t0, a.Tk, a.D, tid);
@@ -192,17 +261,22 @@ __global__ __launch_bounds__(kThreads) void query_image_kernel(AttnArgs a, int v
         }
     }
     top = block_max(top, red);
-    // non-negative floats order as their bits
-    if (tid == 0) atomicMax(reinterpret_cast<uint32_t*>(a.norms), __float_as_uint(top));
+    // non-negative floats order as their bits; most workgroups find that their
+    // maximum is no news and leave the one address alone
+    auto raise = [&](int k, float x) {
+        uint32_t* p = reinterpret_cast<uint32_t*>(a.norms) + k;
+        const uint32_t u = __float_as_uint(x);
+        if (u > __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(p, u);
+    };
+    if (tid == 0) raise(0, top);
     const int64_t nv = a.key_tiles * a.Hkv, i = (int64_t)blockIdx.x * kThreads + tid;
-    for (int64_t j = i; j < nv; j += (int64_t)gridDim.x * kThreads)
-        atomicMax(reinterpret_cast<uint32_t*>(a.norms) + 1, __float_as_uint(a.norms[4 + j]));
+    for (int64_t j = i; j < nv; j += (int64_t)gridDim.x * kThreads) raise(1, a.norms[4 + j]);
     write_image<I::kBytes>(lds, a.query_image + ((int64_t)hq * a.query_tiles + t) * I::kBytes);
 }
 
 template <int DP, bool VEC>
 void launch_bwd(const AttnArgs& a, bool vec_o, hipStream_t stream) {
-    const int64_t nk = a.key_tiles * a.Hkv;
+    const int64_t nk = a.key_tiles * a.Hkv + (a.row_order ? 2 : 0);
     hipLaunchKernelGGL((key_image_kernel<DP, VEC>), dim3((unsigned)(nk ? nk : 1)), dim3(kThreads), 0,
                        stream, a);
     if (a.query_tiles)
@@ -213,7 +287,7 @@ void launch_bwd(const AttnArgs& a, bool vec_o, hipStream_t stream) {
 }  // namespace
 
 void attn_fwd_image_launch(const AttnArgs& a, bool vec, int DP, hipStream_t stream) {
-    const dim3 grid((unsigned)(a.key_tiles * a.Hkv)), block(kThreads);
+    const dim3 grid((unsigned)(a.key_tiles * a.Hkv + (a.row_order ? 1 : 0))), block(kThreads);
     if (DP == 64) {
         if (vec) hipLaunchKernelGGL((fwd_image_kernel<64, true>), grid, block, 0, stream, a);
         else hipLaunchKernelGGL((fwd_image_kernel<64, false>), grid, block, 0, stream, a);
