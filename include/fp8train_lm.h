@@ -183,8 +183,8 @@ size_t attn_bwd_fp8_workspace_size(int64_t S, int64_t Tq, int64_t Tk, int64_t ma
  * t (t_format F32 or FP16): N x k contiguous, 0 <= k <= 4096; w, loss: N
  * floats; g: N x V, g_ld >= V.  loss or g may be NULL, not both.  g may be z
  * itself (same format and stride); otherwise they must not overlap.
- * Errors: FP8T_EINVAL (negative size, V or N above 2^31 - 4097, k > 4096, tau
- * not positive and finite, unknown format, a stride too small, NULL pointer
+ * Errors: FP8T_EINVAL (negative size, N above 2^31 - 4097 or V above 2^31 - 16385, k > 4096, tau
+ * not from 2^-30 to 2^30, unknown format, a stride too small, NULL pointer
  * for non-empty data, no output); FP8T_EHIP.
  */
 int distill_loss(const void* z, int z_format, int64_t z_ld, const int64_t* idx, const void* t,

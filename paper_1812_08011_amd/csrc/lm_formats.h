@@ -33,6 +33,34 @@ __device__ __forceinline__ fmt_t<FMT> fmt_code(float x) {
     else return (uint8_t)f32_to_fp8(x);
 }
 
+// Two FP16 codes of finite values: exponent and significand moved into a
+// float's fields, whose bias is 96 higher, restored by an exact product (FP16's
+// subnormals are FP32 subnormals there).
+__device__ __forceinline__ float2 fp16_finite_pair(uint32_t w) {
+    const uint32_t lo = (uint32_t)((int32_t)(w << 16) >> 2) & 0x9FFFC000u;
+    const uint32_t hi = (uint32_t)((int32_t)w >> 2) & 0x9FFFC000u;
+    return make_float2(__uint_as_float(lo) * 0x1p96f, __uint_as_float(hi) * 0x1p96f);
+}
+// Bits 15 and 31: whether the codes of a word are Inf or NaN (exponent 63).
+__device__ __forceinline__ uint32_t fp16_nonfinite(uint32_t w) {
+    return (w & 0x7E007E00u) + 0x02000200u;
+}
+
+// Two FP16 codes of finite values below FP16's largest, rounded to nearest
+// even: the values times 2^-96 have FP16's exponent in a float's exponent
+// field, so 14 bits are rounded off.  (Below 2^-30 that product itself rounds,
+// at 2^-14 of FP16's step.)
+__device__ __forceinline__ uint32_t fp16_pair(float a, float b) {
+    uint32_t r[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t u = __float_as_uint((i ? b : a) * 0x1p-96f);
+        u += 0x1FFFu + ((u >> 14) & 1u);
+        r[i] = ((u >> 14) & 0x7FFFu) | ((u >> 16) & 0x8000u);
+    }
+    return r[0] | (r[1] << 16);
+}
+
 // Whether the rows of a T x H x D result with strides ts and hs are apart:
 // heads inside tokens or tokens inside heads.
 inline bool rows_apart(int64_t T, int64_t H, int64_t D, int64_t ts, int64_t hs) {
