@@ -61,6 +61,58 @@ __device__ __forceinline__ uint32_t fp16_pair(float a, float b) {
     return r[0] | (r[1] << 16);
 }
 
+// Eight consecutive elements at any address (rows start where they start), as
+// wide as the alignment of one element allows.
+template <int FMT>
+struct Eight;
+template <>
+struct Eight<FP8T_FMT_F32> {
+    typedef float v4 __attribute__((ext_vector_type(4), aligned(4)));
+    v4 a, b;
+};
+template <>
+struct Eight<FP8T_FMT_FP16> {
+    typedef uint32_t v4 __attribute__((ext_vector_type(4), aligned(2)));
+    v4 a;
+};
+template <>
+struct Eight<FP8T_FMT_FP8> {
+    typedef uint32_t v2 __attribute__((ext_vector_type(2), aligned(1)));
+    v2 a;
+};
+
+// Their values, and whether one is Inf or NaN (FP16).
+template <int FMT>
+__device__ __forceinline__ void values_of(const Eight<FMT>& e, bool special, float* x) {
+    if constexpr (FMT == FP8T_FMT_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = e.a[i];
+            x[4 + i] = e.b[i];
+        }
+    } else if constexpr (FMT == FP8T_FMT_FP8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = fp8_to_f32<0>((e.a[i / 4] >> (8 * (i % 4))) & 0xFFu);
+    } else if (__builtin_expect(special, 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = fp16_to_f32((e.a[i / 2] >> (16 * (i % 2))) & 0xFFFFu);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = fp16_finite_pair(e.a[i]);
+            x[2 * i] = p.x;
+            x[2 * i + 1] = p.y;
+        }
+    }
+}
+// Whether an element is Inf or NaN.
+template <int FMT>
+__device__ __forceinline__ bool special_in(const Eight<FMT>& e) {
+    if constexpr (FMT != FP8T_FMT_FP16) return false;
+    else
+        return ((fp16_nonfinite(e.a[0]) | fp16_nonfinite(e.a[1]) | fp16_nonfinite(e.a[2]) |
+                 fp16_nonfinite(e.a[3])) & 0x80008000u) != 0;
+}
 // Whether the rows of a T x H x D result with strides ts and hs are apart:
 // heads inside tokens or tokens inside heads.
 inline bool rows_apart(int64_t T, int64_t H, int64_t D, int64_t ts, int64_t hs) {

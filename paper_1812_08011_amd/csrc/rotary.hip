@@ -1,13 +1,17 @@
 // rotary_embed: pairs of a head's entries turned by position-dependent angles.
 //
-// A workgroup takes a few tokens at a time: their cosines and sines go to LDS
-// once and serve every head, then the threads walk the tokens' pairs.
+// HBM-bound.  A thread owns eight pairs of one token and walks heads with
+// their cosines and sines in registers, so that the angles cost little next to
+// the codes; eight consecutive elements move with one load or store at any
+// address.  A head's entries past R are units of sixteen that are only
+// converted.
 #include "lm_formats.h"
 
 namespace fp8t {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kAcross = 1 << 20;   // workgroups along a grid's first dimension
 
 struct RotaryArgs {
     const void* x;
@@ -17,52 +21,170 @@ struct RotaryArgs {
     int64_t x_ts, x_hs, y_ts, y_hs, T;
     int H, D, R, inverse;
     float mscale, scale;
+    int pair_units, units, groups;     // units per head; threads that share a unit's heads
+    int tokens;                        // per workgroup (gridDim.y > 1: one)
 };
 
 // cos and sin of position * freq: the angle in turns is reduced in double
 // precision (a float angle of 10^5 radians is off by 0.004), its fraction in
 // [-1/2, 1/2] holds float accuracy whatever the position.
+// The nearest quarter turn is taken off; on the eighth of a turn that is left,
+// either way, the Taylor series to the 9th and 8th power are off by less than
+// 3e-8, half a step of FP32 at 1.
 __device__ __forceinline__ float2 turn(int64_t position, double freq, float m, int inverse) {
     const double turns = (double)position * (freq * 0.15915494309189533577);
     const float f = (float)(turns - __builtin_rint(turns));
-    float s, c;
-    sincospif(2.0f * f, &s, &c);
-    return make_float2(m * c, inverse ? -m * s : m * s);
+    const float k = __builtin_rintf(4.0f * f), r = __builtin_fmaf(k, -0.25f, f), r2 = r * r;
+    float s = __builtin_fmaf(r2, 42.0586939f, -76.7058598f);
+    s = __builtin_fmaf(r2, s, 81.6052493f);
+    s = __builtin_fmaf(r2, s, -41.3417022f);
+    s = __builtin_fmaf(r2, s, 6.28318531f) * r;
+    float c = __builtin_fmaf(r2, 60.2446414f, -85.4568172f);
+    c = __builtin_fmaf(r2, c, 64.939394f);
+    c = __builtin_fmaf(r2, c, -19.7392088f);
+    c = __builtin_fmaf(r2, c, 1.0f);
+    // quarter turns: (c, s) -> (-s, c)
+    const int q = (int)k;
+    const float cq = q & 1 ? -s : c, sq = q & 1 ? c : s, sign = q & 2 ? -m : m;
+    return make_float2(sign * cq, (inverse ? -sign : sign) * sq);
 }
+
+// n <= 8 elements from p on.
+template <int FMT>
+__device__ __forceinline__ void load_some(const fmt_t<FMT>* p, int n, float* x) {
+    if (n == 8) {
+        const Eight<FMT> e = *reinterpret_cast<const Eight<FMT>*>(p);
+        values_of<FMT>(e, special_in<FMT>(e), x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < n ? fmt_value<FMT>(p[i]) : 0.0f;
+    }
+}
+template <int FMT>
+__device__ __forceinline__ void store_some(fmt_t<FMT>* p, int n, const float* x) {
+    if (n == 8) {
+        Eight<FMT> e;
+        if constexpr (FMT == FP8T_FMT_F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e.a[i] = x[i];
+                e.b[i] = x[4 + i];
+            }
+        } else if constexpr (FMT == FP8T_FMT_FP16) {
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = maximum3_abs(top, x[2 * i], x[2 * i + 1]);
+            if (__builtin_expect(top < 0x1p31f, 1)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e.a[i] = fp16_pair(x[2 * i], x[2 * i + 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    e.a[i] = (uint32_t)f32_to_fp16_rn(x[2 * i]) |
+                             ((uint32_t)f32_to_fp16_rn(x[2 * i + 1]) << 16);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t lo = f32x2_to_fp8x2<false>(x[4 * i], x[4 * i + 1], 0u);
+                e.a[i] = f32x2_to_fp8x2<true>(x[4 * i + 2], x[4 * i + 3], lo);
+            }
+        }
+        *reinterpret_cast<Eight<FMT>*>(p) = e;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = fmt_code<FMT>(x[i]);
+    }
+}
+__device__ __forceinline__ int up_to_8(int n) { return n < 0 ? 0 : n < 8 ? n : 8; }
 
 template <int FX, int FY, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
-    using TX = fmt_t<FX>;
-    using TY = fmt_t<FY>;
-    const int half = a.R / 2, rest = a.D - a.R;
-    const int items = half + rest;                 // a head's pairs and its copied entries
-    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const int64_t pos = half ? a.positions[t] : 0;
-        for (int j = threadIdx.x; j < items; j += kThreads) {
-            float2 cs = make_float2(1.0f, 0.0f);
-            if (j < half) cs = turn(pos, a.freqs[j], a.mscale, a.inverse);
-            for (int h = 0; h < a.H; ++h) {
-                const TX* x = static_cast<const TX*>(a.x) + t * a.x_ts + h * a.x_hs;
-                TY* y = static_cast<TY*>(a.y) + t * a.y_ts + h * a.y_hs;
-                if (j < half) {
-                    const int i0 = INTERLEAVED ? 2 * j : j, i1 = INTERLEAVED ? 2 * j + 1 : j + half;
-                    const float x0 = fmt_value<FX>(x[i0]), x1 = fmt_value<FX>(x[i1]);
-                    const float r0 = __builtin_fmaf(x0, cs.x, -(x1 * cs.y));
-                    const float r1 = __builtin_fmaf(x1, cs.x, x0 * cs.y);
-                    y[i0] = fmt_code<FY>(r0 * a.scale);
-                    y[i1] = fmt_code<FY>(r1 * a.scale);
-                } else {
-                    const int i = a.R + j - half;
-                    y[i] = fmt_code<FY>(fmt_value<FX>(x[i]) * a.scale);
-                }
+    const int items = a.units * a.groups;                   // threads of a token
+    int64_t t;
+    int id;
+    const int64_t block = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+    if (gridDim.y > 1) {
+        t = block;
+        id = blockIdx.y * kThreads + threadIdx.x;
+        if (id >= items || t >= a.T) return;
+    } else {
+        t = block * a.tokens + threadIdx.x / items;
+        id = threadIdx.x % items;
+        if ((int)threadIdx.x >= a.tokens * items || t >= a.T) return;
+    }
+    const int u = id % a.units, group = id / a.units, half = a.R / 2;
+    // the unit's two runs of up to eight entries
+    const bool turned = u < a.pair_units;
+    const int j0 = 8 * u, c0 = a.R + 16 * (u - a.pair_units), pairs = up_to_8(half - j0);
+    int i0, i1, n0, n1;
+    if (!turned) {
+        i0 = c0;
+        i1 = c0 + 8;
+        n0 = up_to_8(a.D - i0);
+        n1 = up_to_8(a.D - i1);
+    } else if (INTERLEAVED) {
+        i0 = 2 * j0;
+        i1 = i0 + 8;
+        n0 = up_to_8(2 * pairs);
+        n1 = up_to_8(2 * pairs - 8);
+    } else {
+        i0 = j0;
+        i1 = j0 + half;
+        n0 = n1 = pairs;
+    }
+    float2 cs[8];
+    if (turned) {
+        const int64_t position = a.positions[t];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            cs[i] = i < pairs ? turn(position, a.freqs[j0 + i], a.mscale, a.inverse) : make_float2(1.0f, 0.0f);
+    }
+    const fmt_t<FX>* x = static_cast<const fmt_t<FX>*>(a.x) + t * a.x_ts;
+    fmt_t<FY>* y = static_cast<fmt_t<FY>*>(a.y) + t * a.y_ts;
+#pragma unroll 2
+    for (int h = group; h < a.H; h += a.groups) {
+        float p[8], q[8];
+        load_some<FX>(x + h * a.x_hs + i0, n0, p);
+        load_some<FX>(x + h * a.x_hs + i1, n1, q);
+        if (turned) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // pair i: entries i of both runs, or neighbours in one of them
+                float& x0 = INTERLEAVED ? (i < 4 ? p[2 * (i % 4)] : q[2 * (i % 4)]) : p[i];
+                float& x1 = INTERLEAVED ? (i < 4 ? p[2 * (i % 4) + 1] : q[2 * (i % 4) + 1]) : q[i];
+                const float r0 = __builtin_fmaf(x0, cs[i].x, -(x1 * cs[i].y));
+                const float r1 = __builtin_fmaf(x1, cs[i].x, x0 * cs[i].y);
+                x0 = r0;
+                x1 = r1;
             }
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] *= a.scale;
+            q[i] *= a.scale;
+        }
+        store_some<FY>(y + h * a.y_hs + i0, n0, p);
+        store_some<FY>(y + h * a.y_hs + i1, n1, q);
     }
 }
 
 template <int FX, int FY>
-void launch(const RotaryArgs& a, int interleaved, hipStream_t stream) {
-    const dim3 grid((unsigned)(a.T < 65536 ? a.T : 65536));
+void launch(RotaryArgs a, int interleaved, hipStream_t stream) {
+    a.pair_units = (a.R / 2 + 7) / 8;
+    a.units = a.pair_units + (a.D - a.R + 15) / 16;
+    // eight heads a thread; fewer where that leaves the card empty
+    const int64_t want = (int64_t)device_cus() * 2048;
+    int64_t groups = (a.H + 7) / 8;
+    while (groups < a.H && a.T * a.units * groups < want) groups = 2 * groups < a.H ? 2 * groups : a.H;
+    const int64_t cap = (1 << 23) / a.units;
+    a.groups = (int)(groups < cap ? groups : cap);
+    const int64_t items = (int64_t)a.units * a.groups;
+    a.tokens = items < kThreads ? (int)(kThreads / items) : 1;
+    const int64_t blocks = (a.T + a.tokens - 1) / a.tokens, across = blocks < kAcross ? blocks : kAcross;
+    const dim3 grid((unsigned)across, (unsigned)((items + kThreads - 1) / kThreads),
+                    (unsigned)((blocks + across - 1) / across));
     if (interleaved)
         hipLaunchKernelGGL((rotary_kernel<FX, FY, true>), grid, dim3(kThreads), 0, stream, a);
     else
