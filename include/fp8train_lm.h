@@ -107,9 +107,9 @@ int rotary_embed(const void* x, int x_format, int64_t x_ts, int64_t x_hs, const 
  * (workspace_bytes == 0, then a plan that needs none); it holds the partial
  * results of key ranges that several workgroups share.
  * Errors: FP8T_EINVAL (negative size, D not 1 .. FP8T_ATTN_MAX_D, Hq not a
- * multiple of Hkv, S, Tq, Tk, Hq above 2^31 - 4097, a flag not 0/1, sm_scale
- * not positive and finite, negative input stride, an output stride that
- * makes rows overlap, NULL pointer for non-empty data, no output, NULL
+ * multiple of Hkv, Hq above 65535, S, Tk or Tq Hq / Hkv above 2^31 - 4097, a
+ * flag not 0/1, sm_scale not positive and finite, negative input stride, an
+ * output stride that makes rows overlap, NULL pointer for non-empty data, no output, NULL
  * workspace with workspace_bytes > 0, or one that is not 16-byte aligned where
  * it is used); FP8T_EWORKSPACE (0 < workspace_bytes < the query); FP8T_EHIP.
  */

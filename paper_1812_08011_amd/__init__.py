@@ -316,29 +316,36 @@ def col2im_fp16(cols, N, H, W, C, KH, KW, pad, stride, dX, stream=None):
 # Tensors carry their sizes and strides here: T x H x D arrays may be any views
 # whose last dimension is contiguous.
 
+_formats = None
+
+
 def _format(fn, t, allowed):
-    import torch
-    fmt = {torch.float32: FMT_F32, torch.uint16: FMT_FP16, torch.uint8: FMT_FP8,
-           torch.float16: FMT_HALF}.get(t.dtype)
+    global _formats
+    if _formats is None:
+        import torch
+        _formats = {torch.float32: FMT_F32, torch.uint16: FMT_FP16, torch.uint8: FMT_FP8,
+                    torch.float16: FMT_HALF}
+    fmt = _formats.get(t.dtype)
     if fmt not in allowed:
         raise TypeError(f"{fn}: a tensor of type {t.dtype} is not taken here")
     return fmt
 
 
-def _rows(fn, t, shape, dtype=None):
-    """(address, token stride, head stride) of a T x H x D tensor."""
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{fn}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
-    if dtype is not None and t.dtype != dtype:
+def _rows(fn, t, like, dtype):
+    """(address, token stride, head stride) of a T x H x D tensor of the shape
+    `like`."""
+    if t.shape != like:
+        raise ValueError(f"{fn}: shape {tuple(t.shape)} where {tuple(like)} is needed")
+    if t.dtype != dtype:
         raise TypeError(f"{fn}: {t.dtype} where {dtype} is needed")
     ts, hs, ds = t.stride()
-    if ds != 1 and shape[2] > 1:
+    if ds != 1 and like[2] > 1:
         raise ValueError(f"{fn}: the last dimension must be contiguous")
     return t.data_ptr(), ts, hs
 
 
 def _dense(fn, t, shape, dtype):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{fn}: a contiguous {dtype} tensor of shape {tuple(shape)} is needed")
     return t.data_ptr()
 
@@ -362,31 +369,30 @@ def rotary_embed(x, positions, freqs, y, interleaved=False, inverse=False, mscal
     positions * freqs; x, y: T x H x D (float32, FP16 or FP8 codes), positions:
     T int64, freqs: R/2 float64.  y may be x."""
     import torch
-    fn, any_fmt = "rotary_embed", (FMT_F32, FMT_FP16, FMT_FP8)
-    T, H, D = x.shape
+    fn, any_fmt, shape = "rotary_embed", (FMT_F32, FMT_FP16, FMT_FP8), x.shape
+    T, H, D = shape
+    xp, x_ts, x_hs = _rows(fn, x, shape, x.dtype)
+    yp, y_ts, y_hs = _rows(fn, y, shape, y.dtype)
+    pairs = freqs.numel()
     _check(fn, lib().rotary_embed(
-        *_with_format(_rows(fn, x, x.shape), _format(fn, x, any_fmt)),
-        _dense(fn, positions, (T,), torch.int64), _dense(fn, freqs, freqs.shape[:1], torch.float64),
-        T, H, D, 2 * freqs.numel(), int(interleaved), int(inverse), float(mscale), float(scale),
-        *_with_format(_rows(fn, y, x.shape), _format(fn, y, any_fmt)), _stream(stream)))
+        xp, _format(fn, x, any_fmt), x_ts, x_hs, _dense(fn, positions, (T,), torch.int64),
+        _dense(fn, freqs, (pairs,), torch.float64), T, H, D, 2 * pairs, int(interleaved),
+        int(inverse), float(mscale), float(scale), yp, _format(fn, y, any_fmt), y_ts, y_hs,
+        _stream(stream)))
     return y
 
 
-def _with_format(rows, fmt):
-    return (rows[0], fmt) + rows[1:]
-
-
-def _attn_sizes(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal):
+def _attn_operands(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale):
     import torch
+    u8, i64 = torch.uint8, torch.int64
     Tq, Hq, D = q.shape
-    Tk, Hkv, _ = k.shape
-    S = cu_q.numel() - 1
-    if D != k.shape[2]:
+    Tk, Hkv, Dk = k.shape
+    if D != Dk:
         raise ValueError(f"{fn}: q and k have different head dimensions")
-    return ((*_rows(fn, q, (Tq, Hq, D), torch.uint8), *_rows(fn, k, (Tk, Hkv, D), torch.uint8),
-             *_rows(fn, v, (Tk, Hkv, D), torch.uint8), _dense(fn, cu_q, (S + 1,), torch.int64),
-             _dense(fn, cu_k, (S + 1,), torch.int64)),
-            (S, Tq, Tk, int(max_q), int(max_k), Hq, Hkv, D, int(causal)))
+    offsets = cu_q.shape
+    return (*_rows(fn, q, q.shape, u8), *_rows(fn, k, k.shape, u8), *_rows(fn, v, k.shape, u8),
+            _dense(fn, cu_q, offsets, i64), _dense(fn, cu_k, offsets, i64), offsets[0] - 1, Tq, Tk,
+            int(max_q), int(max_k), Hq, Hkv, D, int(causal), float(sm_scale))
 
 
 def attn_fwd_fp8_workspace_size(q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale):
@@ -408,10 +414,9 @@ def attn_fwd_fp8(q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale, o, o8, o8_
     (float32, Hq x Tq) are each optional."""
     import torch
     fn = "attn_fwd_fp8"
-    ins, sizes = _attn_sizes(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal)
     none = (None, 0, 0)
     _check(fn, lib().attn_fwd_fp8(
-        *ins, *sizes, float(sm_scale),
+        *_attn_operands(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale),
         *(none if o is None else _rows(fn, o, q.shape, torch.uint16)),
         *(none if o8 is None else _rows(fn, o8, q.shape, torch.uint8)), float(o8_scale),
         None if lse is None else _dense(fn, lse, (q.shape[1], q.shape[0]), torch.float32),
@@ -425,11 +430,10 @@ def attn_bwd_fp8(q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale, o, d_o, ls
     (FP16 codes) and lse and the error d_o of o (FP8 codes)."""
     import torch
     fn = "attn_bwd_fp8"
-    ins, sizes = _attn_sizes(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal)
     fmt = _format(fn, dq, (FMT_FP16, FMT_FP8))
     _check(fn, lib().attn_bwd_fp8(
-        *ins, *sizes, float(sm_scale), *_rows(fn, o, q.shape, torch.uint16),
-        *_rows(fn, d_o, q.shape, torch.uint8),
+        *_attn_operands(fn, q, k, v, cu_q, cu_k, max_q, max_k, causal, sm_scale),
+        *_rows(fn, o, q.shape, torch.uint16), *_rows(fn, d_o, q.shape, torch.uint8),
         _dense(fn, lse, (q.shape[1], q.shape[0]), torch.float32),
         *_rows(fn, dq, q.shape, dq.dtype), *_rows(fn, dk, k.shape, dq.dtype),
         *_rows(fn, dv, k.shape, dq.dtype), fmt, float(grad_scale), _ptr(workspace),
@@ -448,7 +452,7 @@ def distill_loss(z, idx, t, w, tau, grad_scale, loss, g, stream=None):
     k = idx.shape[1]
 
     def matrix(m, allowed):
-        if tuple(m.shape) != (N, V) or (N > 0 and V > 1 and m.stride(1) != 1):
+        if m.shape != z.shape or (N > 0 and V > 1 and m.stride(1) != 1):
             raise ValueError(f"{fn}: an N x V tensor with contiguous rows is needed")
         return m.data_ptr(), _format(fn, m, allowed), max(m.stride(0), V if N <= 1 else 0)
     _check(fn, lib().distill_loss(

@@ -11,7 +11,7 @@ bool sizes_ok(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int64_t max_k, i
     return S >= 0 && Tq >= 0 && Tk >= 0 && max_q >= 0 && max_k >= 0 && Hq >= 0 && Hkv >= 0 &&
            D >= 1 && D <= FP8T_ATTN_MAX_D && S <= kMaxGemmDim && Tq <= kMaxGemmDim &&
            Tk <= kMaxGemmDim && Hq <= 65535 && (Hkv > 0 ? Hq % Hkv == 0 : Hq == 0) &&
-           (causal | 1) == 1;
+           (Hkv == 0 || Tq * (Hq / Hkv) <= kMaxGemmDim) && (causal | 1) == 1;
 }
 bool rows_ok(const void* p, int64_t ts, int64_t hs, int64_t T, int64_t H) {
     return ts >= 0 && hs >= 0 && (p || T == 0 || H == 0);
@@ -68,6 +68,8 @@ extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     a.Hq = (int)Hq;
     a.Hkv = (int)Hkv;
     a.D = (int)D;
+    a.G = (int)(Hq / Hkv);
+    a.g_magic = a.G > 1 ? ~0ull / (uint64_t)a.G + 1 : 0;
     a.causal = causal;
     a.Tq = Tq;
     a.Tk = Tk;
@@ -114,7 +116,6 @@ extern "C" int attn_bwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
         (!workspace && workspace_bytes))
         return FP8T_EINVAL;
     if (S == 0 || Hq == 0 || (Tq == 0 && Tk == 0)) return FP8T_OK;
-    if ((Tq / 64 + 1) * (Hq / Hkv) > kMaxGemmDim) return FP8T_EINVAL;
     if (!cu_q || !cu_k || (Tq > 0 && !lse)) return FP8T_EINVAL;
     if (!rows_apart(Tq, Hq, D, dq_ts, dq_hs) || !rows_apart(Tk, Hkv, D, dk_ts, dk_hs) ||
         !rows_apart(Tk, Hkv, D, dv_ts, dv_hs) || !aligned(workspace, 16))
@@ -132,6 +133,8 @@ extern "C" int attn_bwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     a.Hq = (int)Hq;
     a.Hkv = (int)Hkv;
     a.D = (int)D;
+    a.G = (int)(Hq / Hkv);
+    a.g_magic = a.G > 1 ? ~0ull / (uint64_t)a.G + 1 : 0;
     a.causal = causal;
     a.Tq = Tq;
     a.Tk = Tk;

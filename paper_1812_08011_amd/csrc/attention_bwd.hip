@@ -13,27 +13,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Four entries of a gradient from column col on.
-template <int FG>
-__device__ __forceinline__ void write4(void* base, int64_t at, int col, int D, const float* x) {
-    fmt_t<FG>* p = static_cast<fmt_t<FG>*>(base) + at + col;
-    if (col + 4 <= D && aligned_to(p, 4 * sizeof(*p))) {
-        if constexpr (FG == FP8T_FMT_FP16) {
-            uint2 w;
-            w.x = (uint32_t)f32_to_fp16_rn(x[0]) | ((uint32_t)f32_to_fp16_rn(x[1]) << 16);
-            w.y = (uint32_t)f32_to_fp16_rn(x[2]) | ((uint32_t)f32_to_fp16_rn(x[3]) << 16);
-            *reinterpret_cast<uint2*>(p) = w;
-        } else {
-            const uint32_t lo = f32x2_to_fp8x2<false>(x[0], x[1], 0u);
-            *reinterpret_cast<uint32_t*>(p) = f32x2_to_fp8x2<true>(x[2], x[3], lo);
-        }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (col + r < D) p[r] = fmt_code<FG>(x[r]);
-    }
-}
-
 // The power of two that dS = p (<e, v> - delta) is held times.  Both terms are
 // at most |e| |v| (delta is a mean of such products), so with the largest norms
 // the scaled dS stays below 2^15, and a dS down to 2^-29 of that bound keeps
@@ -46,30 +25,6 @@ __device__ __forceinline__ float ds_scale(const AttnArgs& a) {
     return __builtin_ldexpf(1.0f, 13 - e);
 }
 
-// Entries that are not finite, of the rows noted in `bits` (row 0 of them is
-// token t0 of `src`), for the columns that see the row: f(d, r, code).
-template <int ND, typename SEES, typename F>
-__device__ __forceinline__ void add_noted(uint32_t bits, const uint8_t* src, int64_t ts, int t0, int D,
-                                          int h, SEES sees, F f) {
-    bits = __builtin_amdgcn_readfirstlane(bits);
-    while (__builtin_expect(bits != 0, 0)) {
-        int hh = h;
-        asm volatile("" : "+v"(hh));                        // nothing of this is hoisted
-        const int t = t0 + __builtin_ctz(bits);
-        bits &= bits - 1;
-        if (!sees(t)) continue;
-        const uint8_t* p = src + (int64_t)t * ts;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int col = 32 * d + 8 * (r / 4) + 4 * hh + r % 4;
-                const uint32_t c = col < D ? p[col] : 0u;
-                if ((c & 0x7Cu) == 0x7Cu) f(d, r, c);
-            }
-    }
-}
-
 // ---- dq ------------------------------------------------------------------------------------
 
 // 128 rows (query, head of the group), 32 per wave; key tiles one ahead in
@@ -79,36 +34,35 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
     using I = KeyImage<DP>;
     constexpr int BM = kAttnRows, N = I::N, NC = DP / 32, ND = DP / 32;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
+    static_assert(sizeof(lds) >= 4 * kRowsOut, "the results' way out fits the buffers");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int l31 = lane & 31, h = lane >> 5;
-    const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
+    const int hk = blockIdx.x % a.Hkv;
     const int slot = ordered_slot(a.row_order, blockIdx.x / a.Hkv);
     if (slot < 0) return;
     int tile;
-    const Seq sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, G, BM, slot, tile));
-    const int64_t nrows = (int64_t)sq.nq * G;
-    const int ntiles = (int)((nrows + BM - 1) / BM);
+    const Seq sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, a.G, BM, slot, tile));
+    const int nrows = sq.nq * a.G, ntiles = (nrows + BM - 1) / BM;
     if (tile >= ntiles) return;
-    tile = ntiles - 1 - tile;                               // the longest first
-    const int64_t row0 = (int64_t)tile * BM, row = row0 + 32 * wave + l31;
+    const int row0 = (ntiles - 1 - tile) * BM, row = row0 + 32 * wave + l31;   // the longest first
     const bool live = row < nrows;
-    const int i = live ? (int)(row / G) : 0, g = live ? (int)(row % G) : 0;
-    const int off = sq.nk - sq.nq;
-    auto limit = [&](int64_t r) {
-        const int64_t n = a.causal ? r / G + 1 + off : sq.nk;
-        return (int)(n < 0 ? 0 : n);
+    const int i = live ? div_g(a, row) : 0, g = live ? row - i * a.G : 0, off = sq.nk - sq.nq;
+    auto limit = [&](int i) {
+        const int n = a.causal ? i + 1 + off : sq.nk;
+        return n < 0 ? 0 : n;
     };
-    const int lim = live ? limit(row) : 0;
-    const int lim_lo = limit(row0), lim_hi = limit(row0 + BM < nrows ? row0 + BM - 1 : nrows - 1);
-    const int64_t w0 = row0 + 32 * wave;
-    const int wave_hi = w0 < nrows ? limit(w0 + 31 < nrows ? w0 + 31 : nrows - 1) : 0;
+    const int lim = live ? limit(i) : 0;
+    const int lim_lo = limit(div_g(a, row0));
+    const int lim_hi = limit(div_g(a, row0 + BM < nrows ? row0 + BM - 1 : nrows - 1));
+    const int w0 = row0 + 32 * wave;
+    const int wave_hi = w0 < nrows ? limit(div_g(a, w0 + 31 < nrows ? w0 + 31 : nrows - 1)) : 0;
     const int first = (int)(sq.k0 / N), j00 = (int)((int64_t)first * N - sq.k0);
     const int t1 = lim_hi > 0 ? (lim_hi - j00 + N - 1) / N : 0;
     const uint8_t* image = a.key_image + ((int64_t)hk * a.key_tiles + first) * I::kBytes;
     if (t1 > 0) image_to_lds<I::kBytes, 4>(image, lds, wave, lane);
 
     const int64_t tq = sq.q0 + i;
-    const int hq = hk * G + g;
+    const int hq = hk * a.G + g;
     const uint8_t* qp = a.q.p + tq * a.q.ts + (int64_t)hq * a.q.hs;
     const uint8_t* ep = a.e.p + tq * a.e.ts + (int64_t)hq * a.e.hs;
     const uint8_t* kp = a.k.p + sq.k0 * a.k.ts + (int64_t)hk * a.k.hs;
@@ -184,18 +138,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
                           [&](int d, int r, uint32_t) { o[d][r] = __uint_as_float(kF32NaN); });
         }
     }
-    if (!live) return;
-    const float f = a.sm_scale / sigma * a.grad_scale;
+    __syncthreads();                                        // the buffers are free
     const int64_t at = tq * a.dq_ts + (int64_t)hq * a.dq_hs;
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float x[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = o[d][4 * q + r] * f;
-            write4<FG>(a.dq, at, 32 * d + 8 * q + 4 * h, a.D, x);
-        }
+    rows_out<DP>(reinterpret_cast<float*>(lds + wave * kRowsOut), o, a.sm_scale / sigma * a.grad_scale, lane,
+                 [&](int r, int col, const float* x) {
+                     const int64_t to = of_lane(at, r);
+                     const int n = __shfl((int)live, r) ? up_to_8(a.D - col) : 0;
+                     if (n) store_some<FG>(static_cast<fmt_t<FG>*>(a.dq) + to + col, n, x);
+                 });
 }
 
 // ---- dk and dv --------------------------------------------------------------------------------
@@ -208,10 +158,11 @@ template <int DP, bool VEC, int FG, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
     using I = QueryImage<DP>;
     constexpr int BN = kAttnDkvKeys, N = I::N, NC = DP / 32, ND = DP / 32;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
+    constexpr int kLds = 2 * I::kBytes > 4 * kRowsOut ? 2 * I::kBytes : 4 * kRowsOut;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kLds];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int l31 = lane & 31, h = lane >> 5;
-    const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
+    const int hk = blockIdx.x % a.Hkv, G = a.G;
     const int slot = ordered_slot(a.key_order, blockIdx.x / a.Hkv);
     if (slot < 0) return;
     int tile;
@@ -325,55 +276,65 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
             add_noted<ND>(noted[0], a.q.p + sq.q0 * a.q.ts + (int64_t)hq * a.q.hs, a.q.ts, i0, a.D, h, sees,
                           [&](int d, int r, uint32_t) { dk[d][r] = __uint_as_float(kF32NaN); });
             add_noted<ND>(noted[1], a.e.p + sq.q0 * a.e.ts + (int64_t)hq * a.e.hs, a.e.ts, i0, a.D, h, sees,
-                          [&](int d, int r, uint32_t c) { dv[d][r] += fp8_to_f32<0>(c); });
+                          [&](int d, int r, uint32_t c) { dv[d][r] += fp8_nonfinite(c); });
         }
     }
-    if (j >= sq.nk) return;
     const float fk = a.sm_scale / sigma * a.grad_scale, fv = __builtin_ldexpf(a.grad_scale, -kAttnPUp);
     const int64_t t = sq.k0 + j;
-    float* part = SPLIT ? a.parts + (((int64_t)blockIdx.y * a.Tk + t) * a.Hkv + hk) * (2 * DP) : nullptr;
+    if constexpr (SPLIT) {
+        if (j >= sq.nk) return;
+        float* part = a.parts + (((int64_t)blockIdx.y * a.Tk + t) * a.Hkv + hk) * (2 * DP) + 4 * h;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float x[4], y[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[r] = dk[d][4 * q + r] * fk;
-                y[r] = dv[d][4 * q + r] * fv;
+            for (int q = 0; q < 4; ++q) {
+                const int at = 32 * d + 8 * q;
+                *reinterpret_cast<float4*>(part + at) =
+                    make_float4(dk[d][4 * q] * fk, dk[d][4 * q + 1] * fk, dk[d][4 * q + 2] * fk,
+                                dk[d][4 * q + 3] * fk);
+                *reinterpret_cast<float4*>(part + DP + at) =
+                    make_float4(dv[d][4 * q] * fv, dv[d][4 * q + 1] * fv, dv[d][4 * q + 2] * fv,
+                                dv[d][4 * q + 3] * fv);
             }
-            const int col = 32 * d + 8 * q + 4 * h;
-            if constexpr (SPLIT) {
-                *reinterpret_cast<float4*>(part + col) = make_float4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<float4*>(part + DP + col) = make_float4(y[0], y[1], y[2], y[3]);
-            } else {
-                write4<FG>(a.dk, t * a.dk_ts + (int64_t)hk * a.dk_hs, col, a.D, x);
-                write4<FG>(a.dv, t * a.dv_ts + (int64_t)hk * a.dv_hs, col, a.D, y);
-            }
-        }
+    } else {
+        __syncthreads();                                    // the buffers are free
+        float* xs = reinterpret_cast<float*>(lds + wave * kRowsOut);
+        auto out = [&](const v16f* acc, float scale, void* base, int64_t ts, int64_t hs) {
+            const int64_t at = t * ts + (int64_t)hk * hs;
+            rows_out<DP>(xs, acc, scale, lane, [&](int r, int col, const float* x) {
+                const int64_t to = of_lane(at, r);
+                const int n = wave0 + r < sq.nk ? up_to_8(a.D - col) : 0;
+                if (n) store_some<FG>(static_cast<fmt_t<FG>*>(base) + to + col, n, x);
+            });
+        };
+        out(dk, fk, a.dk, a.dk_ts, a.dk_hs);
+        out(dv, fv, a.dv, a.dv_ts, a.dv_hs);
+    }
 }
 
-// Sums the partial dk and dv in their order: four entries a thread.  A token of
-// no sequence is not written.
+// Sums the partial dk and dv in their order: eight entries a thread.  A token
+// of no sequence is not written.
 template <int DP, int FG>
 __global__ __launch_bounds__(kThreads) void attn_dkv_join_kernel(AttnArgs a) {
-    constexpr int kPer = 2 * DP / 4;                        // threads per (token, head)
+    constexpr int kPer = 2 * DP / 8;                        // threads per (token, head)
     const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, rows = a.Tk * a.Hkv;
     const int64_t row = id / kPer;
-    const int c = (int)(id % kPer) * 4, col = c % DP;
-    if (row >= rows || col >= a.D) return;
+    const int c = (int)(id % kPer) * 8, col = c % DP, n = up_to_8(a.D - col);
+    if (row >= rows || n == 0) return;
     const int64_t t = row / a.Hkv, hk = row % a.Hkv;
     if (t < clamp_to(a.cu_k[0], a.Tk) || t >= clamp_to(a.cu_k[a.S], a.Tk)) return;
-    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const float* part = a.parts + row * (2 * DP) + c;
     for (int z = 0; z < a.splits; ++z) {
-        const float4 p = *reinterpret_cast<const float4*>(a.parts + (z * rows + row) * (2 * DP) + c);
-        x[0] += p.x;
-        x[1] += p.y;
-        x[2] += p.z;
-        x[3] += p.w;
+        const float4 p = *reinterpret_cast<const float4*>(part + z * rows * (2 * DP));
+        const float4 q = *reinterpret_cast<const float4*>(part + z * rows * (2 * DP) + 4);
+        const float y[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += y[i];
     }
-    if (c < DP) write4<FG>(a.dk, t * a.dk_ts + hk * a.dk_hs, col, a.D, x);
-    else write4<FG>(a.dv, t * a.dv_ts + hk * a.dv_hs, col, a.D, x);
+    const bool is_k = c < DP;
+    const int64_t at = is_k ? t * a.dk_ts + hk * a.dk_hs : t * a.dv_ts + hk * a.dv_hs;
+    store_some<FG>(static_cast<fmt_t<FG>*>(is_k ? a.dk : a.dv) + at + col, n, x);
 }
 
 template <int DP, bool VEC, int FG>
@@ -381,13 +342,13 @@ void launch(const AttnArgs& a, hipStream_t stream) {
     const dim3 block(kThreads);
     if (a.Tq > 0)
         hipLaunchKernelGGL((attn_dq_kernel<DP, VEC, FG>),
-                           dim3((unsigned)(a.Hkv * slots(a.S, a.Tq, a.Hq / a.Hkv, kAttnRows))), block, 0,
+                           dim3((unsigned)(a.Hkv * slots(a.S, a.Tq, a.G, kAttnRows))), block, 0,
                            stream, a);
     if (a.Tk == 0) return;
     const dim3 grid((unsigned)(a.Hkv * slots(a.S, a.Tk, 1, kAttnDkvKeys)), (unsigned)a.splits);
     if (a.splits > 1) {
         hipLaunchKernelGGL((attn_dkv_kernel<DP, VEC, FG, true>), grid, block, 0, stream, a);
-        const int64_t items = a.Tk * a.Hkv * (2 * DP / 4);
+        const int64_t items = a.Tk * a.Hkv * (2 * DP / 8);
         hipLaunchKernelGGL((attn_dkv_join_kernel<DP, FG>), dim3((unsigned)((items + kThreads - 1) / kThreads)),
                            block, 0, stream, a);
     } else {

@@ -177,25 +177,15 @@ struct FwdRows {
                     o[d] = mfma_half(HT::frag(vl, 32 * d + l31, 2 * kt + t, h), pf, o[d]);
             }
         }
+        uint32_t any = noted[0];
 #pragma unroll
-        for (int kt = 0; kt < NK; ++kt) {
-            uint32_t b = __builtin_amdgcn_readfirstlane(noted[kt]);
-            while (__builtin_expect(b != 0, 0)) {
-                int hh = h;
-                asm volatile("" : "+v"(hh));                // nothing of this is hoisted
-                const int key = j0 + 32 * kt + __builtin_ctz(b);
-                b &= b - 1;
-                if ((uint32_t)key >= (uint32_t)lim) continue;
-                const uint8_t* vr = v + (int64_t)key * v_ts;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int col = 32 * d + 8 * (r / 4) + 4 * hh + r % 4;
-                        const uint32_t c = col < D ? vr[col] : 0u;
-                        if ((c & 0x7Cu) == 0x7Cu) o[d][r] += fp8_to_f32<0>(c);
-                    }
-            }
+        for (int kt = 1; kt < NK; ++kt) any |= noted[kt];
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(any) != 0, 0)) {
+#pragma unroll 1
+            for (int kt = 0; kt < NK; ++kt)
+                add_noted<ND>(noted[kt], v, v_ts, j0 + 32 * kt, D, h,
+                              [&](int key) { return (uint32_t)key < (uint32_t)lim; },
+                              [&](int d, int r, uint32_t c) { o[d][r] += fp8_nonfinite(c); });
         }
     }
 };
@@ -204,46 +194,47 @@ struct FwdRows {
 template <int BM, int RW>              // rows, rows from one wave to the next (0: the same rows)
 struct FwdTile {
     Seq sq;
-    int64_t row0, row, nrows, tq;
-    int hk, hq, slot, lim, lim_lo, lim_hi, wave_hi;
+    int64_t tq;
+    int row0, row, nrows, hk, hq, slot, lim, lim_lo, lim_hi, wave_hi;
     bool live;
     // false: nothing to do.  Row r sees keys [0, limit(r)); the longest tiles
     // come first.
     __device__ __forceinline__ bool init(const AttnArgs& a, int wave, int l31) {
         hk = blockIdx.x % a.Hkv;
-        const int G = a.Hq / a.Hkv;
         int tile;
         slot = ordered_slot(a.row_order, blockIdx.x / a.Hkv);
         if (slot < 0) return false;
-        sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, G, BM, slot, tile));
-        nrows = (int64_t)sq.nq * G;
-        const int ntiles = (int)((nrows + BM - 1) / BM);
+        sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, a.G, BM, slot, tile));
+        nrows = sq.nq * a.G;
+        const int ntiles = (nrows + BM - 1) / BM;
         if (tile >= ntiles) return false;
-        row0 = (int64_t)(ntiles - 1 - tile) * BM;
+        row0 = (ntiles - 1 - tile) * BM;
         row = row0 + RW * wave + l31;
         live = row < nrows;
-        const int i = live ? (int)(row / G) : 0, off = sq.nk - sq.nq;
-        auto limit = [&](int64_t r) {
-            const int64_t n = a.causal ? r / G + 1 + off : sq.nk;
-            return (int)(n < 0 ? 0 : n);
+        const int i = live ? div_g(a, row) : 0, off = sq.nk - sq.nq;
+        auto limit = [&](int i) {
+            const int n = a.causal ? i + 1 + off : sq.nk;
+            return n < 0 ? 0 : n;
         };
-        lim = live ? limit(row) : 0;
-        lim_lo = limit(row0);
-        lim_hi = limit(row0 + BM < nrows ? row0 + BM - 1 : nrows - 1);
-        const int64_t w0 = row0 + RW * wave;
-        wave_hi = w0 < nrows ? limit(w0 + 31 < nrows ? w0 + 31 : nrows - 1) : 0;
+        lim = live ? limit(i) : 0;
+        lim_lo = limit(div_g(a, row0));
+        lim_hi = limit(div_g(a, row0 + BM < nrows ? row0 + BM - 1 : nrows - 1));
+        const int w0 = row0 + RW * wave;
+        wave_hi = w0 < nrows ? limit(div_g(a, w0 + 31 < nrows ? w0 + 31 : nrows - 1)) : 0;
         tq = sq.q0 + i;
-        hq = hk * G + (live ? (int)(row % G) : 0);
+        hq = hk * a.G + (live ? row - i * a.G : 0);
         return true;
     }
 };
 
+// xs: kRowsOut bytes of LDS of the wave's own.
 template <int DP, int BM, bool SPLIT>
 __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& sp,
                                             const FwdTile<BM, BM == 128 ? 32 : 0>& t,
-                                            const FwdRows<DP>& x, float ref, float l, int h) {
-    if (!t.live) return;
+                                            const FwdRows<DP>& x, float ref, float l, int lane, void* xs) {
+    const int h = lane >> 5;
     if constexpr (SPLIT) {
+        if (!t.live) return;
         const int64_t part = (int64_t)blockIdx.y * gridDim.x + (int64_t)t.slot * a.Hkv + t.hk;
         const int64_t pr = part * BM + (t.row - t.row0);
         float* po = sp.o + pr * DP;
@@ -255,7 +246,25 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
                     x.o[d][4 * q], x.o[d][4 * q + 1], x.o[d][4 * q + 2], x.o[d][4 * q + 3]);
         if (h == 0) sp.ml[pr] = make_float2(ref, l);
     } else {
-        attn_write_row<DP>(a, t.tq, t.hq, t.lim, ref, l, h, [&](int d, int r) { return x.o[d][r]; });
+        if (a.lse && h == 0 && t.live)
+            a.lse[(int64_t)t.hq * a.Tq + t.tq] = t.lim > 0 ? kAttnLn2 * (ref + log2f(l)) : -INFINITY;
+        if (!a.o && !a.o8) return;
+        // a row that sees nothing has sums of +0
+        const float inv = t.lim > 0 ? 1.0f / l : 1.0f;
+        const int64_t o = t.tq * a.o_ts + (int64_t)t.hq * a.o_hs;
+        const int64_t o8 = t.tq * a.o8_ts + (int64_t)t.hq * a.o8_hs;
+        rows_out<DP>(static_cast<float*>(xs), x.o, inv, lane, [&](int r, int col, const float* v) {
+            const int64_t at = of_lane(o, r), at8 = of_lane(o8, r);
+            const int n = __shfl((int)t.live, r) ? up_to_8(a.D - col) : 0;
+            if (n == 0) return;
+            if (a.o) store_some<FP8T_FMT_FP16>(a.o + at + col, n, v);
+            if (a.o8) {
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = v[i] * a.o8_scale;
+                store_some<FP8T_FMT_FP8>(a.o8 + at8 + col, n, y);
+            }
+        });
     }
 }
 
@@ -295,7 +304,8 @@ __global__ __launch_bounds__(kThreads, 3) void attn_fwd_image_kernel(AttnArgs a,
                a.v.ts, a.D, []() {});
     }
     const float l = both_halves(x.l, Add());
-    finish_rows<DP, 128, SPLIT>(a, sp, t, x, x.ref, l, h);
+    __syncthreads();                                        // the buffers are free
+    finish_rows<DP, 128, SPLIT>(a, sp, t, x, x.ref, l, lane, lds + wave * kRowsOut);
 }
 
 // KW = 1: 128 rows, 32 per wave, every wave walks all key tiles (shared in
@@ -311,9 +321,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
     constexpr int NC = DP / 32, ND = DP / 32, NK = kBN / 32;
     using CT = CodeTile<kBN, DP>;
     using HT = HalfTile<kBN, DP>;
-    __shared__ __attribute__((aligned(16))) uint8_t ks[KW == 1 ? NB * CT::kBytes : 16];
-    __shared__ __attribute__((aligned(16))) uint8_t vs[NB * HT::kBytes];
+    constexpr int kKeys = KW == 1 ? NB * CT::kBytes : 0;    // KW = 4: keys go straight to registers
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kKeys + NB * HT::kBytes];
+    uint8_t* const ks = lds;
+    uint8_t* const vs = lds + kKeys;
     __shared__ uint32_t bad[4][NK];
+    static_assert(sizeof(lds) >= (KW == 1 ? 4 : 1) * kRowsOut && 2 * FwdImage<DP>::kBytes >= 4 * kRowsOut,
+                  "the results' way out fits the buffers");
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
     FwdTile<BM, KW == 1 ? 32 : 0> w;
     if (!w.init(a, wave, l31)) return;
@@ -433,29 +447,27 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
             }
         ref = m;
     }
-    finish_rows<DP, BM, SPLIT>(a, sp, w, x, ref, l, h);
+    // KW = 1: the last step ended at a barrier; KW = 4: one wave is left
+    finish_rows<DP, BM, SPLIT>(a, sp, w, x, ref, l, lane, lds + (KW == 1 ? wave * kRowsOut : 0));
 }
 
 // Joins the partial results of a tile's key ranges, in their order: a wave per
 // row, a lane for every 64th entry.
-template <int DP>
+template <int DP, int BM>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSplit sp) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int hk = blockIdx.x % a.Hkv, G = a.Hq / a.Hkv;
+    const int hk = blockIdx.x % a.Hkv;
     int tile;
-    const int s = slot_owner(a.cu_q, a.S, a.Tq, G, sp.BM, blockIdx.x / a.Hkv, tile);
-    const Seq sq = load_seq(a, s);
-    const int64_t nrows = (int64_t)sq.nq * G;
-    const int ntiles = (int)((nrows + sp.BM - 1) / sp.BM);
+    const Seq sq = load_seq(a, slot_owner(a.cu_q, a.S, a.Tq, a.G, BM, blockIdx.x / a.Hkv, tile));
+    const int nrows = sq.nq * a.G, ntiles = (nrows + BM - 1) / BM;
     if (tile >= ntiles) return;
     tile = ntiles - 1 - tile;
-    const int rr = blockIdx.y * (kThreads / 64) + wave;
-    const int64_t row = (int64_t)tile * sp.BM + rr;
-    if (rr >= sp.BM || row >= nrows) return;
-    const int64_t lim = a.causal ? row / G + 1 + sq.nk - sq.nq : sq.nk;
+    const int rr = blockIdx.y * (kThreads / 64) + wave, row = tile * BM + rr;
+    if (rr >= BM || row >= nrows) return;
+    const int i = div_g(a, row), lim = a.causal ? i + 1 + sq.nk - sq.nq : sq.nk;
     float m = -INFINITY;
     auto at = [&](int z) {
-        return ((int64_t)z * gridDim.x + blockIdx.x) * sp.BM + rr;
+        return ((int64_t)z * gridDim.x + blockIdx.x) * BM + rr;
     };
     for (int z = 0; z < sp.n; ++z) m = fmaxf(m, sp.ml[at(z)].x);
     float l = 0.0f, o[2] = {0.0f, 0.0f};
@@ -467,8 +479,8 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSpl
 #pragma unroll
         for (int u = 0; u < DP / 64; ++u) o[u] += sp.o[at(z) * DP + 64 * u + lane] * f;
     }
-    const int64_t t = sq.q0 + row / G;
-    const int hq = hk * G + (int)(row % G);
+    const int64_t t = sq.q0 + i;
+    const int hq = hk * a.G + row - i * a.G;
     const float inv = 1.0f / l;
 #pragma unroll
     for (int u = 0; u < DP / 64; ++u) {
@@ -497,9 +509,10 @@ void launch(const AttnArgs& a, const AttnFwdPlan& p, const AttnSplit& sp, hipStr
         if (split) hipLaunchKernelGGL((attn_fwd_kernel<DP, 1, VEC, true>), grid, block, 0, stream, a, sp);
         else hipLaunchKernelGGL((attn_fwd_kernel<DP, 1, VEC, false>), grid, block, 0, stream, a, sp);
     }
-    if (split)
-        hipLaunchKernelGGL(attn_join_kernel<DP>, dim3(grid.x, (unsigned)((p.BM + 3) / 4)), block, 0,
-                           stream, a, sp);
+    if (split && p.BM == 32)
+        hipLaunchKernelGGL((attn_join_kernel<DP, 32>), dim3(grid.x, 8), block, 0, stream, a, sp);
+    else if (split)
+        hipLaunchKernelGGL((attn_join_kernel<DP, 128>), dim3(grid.x, 32), block, 0, stream, a, sp);
 }
 
 }  // namespace
@@ -548,7 +561,6 @@ void attn_fwd_launch(AttnArgs a, const AttnFwdPlan& p, bool vec, void* workspace
         sp.ml = reinterpret_cast<float2*>(sp.o + rows * p.DP);
         sp.n = p.splits;
         sp.per = p.per;
-        sp.BM = p.BM;
     }
     if (p.DP == 64) {
         if (vec) launch<64, true>(a, p, sp, stream);

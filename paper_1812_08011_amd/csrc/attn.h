@@ -15,6 +15,8 @@ struct AttnArgs {
     const int64_t* cu_q;
     const int64_t* cu_k;
     int S, Hq, Hkv, D, causal;
+    int G;                   // Hq / Hkv, and floor(2^64 / G) + 1 (0 for G = 1)
+    uint64_t g_magic;
     int64_t Tq, Tk;
     float c2;                // sm_scale log2(e): exponents are kept in base 2
     float sm_scale;
@@ -64,8 +66,9 @@ __device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s) {
     return r;
 }
 
-__device__ __forceinline__ bool aligned_to(const void* p, uintptr_t n) {
-    return ((uintptr_t)p & (n - 1)) == 0;
+// n / G, exact while n G < 2^64.
+__device__ __forceinline__ int div_g(const AttnArgs& a, int n) {
+    return a.g_magic ? (int)__umul64hi((uint64_t)(uint32_t)n, a.g_magic) : n;
 }
 
 // Work of sequences of unknown lengths laid out without a scan: with

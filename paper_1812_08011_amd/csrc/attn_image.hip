@@ -74,16 +74,16 @@ __device__ __forceinline__ void order_tiles(const AttnArgs& a, int* order) {
     constexpr int kTile = KEYS ? kAttnDkvKeys : kAttnRows;
     __shared__ int count[257];
     __shared__ int top;
-    const int tid = threadIdx.x, G = a.Hq / a.Hkv;
+    const int tid = threadIdx.x;
     const int64_t* cu = KEYS ? a.cu_k : a.cu_q;
-    const int64_t T = KEYS ? a.Tk : a.Tq, mult = KEYS ? 1 : G;
+    const int64_t T = KEYS ? a.Tk : a.Tq, mult = KEYS ? 1 : a.G;
     const int n = (int)(T * mult / kTile + a.S);
     // keys that the tile's last row sees, or queries that see the tile's first
     // key; -1: an empty slot
     auto work = [&](int slot) {
         int tile;
         const Seq sq = load_seq(a, slot_owner(cu, a.S, T, mult, kTile, slot, tile));
-        const int64_t len = KEYS ? sq.nk : (int64_t)sq.nq * G, first = (int64_t)tile * kTile;
+        const int64_t len = KEYS ? sq.nk : (int64_t)sq.nq * a.G, first = (int64_t)tile * kTile;
         if (first >= len) return -1;
         const int off = sq.nk - sq.nq;
         if (KEYS) {
@@ -93,7 +93,7 @@ __device__ __forceinline__ void order_tiles(const AttnArgs& a, int* order) {
         // row tiles run backwards in their slots
         const int64_t ntiles = (len + kTile - 1) / kTile, t = ntiles - 1 - tile;
         const int64_t last = (t + 1) * kTile < len ? (t + 1) * kTile - 1 : len - 1;
-        const int64_t lim = a.causal ? last / G + 1 + off : sq.nk;
+        const int64_t lim = a.causal ? div_g(a, (int)last) + 1 + off : sq.nk;
         return lim > 0 ? (int)lim : 0;
     };
     for (int i = tid; i < 257; i += kThreads) count[i] = 0;

@@ -162,4 +162,77 @@ struct HalfTile {
     }
 };
 
+// Inf or NaN from its code.
+__device__ __forceinline__ float fp8_nonfinite(uint32_t c) {
+    return __uint_as_float(((c & 0x80u) << 24) | kF32Inf | ((c & 3u) << 21));
+}
+
+// Entries that are not finite, of the rows noted in `bits` (row 0 of them is
+// token t0 of `src`), for the columns that see the row: f(d, r, code).
+template <int ND, typename SEES, typename F>
+__device__ __forceinline__ void add_noted(uint32_t bits, const uint8_t* src, int64_t ts, int t0, int D,
+                                          int h, SEES sees, F f) {
+    bits = __builtin_amdgcn_readfirstlane(bits);
+    while (__builtin_expect(bits != 0, 0)) {
+        int hh = h;
+        asm volatile("" : "+v"(hh));                        // nothing of this is hoisted
+        const int t = t0 + __builtin_ctz(bits);
+        bits &= bits - 1;
+        if (!sees(t)) continue;
+        const uint8_t* p = src + (int64_t)t * ts;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int col = 32 * d + 8 * (r / 4) + 4 * hh + r % 4;
+                const uint32_t c = col < D ? p[col] : 0u;
+                if ((c & 0x7Cu) == 0x7Cu) f(d, r, c);
+            }
+    }
+}
+
+// A wave's 32 rows (one per lane pair) x DP columns, out of its result registers
+// through `xs` (kRowsOut bytes of LDS of its own), 64 columns at a time: store(r,
+// col, x) is called with every lane active for row r's eight entries from
+// column col on.  Neighbouring lanes get neighbouring entries, and the code
+// for the formats is there once per 64 columns, not once per register quartet:
+// short calls are bound by fetching their instructions.
+constexpr int kRowsOut = 32 * (64 + 4) * 4;
+template <int DP, typename STORE>
+__device__ __forceinline__ void rows_out(float* xs, const v16f* acc, float scale, int lane, STORE store) {
+    const int l31 = lane & 31, h = lane >> 5;
+    auto fence = [&]() {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+#pragma unroll
+    for (int part = 0; part < DP / 64; ++part) {
+        fence();
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const v16f& v = acc[2 * part + d];
+                *reinterpret_cast<float4*>(xs + l31 * 68 + 32 * d + 8 * q + 4 * h) =
+                    make_float4(v[4 * q] * scale, v[4 * q + 1] * scale, v[4 * q + 2] * scale,
+                                v[4 * q + 3] * scale);
+            }
+        fence();
+#pragma unroll 1
+        for (int it = 0; it < 4; ++it) {
+            const int r = it * 8 + lane / 8, c = lane % 8 * 8;
+            const float4 a = *reinterpret_cast<const float4*>(xs + r * 68 + c);
+            const float4 b = *reinterpret_cast<const float4*>(xs + r * 68 + c + 4);
+            const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            store(r, 64 * part + c, x);
+        }
+    }
+}
+
+// A value of lane r's, 64 bits.
+__device__ __forceinline__ int64_t of_lane(int64_t x, int r) {
+    const uint32_t lo = __shfl((int)(uint32_t)x, r), hi = __shfl((int)(uint32_t)((uint64_t)x >> 32), r);
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
 }  // namespace fp8t

@@ -113,6 +113,46 @@ __device__ __forceinline__ bool special_in(const Eight<FMT>& e) {
         return ((fp16_nonfinite(e.a[0]) | fp16_nonfinite(e.a[1]) | fp16_nonfinite(e.a[2]) |
                  fp16_nonfinite(e.a[3])) & 0x80008000u) != 0;
 }
+// n <= 8 results to p on, at any address.
+template <int FMT>
+__device__ __forceinline__ void store_some(fmt_t<FMT>* p, int n, const float* x) {
+    if (n == 8) {
+        Eight<FMT> e;
+        if constexpr (FMT == FP8T_FMT_F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e.a[i] = x[i];
+                e.b[i] = x[4 + i];
+            }
+        } else if constexpr (FMT == FP8T_FMT_FP16) {
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = maximum3_abs(top, x[2 * i], x[2 * i + 1]);
+            if (__builtin_expect(top < 0x1p31f, 1)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e.a[i] = fp16_pair(x[2 * i], x[2 * i + 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    e.a[i] = (uint32_t)f32_to_fp16_rn(x[2 * i]) |
+                             ((uint32_t)f32_to_fp16_rn(x[2 * i + 1]) << 16);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t lo = f32x2_to_fp8x2<false>(x[4 * i], x[4 * i + 1], 0u);
+                e.a[i] = f32x2_to_fp8x2<true>(x[4 * i + 2], x[4 * i + 3], lo);
+            }
+        }
+        *reinterpret_cast<Eight<FMT>*>(p) = e;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = fmt_code<FMT>(x[i]);
+    }
+}
+__device__ __forceinline__ int up_to_8(int n) { return n < 0 ? 0 : n < 8 ? n : 8; }
+
 // Whether the rows of a T x H x D result with strides ts and hs are apart:
 // heads inside tokens or tokens inside heads.
 inline bool rows_apart(int64_t T, int64_t H, int64_t D, int64_t ts, int64_t hs) {
