@@ -92,6 +92,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    uint32_t noted_any = 0;
     for (int t = 0; t < t1; ++t) {
         const uint8_t* buf = lds + (t & 1) * I::kBytes;
         image_barrier();
@@ -133,8 +134,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
                 for (int d = 0; d < ND; ++d)
                     o[d] = mfma_half(I::HT::frag(buf + I::kT, 32 * d + l31, 2 * kt + u, h), f, o[d]);
             }
-            add_noted<ND>(reinterpret_cast<const uint32_t*>(buf + I::kNoted)[kt], kp, a.k.ts, j0 + 32 * kt,
-                          a.D, h, [&](int key) { return (uint32_t)key < (uint32_t)lim; },
+            noted_any |= reinterpret_cast<const uint32_t*>(buf + I::kNoted)[kt];
+        }
+    }
+    if (__builtin_expect(__any(noted_any != 0), 0)) {
+        // keys that are not finite, for the rows that see them
+#pragma unroll 1
+        for (int i = 0; i < t1 * (N / 32); ++i) {
+            const uint8_t* at = image + (int64_t)(i / (N / 32)) * I::kBytes + I::kNoted;
+            add_noted<ND>(reinterpret_cast<const uint32_t*>(at)[i % (N / 32)], kp, a.k.ts, j00 + 32 * i, a.D,
+                          h, [&](int key) { return (uint32_t)key < (uint32_t)lim; },
                           [&](int d, int r, uint32_t) { o[d][r] = __uint_as_float(kF32NaN); });
         }
     }
@@ -211,6 +220,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
         for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
     const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     int b = 0;
+    uint32_t noted_any = 0;
     for (int n = n0; n < steps; n += dn, b ^= 1) {
         image_barrier();
         if (n + dn < steps) issue(n + dn, b ^ 1);
@@ -270,8 +280,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
             }
         }
         const uint32_t* noted = reinterpret_cast<const uint32_t*>(buf + I::kNoted);
-        if (__builtin_expect(__builtin_amdgcn_readfirstlane(noted[0] | noted[1]) != 0, 0)) {
-            const int hq = hk * G + n / ntq;
+        noted_any |= noted[0] | noted[1];
+    }
+    if (__builtin_expect(__any(noted_any != 0), 0)) {
+        // queries and errors that are not finite, for the keys they see
+#pragma unroll 1
+        for (int n = n0; n < steps; n += dn) {
+            const int hq = hk * G + n / ntq, t = ta + n % ntq, i0 = (int)((int64_t)t * N - sq.q0);
+            const uint8_t* at = a.query_image + ((int64_t)hq * a.query_tiles + t) * I::kBytes + I::kNoted;
+            const uint32_t* noted = reinterpret_cast<const uint32_t*>(at);
             auto sees = [&](int i) { return (uint32_t)(i - lo) < seen_by; };
             add_noted<ND>(noted[0], a.q.p + sq.q0 * a.q.ts + (int64_t)hq * a.q.hs, a.q.ts, i0, a.D, h, sees,
                           [&](int d, int r, uint32_t) { dk[d][r] = __uint_as_float(kF32NaN); });

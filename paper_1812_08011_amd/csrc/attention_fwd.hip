@@ -17,42 +17,39 @@ struct Fmax { __device__ float operator()(float a, float b) const { return fmaxf
 struct Add { __device__ float operator()(float a, float b) const { return a + b; } };
 
 // Key tile in flight: the registers between global memory and LDS.
-template <int DP, int NT>
+template <int kBN, int DP, int NT>
 struct Stage {
-    static constexpr int kBN = attn_keys(DP);
     static constexpr int kK = CodeTile<kBN, DP>::template units<NT>();
     static constexpr int kV = HalfTile<kBN, DP>::template units<NT>();
     uint4 k[kK];
     uint2 v[kV][4];
 };
 
-template <int DP, bool VEC, int NT>
-__device__ __forceinline__ void load_k(Stage<DP, NT>& s, const uint8_t* k, int64_t ts, int j0, int nk,
+template <int kBN, int DP, bool VEC, int NT>
+__device__ __forceinline__ void load_k(Stage<kBN, DP, NT>& s, const uint8_t* k, int64_t ts, int j0, int nk,
                                        int D, int tid) {
 #pragma unroll
-    for (int u = 0; u < Stage<DP, NT>::kK; ++u) {
+    for (int u = 0; u < Stage<kBN, DP, NT>::kK; ++u) {
         const int id = tid + u * NT, row = id / (DP / 16), col = id % (DP / 16) * 16;
         s.k[u] = load_codes16<VEC>(k + (int64_t)(j0 + row) * ts, col, D, j0 + row < nk);
     }
 }
-template <int DP, bool VEC, int NT>
-__device__ __forceinline__ void load_v(Stage<DP, NT>& s, const uint8_t* v, int64_t ts, int j0, int nk,
+template <int kBN, int DP, bool VEC, int NT>
+__device__ __forceinline__ void load_v(Stage<kBN, DP, NT>& s, const uint8_t* v, int64_t ts, int j0, int nk,
                                        int D, int tid) {
-    constexpr int kBN = attn_keys(DP);
     using HT = HalfTile<kBN, DP>;
 #pragma unroll
-    for (int u = 0; u < Stage<DP, NT>::kV; ++u) {
+    for (int u = 0; u < Stage<kBN, DP, NT>::kV; ++u) {
         const int id = tid + u * NT, row = j0 + HT::unit_row(id), col = HT::unit_col(id);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             s.v[u][r] = load_codes8<VEC>(v + (int64_t)(row + r) * ts, col, D, row + r < nk);
     }
 }
-template <int DP, int NT>
-__device__ __forceinline__ void store_k(const Stage<DP, NT>& s, uint8_t* lds, int tid) {
-    constexpr int kBN = attn_keys(DP);
+template <int kBN, int DP, int NT>
+__device__ __forceinline__ void store_k(const Stage<kBN, DP, NT>& s, uint8_t* lds, int tid) {
 #pragma unroll
-    for (int u = 0; u < Stage<DP, NT>::kK; ++u) {
+    for (int u = 0; u < Stage<kBN, DP, NT>::kK; ++u) {
         const int id = tid + u * NT, row = id / (DP / 16), col = id % (DP / 16) * 16;
         *reinterpret_cast<uint4*>(lds + row * CodeTile<kBN, DP>::kRow + col) = s.k[u];
     }
@@ -60,13 +57,12 @@ __device__ __forceinline__ void store_k(const Stage<DP, NT>& s, uint8_t* lds, in
 // partial: some row does not see some key of the tile.  Values that are not
 // finite are then taken out (a matrix product would let 0 x NaN into rows that
 // do not see the key) and their keys noted in `bad`.
-template <int DP, int NT>
-__device__ __forceinline__ void store_v(Stage<DP, NT>& s, uint8_t* lds, int tid, bool partial,
+template <int kBN, int DP, int NT>
+__device__ __forceinline__ void store_v(Stage<kBN, DP, NT>& s, uint8_t* lds, int tid, bool partial,
                                         uint32_t* bad) {
-    constexpr int kBN = attn_keys(DP);
     using HT = HalfTile<kBN, DP>;
 #pragma unroll
-    for (int u = 0; u < Stage<DP, NT>::kV; ++u) {
+    for (int u = 0; u < Stage<kBN, DP, NT>::kV; ++u) {
         const int id = tid + u * NT;
         if (partial) {
             const int row = HT::unit_row(id);
@@ -86,14 +82,15 @@ __device__ __forceinline__ void store_v(Stage<DP, NT>& s, uint8_t* lds, int tid,
 
 // What a wave holds of its 32 rows: queries, running sums, statistics.  Lane
 // half h of column l % 32 holds rows 8 g + 4 h + r of every result.
-template <int DP>
+template <int DP, int N>
 struct FwdRows {
-    static constexpr int N = attn_keys(DP), NC = DP / 32, ND = DP / 32, NK = N / 32;
+    static constexpr int NC = DP / 32, ND = DP / 32, NK = N / 32;
     using HT = HalfTile<N, DP>;
     Widen widen;
     v8h qf[NC][2];
     v16f o[ND];
     float ref, mu, l, c2;              // reference; the same, 0 before the first key; sum; scale
+    uint32_t noted_any;                // keys with values that are not finite came by
 
     template <bool VEC>
     __device__ __forceinline__ void init(const AttnArgs& a, const uint8_t* q, int h, bool live) {
@@ -110,17 +107,17 @@ struct FwdRows {
             for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
         ref = -INFINITY;
         mu = l = 0.0f;
+        noted_any = 0;
     }
 
     // One key tile whose first key is j0 (negative: keys of another sequence
     // first): kf(kt, c) gives the key operand, vl the values in LDS; next() runs
     // once the key operands are used up.  partial: some row does not see some
     // key; a row sees keys [0, lim).  noted: the keys whose values are not
-    // finite, v their sequence's first value.
+    // finite and left out of vl.
     template <typename KF, typename NEXT>
     __device__ __forceinline__ void step(KF kf, const uint8_t* vl, int j0, int lim, bool partial, int h,
-                                         int l31, const uint32_t* noted, const uint8_t* v, int64_t v_ts,
-                                         int D, NEXT next) {
+                                         int l31, const uint32_t* noted, NEXT next) {
         const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
         v16f st[NK];
 #pragma unroll
@@ -177,16 +174,17 @@ struct FwdRows {
                     o[d] = mfma_half(HT::frag(vl, 32 * d + l31, 2 * kt + t, h), pf, o[d]);
             }
         }
-        uint32_t any = noted[0];
 #pragma unroll
-        for (int kt = 1; kt < NK; ++kt) any |= noted[kt];
-        if (__builtin_expect(__builtin_amdgcn_readfirstlane(any) != 0, 0)) {
-#pragma unroll 1
-            for (int kt = 0; kt < NK; ++kt)
-                add_noted<ND>(noted[kt], v, v_ts, j0 + 32 * kt, D, h,
-                              [&](int key) { return (uint32_t)key < (uint32_t)lim; },
-                              [&](int d, int r, uint32_t c) { o[d][r] += fp8_nonfinite(c); });
-        }
+        for (int kt = 0; kt < NK; ++kt) noted_any |= noted[kt];
+    }
+
+    // The values that are not finite of the keys noted in `bits`, from key j0
+    // on, for the rows that see them.  After the last step: inside it this
+    // costs the loop 50 registers.
+    __device__ __forceinline__ void add(uint32_t bits, int j0, int lim, int h, const uint8_t* v,
+                                        int64_t v_ts, int D) {
+        add_noted<ND>(bits, v, v_ts, j0, D, h, [&](int key) { return (uint32_t)key < (uint32_t)lim; },
+                      [&](int d, int r, uint32_t c) { o[d][r] += fp8_nonfinite(c); });
     }
 };
 
@@ -228,10 +226,10 @@ struct FwdTile {
 };
 
 // xs: kRowsOut bytes of LDS of the wave's own.
-template <int DP, int BM, bool SPLIT>
+template <int DP, int N, int BM, bool SPLIT>
 __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& sp,
                                             const FwdTile<BM, BM == 128 ? 32 : 0>& t,
-                                            const FwdRows<DP>& x, float ref, float l, int lane, void* xs) {
+                                            const FwdRows<DP, N>& x, float ref, float l, int lane, void* xs) {
     const int h = lane >> 5;
     if constexpr (SPLIT) {
         if (!t.live) return;
@@ -271,7 +269,7 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
 // 128 rows, 32 per wave; key tiles come from their image by direct loads into
 // LDS, one tile ahead.
 template <int DP, bool VEC, bool SPLIT>
-__global__ __launch_bounds__(kThreads, 3) void attn_fwd_image_kernel(AttnArgs a, AttnSplit sp) {
+__global__ __launch_bounds__(kThreads, 2) void attn_fwd_image_kernel(AttnArgs a, AttnSplit sp) {
     using I = FwdImage<DP>;
     constexpr int N = I::N;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * I::kBytes];
@@ -289,7 +287,7 @@ __global__ __launch_bounds__(kThreads, 3) void attn_fwd_image_kernel(AttnArgs a,
     const uint8_t* image = a.key_image + ((int64_t)t.hk * a.key_tiles + first) * I::kBytes;
     const uint8_t* vp = a.v.p + t.sq.k0 * a.v.ts + (int64_t)t.hk * a.v.hs;
     if (t0 < t1) image_to_lds<I::kBytes, 4>(image + (int64_t)t0 * I::kBytes, lds, wave, lane);
-    FwdRows<DP> x;
+    FwdRows<DP, N> x;
     x.template init<VEC>(a, a.q.p + t.tq * a.q.ts + (int64_t)t.hq * a.q.hs, h, t.live);
     for (int n = t0; n < t1; ++n) {
         const uint8_t* buf = lds + ((n - t0) & 1) * I::kBytes;
@@ -300,12 +298,19 @@ __global__ __launch_bounds__(kThreads, 3) void attn_fwd_image_kernel(AttnArgs a,
         const int j0 = j00 + n * N;
         if (j0 >= t.wave_hi) continue;
         x.step([&](int kt, int c) { return I::CT::frag(buf, 32 * kt + l31, c, h); }, buf + I::kV, j0, t.lim,
-               j0 < 0 || j0 + N > t.lim_lo, h, l31, reinterpret_cast<const uint32_t*>(buf + I::kNoted), vp,
-               a.v.ts, a.D, []() {});
+               j0 < 0 || j0 + N > t.lim_lo, h, l31, reinterpret_cast<const uint32_t*>(buf + I::kNoted),
+               []() {});
+    }
+    if (__builtin_expect(__any(x.noted_any != 0), 0)) {
+#pragma unroll 1
+        for (int i = t0 * (N / 32); i < t1 * (N / 32); ++i) {
+            const uint8_t* at = image + (int64_t)(i / (N / 32)) * I::kBytes + I::kNoted;
+            x.add(reinterpret_cast<const uint32_t*>(at)[i % (N / 32)], j00 + 32 * i, t.lim, h, vp, a.v.ts, a.D);
+        }
     }
     const float l = both_halves(x.l, Add());
     __syncthreads();                                        // the buffers are free
-    finish_rows<DP, 128, SPLIT>(a, sp, t, x, x.ref, l, lane, lds + wave * kRowsOut);
+    finish_rows<DP, N, 128, SPLIT>(a, sp, t, x, x.ref, l, lane, lds + wave * kRowsOut);
 }
 
 // KW = 1: 128 rows, 32 per wave, every wave walks all key tiles (shared in
@@ -316,13 +321,14 @@ __global__ __launch_bounds__(kThreads, 3) void attn_fwd_image_kernel(AttnArgs a,
 // results go to the workspace.
 template <int DP, int KW, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnSplit sp) {
-    constexpr int NT = kThreads / KW, BM = 128 / KW, kBN = attn_keys(DP);
+    constexpr int NT = kThreads / KW, BM = 128 / KW, kBN = KW == 1 ? attn_keys(DP) : attn_keys(DP) / 2;
     constexpr int NB = KW == 1 ? 2 : 4;                     // LDS buffers: double, or one per wave
     constexpr int NC = DP / 32, ND = DP / 32, NK = kBN / 32;
     using CT = CodeTile<kBN, DP>;
     using HT = HalfTile<kBN, DP>;
     constexpr int kKeys = KW == 1 ? NB * CT::kBytes : 0;    // KW = 4: keys go straight to registers
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kKeys + NB * HT::kBytes];
+    constexpr int kTiles = kKeys + NB * HT::kBytes, kJoin = KW == 1 ? 0 : 3 * ND * 16 * 64 * 4;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kTiles > kJoin ? kTiles : kJoin];
     uint8_t* const ks = lds;
     uint8_t* const vs = lds + kKeys;
     __shared__ uint32_t bad[4][NK];
@@ -339,17 +345,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
     }
     const uint8_t* kp = a.k.p + sq.k0 * a.k.ts + (int64_t)w.hk * a.k.hs;
     const uint8_t* vp = a.v.p + sq.k0 * a.v.ts + (int64_t)w.hk * a.v.hs;
-    FwdRows<DP> x;
+    FwdRows<DP, kBN> x;
     x.template init<VEC>(a, a.q.p + w.tq * a.q.ts + (int64_t)w.hq * a.q.hs, h, w.live);
     auto is_partial = [&](int t) { return (t + 1) * kBN > w.lim_lo; };
 
-    Stage<DP, NT> sg;
+    Stage<kBN, DP, NT> sg;
     if constexpr (KW == 1) {
         if (tid < 4 * NK) bad[tid / NK][tid % NK] = 0u;
         __syncthreads();
         if (t0 < t1) {
-            load_k<DP, VEC>(sg, kp, a.k.ts, t0 * kBN, sq.nk, a.D, tid);
-            load_v<DP, VEC>(sg, vp, a.v.ts, t0 * kBN, sq.nk, a.D, tid);
+            load_k<kBN, DP, VEC>(sg, kp, a.k.ts, t0 * kBN, sq.nk, a.D, tid);
+            load_v<kBN, DP, VEC>(sg, vp, a.v.ts, t0 * kBN, sq.nk, a.D, tid);
             store_k(sg, ks, tid);
             store_v(sg, vs, tid, is_partial(t0), bad[0]);
         }
@@ -357,14 +363,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
         for (int t = t0; t < t1; ++t) {
             const int b = (t - t0) & 1, q = (t - t0) % 3;
             if (t + 1 < t1) {
-                load_k<DP, VEC>(sg, kp, a.k.ts, (t + 1) * kBN, sq.nk, a.D, tid);
-                load_v<DP, VEC>(sg, vp, a.v.ts, (t + 1) * kBN, sq.nk, a.D, tid);
+                load_k<kBN, DP, VEC>(sg, kp, a.k.ts, (t + 1) * kBN, sq.nk, a.D, tid);
+                load_v<kBN, DP, VEC>(sg, vp, a.v.ts, (t + 1) * kBN, sq.nk, a.D, tid);
             }
             if (t * kBN < w.wave_hi) {
                 const uint8_t* kl = ks + b * CT::kBytes;
                 x.step([&](int kt, int c) { return CT::frag(kl, 32 * kt + l31, c, h); },
-                       vs + b * HT::kBytes, t * kBN, w.lim, is_partial(t), h, l31, bad[q], vp, a.v.ts,
-                       a.D, []() {});
+                       vs + b * HT::kBytes, t * kBN, w.lim, is_partial(t), h, l31, bad[q], []() {});
             }
             // noted keys: slot q is read here, the next one written, the one
             // read in the last step cleared
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
                     kf[kt][c] = load_codes16<VEC>(kp + (int64_t)j * a.k.ts, 32 * c + 16 * h, a.D,
                                                   j < sq.nk);
             }
-            load_v<DP, VEC>(sg, vp, a.v.ts, t * kBN, sq.nk, a.D, lane);
+            load_v<kBN, DP, VEC>(sg, vp, a.v.ts, t * kBN, sq.nk, a.D, lane);
         };
         // a wave works by itself here: its LDS accesses are ordered
         auto fence = [&]() {
@@ -402,10 +407,25 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
             store_v(sg, vl, lane, is_partial(t), bad[wave]);
             fence();
             x.step([&](int kt, int c) { return kf[kt][c]; }, vl, t * kBN, w.lim, is_partial(t), h, l31,
-                   bad[wave], vp, a.v.ts, a.D, [&]() {
+                   bad[wave], [&]() {
                        if (t + KW < t1) load(t + KW);
                    });
         }
+    }
+    if (__builtin_expect(__any(x.noted_any != 0), 0)) {
+        // the partial tiles again, each key's row looked at by the whole wave
+        int t = w.lim_lo / kBN > t0 ? w.lim_lo / kBN : t0;
+        if (KW > 1) t += (t0 + wave - t % KW + KW * KW) % KW;   // this wave's tiles
+#pragma unroll 1
+        for (; t < t1; t += KW)
+#pragma unroll 1
+            for (int j = t * kBN; j < (t + 1) * kBN && j < sq.nk; ++j) {
+                bool odd = false;
+#pragma unroll
+                for (int c = lane; c < DP; c += 64)
+                    if (c < a.D) odd |= (vp[(int64_t)j * a.v.ts + c] & 0x7Cu) == 0x7Cu;
+                if (__any(odd)) x.add(1u, j, w.lim, h, vp, a.v.ts, a.D);
+            }
     }
     float l = both_halves(x.l, Add()), ref = x.ref;
 
@@ -427,7 +447,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
             l += refs[v][l31] == m ? ls[v][l31] : ls[v][l31] * exp2f(refs[v][l31] - m);
         const float f = ref == m ? 1.0f : exp2f(ref - m);
         float* xs = reinterpret_cast<float*>(vs);           // [wave - 1][register][lane]
-        static_assert(NB * HT::kBytes >= 3 * ND * 16 * 64 * 4, "the joined waves' sums fit");
         if (wave) {
 #pragma unroll
             for (int d = 0; d < ND; ++d)
@@ -448,7 +467,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
         ref = m;
     }
     // KW = 1: the last step ended at a barrier; KW = 4: one wave is left
-    finish_rows<DP, BM, SPLIT>(a, sp, w, x, ref, l, lane, lds + (KW == 1 ? wave * kRowsOut : 0));
+    finish_rows<DP, kBN, BM, SPLIT>(a, sp, w, x, ref, l, lane, lds + (KW == 1 ? wave * kRowsOut : 0));
 }
 
 // Joins the partial results of a tile's key ranges, in their order: a wave per
@@ -534,7 +553,7 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     const int64_t tiles_q = (max_q * G + p.BM - 1) / p.BM;
     int64_t groups = p.slots < S * tiles_q ? p.slots : S * tiles_q;
     groups *= Hkv;
-    const int kBN = attn_keys(p.DP);
+    const int kBN = p.BM == 32 ? attn_keys(p.DP) / 2 : attn_keys(p.DP);
     const int64_t tiles_k = (max_k + kBN - 1) / kBN;
     const int64_t want = 4 * (int64_t)device_cus(), least = p.BM == 32 ? 8 : 16;
     int64_t n = groups > 0 && groups * 2 <= want ? want / groups : 1;

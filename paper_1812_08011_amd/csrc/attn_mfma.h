@@ -183,10 +183,14 @@ __device__ __forceinline__ void add_noted(uint32_t bits, const uint8_t* src, int
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int col = 32 * d + 8 * (r / 4) + 4 * hh + r % 4;
-                const uint32_t c = col < D ? p[col] : 0u;
-                if ((c & 0x7Cu) == 0x7Cu) f(d, r, c);
+            for (int q = 0; q < 4; ++q) {
+                asm volatile("" : "+v"(hh));                // four loads at a time
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int col = 32 * d + 8 * q + 4 * hh + r;
+                    const uint32_t c = col < D ? p[col] : 0u;
+                    if ((c & 0x7Cu) == 0x7Cu) f(d, 4 * q + r, c);
+                }
             }
     }
 }
