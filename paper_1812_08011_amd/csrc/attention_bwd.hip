@@ -298,32 +298,26 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
     }
     const float fk = a.sm_scale / sigma * a.grad_scale, fv = __builtin_ldexpf(a.grad_scale, -kAttnPUp);
     const int64_t t = sq.k0 + j;
-    if constexpr (SPLIT) {
-        if (j >= sq.nk) return;
-        float* part = a.parts + (((int64_t)blockIdx.y * a.Tk + t) * a.Hkv + hk) * (2 * DP) + 4 * h;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int at = 32 * d + 8 * q;
-                *reinterpret_cast<float4*>(part + at) =
-                    make_float4(dk[d][4 * q] * fk, dk[d][4 * q + 1] * fk, dk[d][4 * q + 2] * fk,
-                                dk[d][4 * q + 3] * fk);
-                *reinterpret_cast<float4*>(part + DP + at) =
-                    make_float4(dv[d][4 * q] * fv, dv[d][4 * q + 1] * fv, dv[d][4 * q + 2] * fv,
-                                dv[d][4 * q + 3] * fv);
-            }
-    } else {
-        __syncthreads();                                    // the buffers are free
-        float* xs = reinterpret_cast<float*>(lds + wave * kRowsOut);
-        auto out = [&](const v16f* acc, float scale, void* base, int64_t ts, int64_t hs) {
-            const int64_t at = t * ts + (int64_t)hk * hs;
-            rows_out<DP>(xs, acc, scale, lane, [&](int r, int col, const float* x) {
-                const int64_t to = of_lane(at, r);
-                const int n = wave0 + r < sq.nk ? up_to_8(a.D - col) : 0;
+    __syncthreads();                                        // the buffers are free
+    float* xs = reinterpret_cast<float*>(lds + wave * kRowsOut);
+    auto out = [&](const v16f* acc, float scale, void* base, int64_t ts, int64_t hs) {
+        const int64_t at = t * ts + (int64_t)hk * hs;
+        rows_out<DP>(xs, acc, scale, lane, [&](int r, int col, const float* x) {
+            const int64_t to = of_lane(at, r);
+            if (wave0 + r >= sq.nk) return;
+            if constexpr (SPLIT) {
+                store_some<FP8T_FMT_F32>(static_cast<float*>(base) + to + col, 8, x);
+            } else {
+                const int n = up_to_8(a.D - col);
                 if (n) store_some<FG>(static_cast<fmt_t<FG>*>(base) + to + col, n, x);
-            });
-        };
+            }
+        });
+    };
+    if constexpr (SPLIT) {
+        float* part = a.parts + (int64_t)blockIdx.y * a.Tk * a.Hkv * (2 * DP);
+        out(dk, fk, part, (int64_t)a.Hkv * (2 * DP), 2 * DP);
+        out(dv, fv, part + DP, (int64_t)a.Hkv * (2 * DP), 2 * DP);
+    } else {
         out(dk, fk, a.dk, a.dk_ts, a.dk_hs);
         out(dv, fv, a.dv, a.dv_ts, a.dv_hs);
     }

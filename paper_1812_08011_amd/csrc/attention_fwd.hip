@@ -232,17 +232,24 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
                                             const FwdRows<DP, N>& x, float ref, float l, int lane, void* xs) {
     const int h = lane >> 5;
     if constexpr (SPLIT) {
-        if (!t.live) return;
         const int64_t part = (int64_t)blockIdx.y * gridDim.x + (int64_t)t.slot * a.Hkv + t.hk;
         const int64_t pr = part * BM + (t.row - t.row0);
-        float* po = sp.o + pr * DP;
+        if (h == 0 && t.live) sp.ml[pr] = make_float2(ref, l);
+        if constexpr (BM == 32) {                           // few of the rows are there
+            if (!t.live) return;
+            float* po = sp.o + pr * DP + 4 * h;
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
+            for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<float4*>(po + 32 * d + 8 * q + 4 * h) = make_float4(
-                    x.o[d][4 * q], x.o[d][4 * q + 1], x.o[d][4 * q + 2], x.o[d][4 * q + 3]);
-        if (h == 0) sp.ml[pr] = make_float2(ref, l);
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<float4*>(po + 32 * d + 8 * q) = make_float4(
+                        x.o[d][4 * q], x.o[d][4 * q + 1], x.o[d][4 * q + 2], x.o[d][4 * q + 3]);
+        } else {
+            rows_out<DP>(static_cast<float*>(xs), x.o, 1.0f, lane, [&](int r, int col, const float* v) {
+                const int64_t to = of_lane(pr, r);
+                if (__shfl((int)t.live, r)) store_some<FP8T_FMT_F32>(sp.o + to * DP + col, 8, v);
+            });
+        }
     } else {
         if (a.lse && h == 0 && t.live)
             a.lse[(int64_t)t.hq * a.Tq + t.tq] = t.lim > 0 ? kAttnLn2 * (ref + log2f(l)) : -INFINITY;
@@ -560,7 +567,7 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     groups *= Hkv;
     const int kBN = p.BM == 32 ? attn_keys(p.DP) / 2 : attn_keys(p.DP);
     const int64_t tiles_k = (max_k + kBN - 1) / kBN;
-    const int64_t want = 4 * (int64_t)device_cus(), least = p.BM == 32 ? 8 : 16;
+    const int64_t want = (p.BM == 32 ? 2 : 4) * (int64_t)device_cus(), least = p.BM == 32 ? 8 : 16;
     int64_t n = groups > 0 && groups * 2 <= want ? want / groups : 1;
     if (n > tiles_k / least) n = tiles_k / least;
     if (n > 64) n = 64;
