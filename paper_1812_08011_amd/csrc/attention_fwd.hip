@@ -548,8 +548,26 @@ void launch(const AttnArgs& a, const AttnFwdPlan& p, const AttnSplit& sp, hipStr
 
 }  // namespace
 
-// Rows of 32 take the kernel that shares out the keys inside a workgroup; the
-// keys are shared out over workgroups where the rows alone leave CUs idle.
+// Which kernel, by the packed rows (query, head of the group) of the longest
+// sequence.  Measured with 16 query and 4 key/value heads unless stated:
+//
+// * up to 32 rows: the kernel whose waves share out the keys of 32 rows.  8
+//   sequences with 2048 keys, 4 rows: 12 us against 31 us (D 64) and 16
+//   against 30 us (D 128) for the kernel of 128 rows; with 64 and 128 rows the
+//   two lie within a third of each other, either way by the number of keys.
+// * 4096 rows and more: keys from tiles laid out beforehand, which 32 row tiles
+//   or more read then.  4 sequences of 4096 tokens, D 128: 282 us, directly
+//   from the operands 318 us; 16 heads without groups: 296 and 313 us; 1024
+//   tokens over 8192 keys: 292 and 320 us.  With 2048 rows the layout costs what
+//   it saves (64.5 and 63.9 us) and below that more (1024 rows: 23 and 18 us).
+// * D up to 64 pays for 64 columns, above for 128: half the products and half
+//   the loads.
+//
+// The keys are shared out over workgroups where the rows leave CUs idle, until
+// there are 4 workgroups per CU (2 for the kernel of few rows: 27 us for 8
+// tokens over long histories where 4 take 31 us, a longer join), with at least
+// 8 steps of keys each: with 16, 64 rows over 4 x 4096 keys take 36 us in place
+// of 23 us; with 4, 4 rows over 8 x 2048 keys take 15 us in place of 12 us.
 AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int64_t max_k, int64_t Hq,
                           int64_t Hkv, int64_t D) {
     AttnFwdPlan p = {};
@@ -557,8 +575,7 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     p.DP = D <= 64 ? 64 : 128;
     p.BM = max_q * G <= 32 ? 32 : 128;
     p.slots = slots(S, Tq, G, p.BM);
-    // images pay where many row tiles read them (measured below)
-    p.image = p.BM == 128 && max_q * G >= 1024;
+    p.image = p.BM == 128 && max_q * G >= 4096;
     const int64_t image = p.image ? image_tiles(Tk, attn_keys(p.DP)) * Hkv *
                                         (p.DP == 64 ? FwdImage<64>::kBytes : FwdImage<128>::kBytes)
                                   : 0;
@@ -567,7 +584,7 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     groups *= Hkv;
     const int kBN = p.BM == 32 ? attn_keys(p.DP) / 2 : attn_keys(p.DP);
     const int64_t tiles_k = (max_k + kBN - 1) / kBN;
-    const int64_t want = (p.BM == 32 ? 2 : 4) * (int64_t)device_cus(), least = p.BM == 32 ? 8 : 16;
+    const int64_t want = (p.BM == 32 ? 2 : 4) * (int64_t)device_cus(), least = 8;
     int64_t n = groups > 0 && groups * 2 <= want ? want / groups : 1;
     if (n > tiles_k / least) n = tiles_k / least;
     if (n > 64) n = 64;
