@@ -68,19 +68,23 @@ __device__ __forceinline__ float block_max(float x, float* red) {
 // counting sort over 256 classes), so that no long tile starts last: with
 // sequences of many lengths in one batch the order of the slots leaves the
 // card waiting for the last long sequence.  Rows (KEYS false) or keys.  The
-// order inside a class is open; no result depends on it.
-template <bool KEYS>
-__device__ __forceinline__ void order_tiles(const AttnArgs& a, int* order) {
+// order inside a class is open; no result depends on it.  lds: ORDER ints of
+// the workgroup's, where the first slots' work is kept (it takes a search
+// through the offsets); the others' is looked up again.
+template <bool KEYS, int ORDER>
+__device__ __forceinline__ void order_tiles(const AttnArgs& a, int* order, uint8_t* lds) {
     constexpr int kTile = KEYS ? kAttnDkvKeys : kAttnRows;
-    __shared__ int count[257];
+    static_assert(kThreads == 256, "a thread per class");
+    __shared__ int count[257], sums[kThreads / 64];
     __shared__ int top;
+    int* kept = reinterpret_cast<int*>(lds);
     const int tid = threadIdx.x;
     const int64_t* cu = KEYS ? a.cu_k : a.cu_q;
     const int64_t T = KEYS ? a.Tk : a.Tq, mult = KEYS ? 1 : a.G;
     const int n = (int)(T * mult / kTile + a.S);
     // keys that the tile's last row sees, or queries that see the tile's first
     // key; -1: an empty slot
-    auto work = [&](int slot) {
+    auto look_up = [&](int slot) {
         int tile;
         const Seq sq = load_seq(a, slot_owner(cu, a.S, T, mult, kTile, slot, tile));
         const int64_t len = KEYS ? sq.nk : (int64_t)sq.nq * a.G, first = (int64_t)tile * kTile;
@@ -96,25 +100,38 @@ __device__ __forceinline__ void order_tiles(const AttnArgs& a, int* order) {
         const int64_t lim = a.causal ? div_g(a, (int)last) + 1 + off : sq.nk;
         return lim > 0 ? (int)lim : 0;
     };
-    for (int i = tid; i < 257; i += kThreads) count[i] = 0;
-    if (tid == 0) top = 1;
+    count[tid] = 0;
+    if (tid == 0) {
+        count[256] = 0;
+        top = 1;
+    }
     __syncthreads();
     int most = 1;
-    for (int i = tid; i < n; i += kThreads) most = max(most, work(i));
+    for (int i = tid; i < n; i += kThreads) {
+        const int w = look_up(i);
+        if (i < ORDER) kept[i] = w;                         // read by this thread only
+        most = max(most, w);
+    }
     atomicMax(&top, most);
     __syncthreads();
     const float per = 255.0f / (float)top;
+    auto work = [&](int i) { return i < ORDER ? kept[i] : look_up(i); };
     auto place = [&](int w) { return w < 0 ? 256 : 255 - (int)((float)w * per); };
     for (int i = tid; i < n; i += kThreads) atomicAdd(&count[place(work(i))], 1);
     __syncthreads();
-    if (tid == 0) {
-        int sum = 0;
-        for (int i = 0; i < 257; ++i) {
-            const int c = count[i];
-            count[i] = sum;
-            sum += c;
-        }
+    // each class starts where the ones before it end
+    const int own = count[tid];
+    int sum = own;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int below = __shfl_up(sum, d);
+        if ((tid & 63) >= d) sum += below;
     }
+    if ((tid & 63) == 63) sums[tid >> 6] = sum;
+    __syncthreads();
+    for (int i = 0; i < tid >> 6; ++i) sum += sums[i];
+    count[tid] = sum - own;
+    if (tid == 255) count[256] = sum;
     __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
         const int w = work(i);
@@ -124,13 +141,13 @@ __device__ __forceinline__ void order_tiles(const AttnArgs& a, int* order) {
 
 template <int DP, bool VEC>
 __global__ __launch_bounds__(kThreads) void fwd_image_kernel(AttnArgs a) {
+    using I = FwdImage<DP>;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[I::kBytes];
     if (a.row_order && blockIdx.x == 0) {
-        order_tiles<false>(a, a.row_order);
+        order_tiles<false, I::kBytes / 4>(a, a.row_order, lds);
         return;
     }
     const int block = blockIdx.x - (a.row_order ? 1 : 0);
-    using I = FwdImage<DP>;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[I::kBytes];
     const int tid = threadIdx.x, hk = block % a.Hkv, t = block / a.Hkv;
     const int64_t t0 = (int64_t)t * I::N;
     uint32_t* noted = reinterpret_cast<uint32_t*>(lds + I::kNoted);
@@ -159,8 +176,8 @@ __global__ __launch_bounds__(kThreads) void key_image_kernel(AttnArgs a) {
     const int tid = threadIdx.x;
     if (blockIdx.x == 0 && tid < 2) a.norms[tid] = 0.0f;
     if (a.row_order && blockIdx.x < 2) {
-        if (blockIdx.x == 0) order_tiles<false>(a, a.row_order);
-        else order_tiles<true>(a, a.key_order);
+        if (blockIdx.x == 0) order_tiles<false, I::kBytes / 4>(a, a.row_order, lds);
+        else order_tiles<true, I::kBytes / 4>(a, a.key_order, lds);
         return;
     }
     if (a.key_tiles == 0) return;
