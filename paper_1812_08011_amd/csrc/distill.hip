@@ -1,12 +1,15 @@
 // distill_loss: Kullback-Leibler loss against a teacher's top logits and the
 // gradient of the student's logits.  One workgroup per row.
 //
-// HBM-bound: a row's logits are read once and stay in registers as they are
-// stored until the gradient is written; exp(z / tau - max) is taken twice, for
-// the sum and for the gradient (keeping it would take twice the registers of
-// FP16 logits and halve the rows that a CU works on at once: 132 us against 126
-// for 4096 x 32768).  Rows past the registers (131072 FP16 logits, 65536 floats)
-// are read a second time, mostly from the caches.
+// HBM-bound: every logit is read once from memory and every gradient written
+// once.  Between the two, floats stay in registers (rows of 65536 at most)
+// where the memory would have to give them again: 4096 x 32768 floats take
+// 207 us, read twice 277 us.  FP16 logits are read a second time, from the
+// caches: a first pass that takes maximum and sum together decodes a logit once
+// more instead of twice more, and a row in flight costs no registers, so a CU
+// works on more rows: 4096 x 32768 in 143 us (4 bytes a logit, 3.8 TB/s), from
+// registers 159 us; 2048 x 50001, rows at odd addresses, 123 and 189 us.
+// exp(z / tau - max) is taken twice, for the sum and for the gradient.
 #include "lm_formats.h"
 
 namespace fp8t {
@@ -281,14 +284,23 @@ void launch_rows(const DistillArgs& a, hipStream_t stream) {
 
 template <int FZ, int FG>
 void launch(const DistillArgs& a, hipStream_t stream) {
-    // the fewest threads whose registers (64 for the row at most) hold it
-    constexpr int kMost = FZ == FP8T_FMT_FP16 ? 16 : 8;
-    if (a.V <= 256 * 8) launch_rows<FZ, FG, 256, 1>(a, stream);
-    else if (a.V <= 256 * 32) launch_rows<FZ, FG, 256, 4>(a, stream);
-    else if (a.V <= 256 * 8 * kMost) launch_rows<FZ, FG, 256, kMost>(a, stream);
-    else if (a.V <= 512 * 8 * kMost) launch_rows<FZ, FG, 512, kMost>(a, stream);
-    else if (a.V <= 1024 * 8 * kMost) launch_rows<FZ, FG, 1024, kMost>(a, stream);
-    else launch_rows<FZ, FG, 1024, 0>(a, stream);
+    // FP16: threads by the work of a row.  4096 x 10000: 44 us with 256, 51 with
+    // 512; 4096 x 32768: 160 and 143; 512 x 300000: 200 with 512, 188 with 1024.
+    // Floats: the fewest threads whose registers (64 for the row at most) hold
+    // it, as the waits at a row's sums cost more with more waves (4096 x 6000:
+    // 39 us with 256, 61 with 1024); then a second reading.
+    if constexpr (FZ == FP8T_FMT_FP16) {
+        if (a.V <= 12288) launch_rows<FZ, FG, 256, 0>(a, stream);
+        else if (a.V <= 65536) launch_rows<FZ, FG, 512, 0>(a, stream);
+        else launch_rows<FZ, FG, 1024, 0>(a, stream);
+    } else {
+        if (a.V <= 256 * 8) launch_rows<FZ, FG, 256, 1>(a, stream);
+        else if (a.V <= 256 * 32) launch_rows<FZ, FG, 256, 4>(a, stream);
+        else if (a.V <= 256 * 64) launch_rows<FZ, FG, 256, 8>(a, stream);
+        else if (a.V <= 512 * 64) launch_rows<FZ, FG, 512, 8>(a, stream);
+        else if (a.V <= 1024 * 64) launch_rows<FZ, FG, 1024, 8>(a, stream);
+        else launch_rows<FZ, FG, 1024, 0>(a, stream);
+    }
 }
 
 }  // namespace
