@@ -8,8 +8,9 @@
  * allocates or synchronizes, work is enqueued on `stream`, arguments are
  * validated before anything is enqueued, sizes and strides count elements.
  *
- * Results are functions of the inputs alone on a given device (no atomics
- * whose order could change them).  Sums, softmax statistics and log-sum-exps
+ * Results are functions of the arguments alone on a given device (no atomics
+ * whose order could change them); attention's size hints and workspace choose
+ * the order of its sums, so a call with others may differ in the last bits.  Sums, softmax statistics and log-sum-exps
  * are FP32; every result is rounded once, from FP32, to its storage format.
  */
 #ifndef FP8TRAIN_LM_H
@@ -104,8 +105,10 @@ int rotary_embed(const void* x, int x_format, int64_t x_ts, int64_t x_hs, const 
  * max_q, max_k: the longest nq and nk, which choose the plan (a wrong value
  * costs speed only).  sm_scale > 0 and finite.
  * workspace: attn_fwd_fp8_workspace_size bytes for the fastest plan, or none
- * (workspace_bytes == 0, then a plan that needs none); it holds the partial
- * results of key ranges that several workgroups share.
+ * (workspace_bytes == 0, then a plan that needs none); it holds keys and
+ * values laid out for the matrix cores, an order of the tiles and the partial
+ * results of key ranges that several workgroups share.  Nothing in it is kept
+ * from one call for the next.
  * Errors: FP8T_EINVAL (negative size, D not 1 .. FP8T_ATTN_MAX_D, Hq not a
  * multiple of Hkv, Hq above 65535, S, Tk or Tq Hq / Hkv above 2^31 - 4097, a
  * flag not 0/1, sm_scale not positive and finite, negative input stride, an
@@ -143,7 +146,9 @@ size_t attn_fwd_fp8_workspace_size(int64_t S, int64_t Tq, int64_t Tk, int64_t ma
  * The two products with p_j and dS_j use them as IEEE half scaled by a power
  * of two (chosen from the largest norms of d_o's and v's rows).
  * workspace: at least attn_bwd_fp8_workspace_size bytes, 16-byte aligned (it
- * holds delta and the norms).  Every other convention is attn_fwd_fp8's.
+ * holds the norms, delta, queries, errors, keys and values laid out for the
+ * matrix cores, an order of the tiles and partial results of dk and dv).
+ * Every other convention is attn_fwd_fp8's.
  * Errors: as attn_fwd_fp8, FP8T_EINVAL for another grad_format or a workspace
  * that is not 16-byte aligned, and FP8T_EWORKSPACE for workspace_bytes below
  * the query (0 included, where the query is not 0).

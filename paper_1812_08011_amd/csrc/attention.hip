@@ -83,6 +83,9 @@ extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     a.o8_hs = o8_hs;
     a.o8_scale = o8_scale;
     a.lse = lse;
+    // Other operands are read byte by byte: 4096 tokens, 16 heads of 128 forward
+    // 140 us in place of 122, backward 448 in place of 350; 300 tokens forward,
+    // where every tile pays, 46 in place of 14.
     const bool vec = D % 16 == 0 && rows16(a.q) && rows16(a.k) && rows16(a.v);
     attn_fwd_launch(a, p, vec, workspace, stream);
     return launch_status();

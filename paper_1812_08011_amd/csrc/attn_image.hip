@@ -1,5 +1,10 @@
 // Builds the images (attn_image.h).  A workgroup builds one tile of one head in
 // LDS and writes it out 16 bytes a thread.
+//
+// Bound by what they read and write.  8192 tokens of 128: keys of 4 heads for
+// the forward pass 7 us (8 MB in, 13 out), keys for the backward pass 14 us (8
+// in, 18 out, and the norms), queries and errors of 16 heads 40 us (67 MB with
+// o in, 105 out: 4.3 TB/s).
 #include "attn_image.h"
 
 namespace fp8t {
@@ -67,7 +72,11 @@ __device__ __forceinline__ float block_max(float x, float* red) {
 // Orders the tiles of all sequences by their work, the longest first (a
 // counting sort over 256 classes), so that no long tile starts last: with
 // sequences of many lengths in one batch the order of the slots leaves the
-// card waiting for the last long sequence.  Rows (KEYS false) or keys.  The
+// card waiting for the last long sequence.  8 sequences of 1 to 8192 tokens, 16
+// heads of 64: forward 224 us, in the order of the slots 240; backward 726 and
+// 781.  8 causal sequences of 2048, 16 heads of 128: 153 and 164; 606 and 703.
+// Sequences of one length gain too, by their causal tiles.  It costs 4 us of
+// one workgroup beside the others.  Rows (KEYS false) or keys.  The
 // order inside a class is open; no result depends on it.  lds: ORDER ints of
 // the workgroup's, where the first slots' work is kept (it takes a search
 // through the offsets); the others' is looked up again.
