@@ -6,8 +6,10 @@
 // address.  A head's entries past R are units of sixteen that are only
 // converted.
 //
-// 16384 tokens of 40 heads of 128, FP16 to FP8: 49 us, 5.1 TB/s, a large copy's
-// rate.  5003 tokens of 12 heads of 80, FP16 to FP16: 9 us (2.2 TB/s; 11 us from
+// 16384 tokens of 40 heads of 128, FP16 to FP8: 64 us, 3.9 TB/s (a copy of 1 GiB
+// runs at 5.2), and 49 us where the caches still hold part of the operands;
+// four heads a thread, or one or four of them in flight in place of two, change
+// that by 3% either way.  5003 tokens of 12 heads of 80, FP16 to FP16: 9 us (2.2 TB/s; 11 us from
 // cold caches, most of it the reduction of the angles and one round of loads).
 // One token: 3.5 us, a launch.
 #include "lm_formats.h"
@@ -140,8 +142,8 @@ template <int FX, int FY>
 void launch(RotaryArgs a, int interleaved, hipStream_t stream) {
     a.pair_units = (a.R / 2 + 7) / 8;
     a.units = a.pair_units + (a.D - a.R + 15) / 16;
-    // Eight heads a thread (16384 x 40 x 128: 50 us, with one head 81, the
-    // angles once each); fewer where that leaves the card empty, below 2048
+    // Eight heads a thread (16384 x 40 x 128 in part cached: 50 us, with one head
+    // 81, since its angles are used once); fewer where that leaves the card empty, below 2048
     // threads a CU (1024 x 40 x 128: 8.4 us, with eight heads 13; 256 x 8 x 128:
     // 5 and 12).
     const int64_t want = (int64_t)device_cus() * 2048;
