@@ -110,7 +110,9 @@ int rotary_embed(const void* x, int x_format, int64_t x_ts, int64_t x_hs, const 
  * results of key ranges that several workgroups share.  Nothing in it is kept
  * from one call for the next.
  * Errors: FP8T_EINVAL (negative size, D not 1 .. FP8T_ATTN_MAX_D, Hq not a
- * multiple of Hkv, Hq above 65535, S, Tk or Tq Hq / Hkv above 2^31 - 4097, a
+ * multiple of Hkv, Hq above 65535, S, Tk or Tq Hq / Hkv above 2^31 - 4097, more
+ * than 2^24 - 1 tiles of rows or keys (S Hkv and one for every 32 or more rows
+ * or 64 or more keys of a head), a
  * flag not 0/1, sm_scale not positive and finite, negative input stride, an
  * output stride that makes rows overlap, NULL pointer for non-empty data, no output, NULL
  * workspace with workspace_bytes > 0, or one that is not 16-byte aligned where

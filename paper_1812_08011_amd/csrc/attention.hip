@@ -52,6 +52,7 @@ extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     if ((o && !rows_apart(Tq, Hq, D, o_ts, o_hs)) || (o8 && !rows_apart(Tq, Hq, D, o8_ts, o8_hs)))
         return FP8T_EINVAL;
     AttnFwdPlan p = attn_fwd_plan(S, Tq, Tk, max_q, max_k, Hq, Hkv, D);
+    if (!p.fits) return FP8T_EINVAL;
     if (workspace_bytes && workspace_bytes < p.bytes) return FP8T_EWORKSPACE;
     if (p.bytes && !workspace_bytes) {
         p.splits = 1;
@@ -124,6 +125,7 @@ extern "C" int attn_bwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
         !rows_apart(Tk, Hkv, D, dv_ts, dv_hs) || !aligned(workspace, 16))
         return FP8T_EINVAL;
     const AttnBwdPlan p = attn_bwd_plan(S, Tq, Tk, max_q, max_k, Hq, Hkv, D);
+    if (!p.fits) return FP8T_EINVAL;
     if (workspace_bytes < p.bytes) return FP8T_EWORKSPACE;
     AttnArgs a = {};
     a.q = {q, q_ts, q_hs};

@@ -418,6 +418,9 @@ AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     if (n > steps / 16) n = steps / 16;
     if (n > 16) n = 16;
     p.splits = n > 1 ? (int)n : 1;
+    p.fits = row_slots * Hkv <= kAttnGrid && tiles * Hkv <= kAttnGrid && p.key_tiles * Hkv < kAttnGrid - 1 &&
+             p.query_tiles * Hq <= kAttnGrid &&
+             (p.splits == 1 || Tk * Hkv * (2 * p.DP / 8) / kThreads < kAttnGrid);
     p.bytes = p.parts + (p.splits > 1 ? (size_t)p.splits * Tk * Hkv * 2 * p.DP * 4 : 0);
     return p;
 }

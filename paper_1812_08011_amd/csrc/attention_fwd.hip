@@ -616,6 +616,8 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     p.splits = n > 1 ? (int)n : 1;
     p.per = (int)((tiles_k + p.splits - 1) / p.splits);
     p.order = p.image && S > 1;
+    p.fits = p.slots * Hkv <= kAttnGrid &&
+             (!p.image || image_tiles(Tk, attn_keys(p.DP)) * Hkv < kAttnGrid);
     p.image_bytes = (size_t)image + (p.order ? (p.slots * 4 + 15) / 16 * 16 : 0);
     p.bytes = p.image_bytes +
               (p.splits > 1 ? (size_t)p.splits * p.slots * Hkv * p.BM * (p.DP * 4 + 8) : 0);

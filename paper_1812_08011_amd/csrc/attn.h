@@ -91,6 +91,8 @@ __device__ __forceinline__ int slot_owner(const int64_t* cu, int S, int64_t T, i
 }
 // The tile that a workgroup takes: the slot, and its sequence and place there.
 __device__ __forceinline__ int ordered_slot(const int* order, int n) { return order ? order[n] : n; }
+// Workgroups of 256 threads along a grid's first dimension.
+constexpr int64_t kAttnGrid = (1 << 24) - 1;
 inline int64_t slots(int64_t S, int64_t T, int64_t mult, int64_t tile) {
     return S > 0 ? T * mult / tile + S : 0;
 }

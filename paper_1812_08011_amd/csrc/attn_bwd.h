@@ -7,6 +7,7 @@ namespace fp8t {
 
 struct AttnBwdPlan {
     int DP, splits;                    // padded D; workgroups that share a key tile's queries
+    bool fits;                         // no grid is too large
     int64_t key_tiles, query_tiles;    // of the images
     // byte offsets into the workspace, and its size
     size_t norms, delta, key_image, query_image, order, key_order, parts, bytes;

@@ -8,6 +8,7 @@ namespace fp8t {
 struct AttnFwdPlan {
     int DP, BM, splits, per;           // padded D, rows per workgroup, key ranges and tiles in each
     int64_t slots;                     // row tiles of all sequences, empty ones included
+    bool fits;                         // no grid is too large
     bool image, order;                 // keys and values through images; row tiles in an order
     size_t image_bytes, bytes;         // workspace: images and order first, then partial results
 };
