@@ -393,6 +393,9 @@ void launch_fmt(const AttnArgs& a, int grad_format, hipStream_t stream) {
 AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int64_t max_k, int64_t Hq,
                           int64_t Hkv, int64_t D) {
     AttnBwdPlan p = {};
+    const int64_t G = Hkv ? Hq / Hkv : 1;
+    max_q = hint(max_q, G);
+    max_k = hint(max_k, 1);
     p.DP = D <= 64 ? 64 : 128;
     const auto up = [](int64_t n) { return (size_t)((n + 15) / 16 * 16); };
     p.key_tiles = image_tiles(Tk, 64);
@@ -404,14 +407,14 @@ AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
                                       (p.DP == 64 ? KeyImage<64>::kBytes : KeyImage<128>::kBytes);
     p.order = p.query_image + (size_t)(p.query_tiles * Hq) *
                                   (p.DP == 64 ? QueryImage<64>::kBytes : QueryImage<128>::kBytes);
-    const int64_t row_slots = slots(S, Tq, Hkv ? Hq / Hkv : 1, kAttnRows);
+    const int64_t row_slots = slots(S, Tq, G, kAttnRows);
     p.key_order = p.order + (S > 1 ? up(row_slots * 4) : 0);
     p.parts = p.key_order + (S > 1 ? up(slots(S, Tk, 1, kAttnDkvKeys) * 4) : 0);
     // The steps of a key tile are shared out where the tiles leave CUs idle,
     // until there are 4 workgroups per CU, with 16 steps of 32 queries each at
     // least.  8192 causal tokens, 4 key heads: 640 us and 25 for the join; with
     // 2 per CU 835 and 15 (the causal tiles differ in length), with 8 560 and 51.
-    const int64_t G = Hkv ? Hq / Hkv : 1, tiles = slots(S, Tk, 1, kAttnDkvKeys);
+    const int64_t tiles = slots(S, Tk, 1, kAttnDkvKeys);
     const int64_t some = S * ((max_k + kAttnDkvKeys - 1) / kAttnDkvKeys), groups = (tiles < some ? tiles : some) * Hkv;
     const int64_t steps = (max_q + 31) / 32 * G, want = 4 * (int64_t)device_cus();
     int64_t n = groups > 0 && 2 * groups <= want ? want / groups : 1;

@@ -597,6 +597,8 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
                           int64_t Hkv, int64_t D) {
     AttnFwdPlan p = {};
     const int64_t G = Hkv ? Hq / Hkv : 1;
+    max_q = hint(max_q, G);
+    max_k = hint(max_k, 1);
     p.DP = D <= 64 ? 64 : 128;
     p.BM = max_q * G <= 32 ? 32 : 128;
     p.slots = slots(S, Tq, G, p.BM);

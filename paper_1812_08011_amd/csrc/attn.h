@@ -96,5 +96,12 @@ constexpr int64_t kAttnGrid = (1 << 24) - 1;
 inline int64_t slots(int64_t S, int64_t T, int64_t mult, int64_t tile) {
     return S > 0 ? T * mult / tile + S : 0;
 }
+// The size hints as the plans take them: at most what a call may hold, so that
+// neither a plan's products nor a kernel's tile numbers (32 bits) overflow
+// whatever a caller expects.
+inline int64_t hint(int64_t n, int64_t mult) {
+    const int64_t most = kMaxGemmDim / (mult > 0 ? mult : 1);
+    return n < most ? n : most;
+}
 
 }  // namespace fp8t
