@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     const fmt_t<FX>* x = static_cast<const fmt_t<FX>*>(a.x) + t * a.x_ts;
     fmt_t<FY>* y = static_cast<fmt_t<FY>*>(a.y) + t * a.y_ts;
 #pragma unroll 2
-    for (int h = group; h < a.H; h += a.groups) {
+    for (uint32_t h = group; h < (uint32_t)a.H; h += a.groups) {   // the last step may pass 2^31
         float p[8], q[8];
         load_some<FX>(x + h * a.x_hs + i0, n0, p);
         load_some<FX>(x + h * a.x_hs + i1, n1, q);
