@@ -515,23 +515,25 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSpl
     tile = ntiles - 1 - tile;
     const int rr = blockIdx.y * (kThreads / 64) + wave, row = tile * BM + rr;
     if (rr >= BM || row >= nrows) return;
-    const int i = div_g(a, row), lim = a.causal ? i + 1 + sq.nk - sq.nq : sq.nk;
-    // lane z takes range z's reference and sum (there are at most 64)
+    const int i = div_g(a, row), off = sq.nk - sq.nq, lim = a.causal ? i + 1 + off : sq.nk;
+    // lane z takes range z's reference and sum (there are at most 64).  A range
+    // without a key has neither; one whose scores are all NaN has a sum of NaN,
+    // which has to come through.
     const int64_t stride = (int64_t)gridDim.x * BM, first = (int64_t)blockIdx.x * BM + rr;
     const float2 ml = lane < sp.n ? sp.ml[lane * stride + first] : make_float2(-INFINITY, 0.0f);
+    const bool some = ml.x != -INFINITY || ml.y != 0.0f;
     float m = ml.x;
 #pragma unroll
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    // a range without a key has no sums either
-    const float f = ml.x == -INFINITY ? 0.0f : ml.x == m ? 1.0f : exp2f(ml.x - m);
-    float l = f == 0.0f ? 0.0f : ml.y * f;
+    const float f = ml.x == m ? 1.0f : exp2f(ml.x - m);
+    float l = some ? ml.y * f : 0.0f;
 #pragma unroll
     for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
     float o[2] = {0.0f, 0.0f};
 #pragma unroll 4
     for (int z = 0; z < sp.n; ++z) {
+        if (!__shfl((int)some, z)) continue;
         const float w = __shfl(f, z);
-        if (w == 0.0f) continue;
 #pragma unroll
         for (int u = 0; u < DP / 64; ++u) o[u] += sp.o[(z * stride + first) * DP + 64 * u + lane] * w;
     }
