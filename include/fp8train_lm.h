@@ -89,7 +89,8 @@ int rotary_embed(const void* x, int x_format, int64_t x_ts, int64_t x_hs, const 
  *   s_j = sm_scale <q, K_j>,  p_j = exp(s_j) / sum exp(s),  o = sum p_j V_j,
  *   lse = log(sum exp(s))
  * A row that sees no key has o = +0 and lse = -Inf.  Keys that a row does not
- * see do not enter it, whatever they hold (NaN and Inf included).
+ * see do not enter it, whatever they hold (NaN and Inf included); an infinite
+ * value that it sees enters as that infinity, however small its p is.
  * <q, K_j> and sums are FP32 of exact products; p_j enters the second
  * product as IEEE half relative to the row's running maximum.
  *

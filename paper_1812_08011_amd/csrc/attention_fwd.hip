@@ -195,6 +195,23 @@ struct FwdRows {
         add_noted<ND>(bits, v, v_ts, j0, D, h, [&](int key) { return (uint32_t)key < (uint32_t)lim; },
                       [&](int d, int r, uint32_t c) { o[d][r] += fp8_nonfinite(c); });
     }
+
+    // Whether the sums are finite; those that are not, cleared.
+    __device__ __forceinline__ bool finite() const {
+        float top = 0.0f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) top = maximum3_abs(top, o[d][r], o[d][r + 1]);
+        return top < INFINITY;
+    }
+    __device__ __forceinline__ void clear_odd() {
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (!(__builtin_fabsf(o[d][r]) < INFINITY)) o[d][r] = 0.0f;
+    }
 };
 
 // A workgroup's tile of rows and this lane's row in it.
@@ -443,22 +460,29 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
                    });
         }
     }
-    if (__builtin_expect(__any(x.noted_any != 0), 0)) {
-        // the partial tiles again, each key's row looked at by the whole wave
-        int t = w.lim_lo / kBN > t0 ? w.lim_lo / kBN : t0;
-        if (KW > 1) t += (t0 + wave - t % KW + KW * KW) % KW;   // this wave's tiles
+    float l = both_halves(x.l, Add()), ref = x.ref;
+    // A value that is not finite in a tile that every row sees has made its
+    // column's sums Inf, or NaN where its p underflowed (0 x Inf): they start
+    // again from 0.
+    const bool odd = !x.finite() && l == l;
+    if (__builtin_expect(__any(x.noted_any != 0 || odd), 0)) {
+        if (odd) x.clear_odd();
+        // the wave's tiles again, 32 keys at a time looked at by the whole wave
 #pragma unroll 1
-        for (; t < t1; t += KW)
+        for (int t = t0 + (KW > 1 ? wave : 0); t < t1; t += KW)
 #pragma unroll 1
-            for (int j = t * kBN; j < (t + 1) * kBN && j < sq.nk; ++j) {
-                bool odd = false;
+            for (int j0 = t * kBN; j0 < (t + 1) * kBN && j0 < sq.nk; j0 += 32) {
+                uint32_t some = 0;
 #pragma unroll
-                for (int c = lane; c < DP; c += 64)
-                    if (c < a.D) odd |= (vp[(int64_t)j * a.v.ts + c] & 0x7Cu) == 0x7Cu;
-                if (__any(odd)) x.add(1u, j, w.lim, h, vp, a.v.ts, a.D);
+                for (int c = 0; c < NC; ++c) {
+                    const uint4 u = load_codes16<VEC>(vp + (int64_t)(j0 + l31) * a.v.ts, 32 * c + 16 * h, a.D,
+                                                      j0 + l31 < sq.nk);
+                    some |= nonfinite_in(u.x) | nonfinite_in(u.y) | nonfinite_in(u.z) | nonfinite_in(u.w);
+                }
+                const uint64_t rows = __ballot((some & 0x80808080u) != 0);
+                x.add((uint32_t)rows | (uint32_t)(rows >> 32), j0, w.lim, h, vp, a.v.ts, a.D);
             }
     }
-    float l = both_halves(x.l, Add()), ref = x.ref;
 
     if constexpr (KW > 1) {
         // join the waves: references first, then the scaled sums
@@ -476,7 +500,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
 #pragma unroll
         for (int v = 0; v < KW; ++v)
             l += refs[v][l31] == m ? ls[v][l31] : ls[v][l31] * exp2f(refs[v][l31] - m);
-        const float f = ref == m ? 1.0f : exp2f(ref - m);
+        const float f = part_weight(ref, m);
         float* xs = reinterpret_cast<float*>(vs);           // [wave - 1][register][lane]
         if (wave) {
 #pragma unroll
@@ -525,7 +549,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSpl
     float m = ml.x;
 #pragma unroll
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    const float f = ml.x == m ? 1.0f : exp2f(ml.x - m);
+    const float f = part_weight(ml.x, m);
     float l = some ? ml.y * f : 0.0f;
 #pragma unroll
     for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);

@@ -98,6 +98,10 @@ struct Widen {
     }
 };
 
+// Bits 7, 15, 23 and 31: whether the code bytes of a word are Inf or NaN.
+__device__ __forceinline__ uint32_t nonfinite_in(uint32_t w) {
+    return (w & 0x7C7C7C7Cu) + 0x04040404u;
+}
 // Code bytes that are Inf or NaN (exponent all ones), 0xFF each.
 __device__ __forceinline__ uint32_t nonfinite_bytes(uint32_t w) {
     const uint32_t t = (w & 0x7C7C7C7Cu) ^ 0x7C7C7C7Cu;          // 0 where the exponent is all ones
@@ -165,6 +169,13 @@ struct HalfTile {
 // Inf or NaN from its code.
 __device__ __forceinline__ float fp8_nonfinite(uint32_t c) {
     return __uint_as_float(((c & 0x80u) << 24) | kF32Inf | ((c & 3u) << 21));
+}
+
+// The weight, against the largest reference m, of sums held relative to `ref`.
+// It does not underflow to 0: an infinity that a seen value has left in the
+// sums stays one, and finite sums times 2^-126 are lost in any other rounding.
+__device__ __forceinline__ float part_weight(float ref, float m) {
+    return ref == m ? 1.0f : fmaxf(exp2f(ref - m), 0x1p-126f);
 }
 
 // Entries that are not finite, of the rows noted in `bits` (row 0 of them is
