@@ -339,7 +339,7 @@ def _rows(fn, t, like, dtype):
     if t.dtype != dtype:
         raise TypeError(f"{fn}: {t.dtype} where {dtype} is needed")
     ts, hs, ds = t.stride()
-    if ds != 1 and like[2] > 1:
+    if ds != 1 and like[2] > 1 and t.numel():      # an empty tensor may have any strides
         raise ValueError(f"{fn}: the last dimension must be contiguous")
     return t.data_ptr(), ts, hs
 
