@@ -628,7 +628,7 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     p.DP = D <= 64 ? 64 : 128;
     p.BM = max_q * G <= 32 ? 32 : 128;
     p.slots = slots(S, Tq, G, p.BM);
-    p.image = p.BM == 128 && max_q * G >= 4096;
+    p.image = p.BM == 128 && max_q * G >= 4096 && Tk > 0;     // no keys: no tiles to launch for
     const int64_t image = p.image ? image_tiles(Tk, attn_keys(p.DP)) * Hkv *
                                         (p.DP == 64 ? FwdImage<64>::kBytes : FwdImage<128>::kBytes)
                                   : 0;
