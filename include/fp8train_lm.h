@@ -146,10 +146,12 @@ size_t attn_fwd_fp8_workspace_size(int64_t S, int64_t Tq, int64_t Tk, int64_t ma
  * as q, k, v's.  Rows that see no key have dq = +0; keys that no query sees
  * have dK = dV = +0.
  * o (FP16 codes) and lse are attn_fwd_fp8's results for the same arguments.
- * The two products with p_j and dS_j use them as IEEE half scaled by a power
- * of two (chosen from the largest norms of d_o's and v's rows).
+ * The two products with p_j and dS_j use them as IEEE half: p_j times 2^15 (dV
+ * loses up to 2^-40 of each error e), dS_j times a power of two that the row
+ * (for dq) or the key (for dK) finds for itself, whatever other rows, keys and
+ * sequences hold.
  * workspace: at least attn_bwd_fp8_workspace_size bytes, 16-byte aligned (it
- * holds the norms, delta, queries, errors, keys and values laid out for the
+ * holds delta, queries, errors, keys and values laid out for the
  * matrix cores, an order of the tiles and partial results of dk and dv).
  * Every other convention is attn_fwd_fp8's.
  * Errors: as attn_fwd_fp8, FP8T_EINVAL for another grad_format or a workspace

@@ -8,9 +8,9 @@
 // delta = <e, o> enters as the start of the product <e, V_j>'s sums.
 //
 // The operands are IEEE halves, FP8 codes exactly.  p (at most 1) is held times
-// 2^15 and dS times a power of two (ds_scale), so that both keep all 11 bits
-// over 2^29 down from the largest: smaller ones are lost against a sum's final
-// rounding to 10 bits.  Sums are FP32.
+// 2^15: all 11 bits down to 2^-29, steps of 2^-39 below, so that dv loses at most
+// 2^-40 of every error it sums.  dS is held times a power of two that its row or
+// its key finds for itself (kDsFirst).  Sums are FP32.
 //
 // The three products of dq and the four of dk and dv bound them: with 8192
 // causal tokens, 16 heads of 128 and 4 key heads 412 GFLOP in 397 us (1038
@@ -28,16 +28,42 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// The power of two that dS = p (<e, v> - delta) is held times.  Both terms are
-// at most |e| |v| (delta is a mean of such products), so with the largest norms
-// the scaled dS stays below 2^15, and a dS down to 2^-29 of that bound keeps
-// all 11 bits of a half.
-__device__ __forceinline__ float ds_scale(const AttnArgs& a) {
-    const float bound = __builtin_sqrtf(a.norms[0]) * __builtin_sqrtf(a.norms[1]);
-    if (!(bound > 0.0f)) return 1.0f;
+// dS = p (<e, v> - delta) is held times a power of two of the lane's own -- a
+// row's in dq, a key's in dk -- so that what one row or key keeps does not
+// depend on any other.  It starts so large that any dS that reaches a result
+// has all 11 bits of a half, and goes down when one of the sum passes kDsRoom
+// (the largest half is 65504), the sums so far with it: the first steps of a
+// wave do that, later ones seldom.  The largest then lies in [2^11, 2^12) --
+// nearer to the largest half the sums went down more often, 2% of the time -- so
+// that a dS down to 2^-25 of it keeps all 11 bits, with steps of 2^-35 below.
+constexpr float kDsFirst = 0x1p64f;    // |<e, v>| and |delta| stay below 2^56: no overflow
+constexpr float kDsRoom = 61440.0f;
+__device__ __forceinline__ bool ds_passes(const float* ds) {
+    // two chains; a NaN passes nothing: its row's or its key's result is NaN
+    float a = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+        a = maximum3_abs(a, ds[r], ds[r + 1]);
+        b = maximum3_abs(b, ds[r + 2], ds[r + 3]);
+    }
+    return __any(maximum3_abs(kDsRoom, a, b) > kDsRoom);
+}
+// The factor that brings the largest finite one down; ds times it.
+__device__ __forceinline__ float ds_down(float* ds) {
+    float top = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const float x = __builtin_fabsf(ds[r]);
+        top = fmaxf(top, x < INFINITY ? x : 0.0f);
+    }
+    top = both_halves(top, [](float a, float b) { return fmaxf(a, b); });
+    if (!(top > kDsRoom)) return 1.0f;
     int e;
-    (void)__builtin_frexpf(bound, &e);                      // bound < 2^e
-    return __builtin_ldexpf(1.0f, 13 - e);
+    (void)__builtin_frexpf(top, &e);                        // top < 2^e
+    const float f = __builtin_ldexpf(1.0f, 12 - e);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ds[r] *= f;
+    return f;
 }
 
 // ---- dq ------------------------------------------------------------------------------------
@@ -93,13 +119,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
         ef[c][0] = widen(w.x, w.y);
         ef[c][1] = widen(w.z, w.w);
     }
-    const float sigma = ds_scale(a);
-    float lse2 = INFINITY, delta = 0.0f;                    // a row that sees nothing: p = 0
+    float sigma = kDsFirst, lse2 = INFINITY, delta = 0.0f;  // a row that sees nothing: p = 0
     if (lim > 0) {
         lse2 = a.lse[(int64_t)hq * a.Tq + tq] * kAttnLog2e;
         delta = a.delta[(int64_t)hq * a.Tq + tq] * sigma;
     }
-    const float sg = __uint_as_float(in_vgpr(__float_as_uint(sigma)));
 
     v16f o[ND];
 #pragma unroll
@@ -133,7 +157,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r], c2, -lse2));
-                ds[r] = p * __builtin_fmaf(dp[r], sg, -delta);
+                ds[r] = p * __builtin_fmaf(dp[r], sigma, -delta);
             }
             if (partial) {
                 int key = j0 + 32 * kt + 4 * h;
@@ -141,6 +165,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if ((uint32_t)(key + 8 * (r / 4) + r % 4) >= (uint32_t)lim) ds[r] = 0.0f;
+            }
+            if (__builtin_expect(ds_passes(ds), 0)) {
+                const float f = ds_down(ds);
+                sigma *= f;
+                delta *= f;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[d][r] *= f;
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -224,9 +257,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
         kf[c][1] = widen(w.z, w.w);
         vf[c] = load_codes16<VEC>(vp, 32 * c + 16 * h, a.D, j < sq.nk);
     }
-    const float sigma = ds_scale(a);
     // p is held times 2^15, dS times sigma: p (dP - delta) sigma 2^-15
-    const float sg = __uint_as_float(in_vgpr(__float_as_uint(__builtin_ldexpf(sigma, -kAttnPUp))));
+    float sg = j < sq.nk ? __builtin_ldexpf(kDsFirst, -kAttnPUp) : 0.0f;
 
     v16f dk[ND], dv[ND];
 #pragma unroll
@@ -285,6 +317,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
             for (int r = 0; r < 16; ++r)
                 if ((uint32_t)(i + 8 * (r / 4) + r % 4) >= seen_by) p[r] = ds[r] = 0.0f;
         }
+        if (__builtin_expect(ds_passes(ds), 0)) {
+            const float f = ds_down(ds);
+            sg *= f;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dk[d][r] *= f;
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const v8h pf = to_half8(p + 8 * t), sf = to_half8(ds + 8 * t);
@@ -311,7 +351,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
                           [&](int d, int r, uint32_t c) { dv[d][r] += fp8_nonfinite(c); });
         }
     }
-    const float fk = a.sm_scale / sigma * a.grad_scale, fv = __builtin_ldexpf(a.grad_scale, -kAttnPUp);
+    const float fk = __builtin_ldexpf(a.sm_scale / sg, -kAttnPUp) * a.grad_scale, fv = __builtin_ldexpf(a.grad_scale, -kAttnPUp);
     const int64_t t = sq.k0 + j;
     __syncthreads();                                        // the buffers are free
     float* xs = reinterpret_cast<float*>(lds + wave * kRowsOut);
@@ -400,8 +440,7 @@ AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     const auto up = [](int64_t n) { return (size_t)((n + 15) / 16 * 16); };
     p.key_tiles = image_tiles(Tk, 64);
     p.query_tiles = image_tiles(Tq, 32);
-    p.norms = 0;
-    p.delta = up((4 + p.key_tiles * Hkv) * 4);
+    p.delta = 0;
     p.key_image = p.delta + up(Hq * Tq * 4);
     p.query_image = p.key_image + (size_t)(p.key_tiles * Hkv) *
                                       (p.DP == 64 ? KeyImage<64>::kBytes : KeyImage<128>::kBytes);
@@ -431,7 +470,6 @@ AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
 void attn_bwd_launch(AttnArgs a, const AttnBwdPlan& p, int grad_format, bool vec, void* workspace,
                      hipStream_t stream) {
     uint8_t* w = static_cast<uint8_t*>(workspace);
-    a.norms = reinterpret_cast<float*>(w + p.norms);
     a.delta = reinterpret_cast<float*>(w + p.delta);
     a.key_image = w + p.key_image;
     a.query_image = w + p.query_image;

@@ -32,7 +32,6 @@ struct AttnArgs {
     int64_t dq_ts, dq_hs, dk_ts, dk_hs, dv_ts, dv_hs;
     float grad_scale;
     float* delta;            // Hq x Tq
-    float* norms;            // the largest squared row norms of e and v; v's per workgroup from 4 on
     // images (attn_image.h), [head][tile]
     uint8_t* key_image;
     uint8_t* query_image;

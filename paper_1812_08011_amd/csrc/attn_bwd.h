@@ -10,7 +10,7 @@ struct AttnBwdPlan {
     bool fits;                         // no grid is too large
     int64_t key_tiles, query_tiles;    // of the images
     // byte offsets into the workspace, and its size
-    size_t norms, delta, key_image, query_image, order, key_order, parts, bytes;
+    size_t delta, key_image, query_image, order, key_order, parts, bytes;
 };
 
 AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int64_t max_k, int64_t Hq,

@@ -3,7 +3,7 @@
 //
 // Bound by what they read and write.  8192 tokens of 128: keys of 4 heads for
 // the forward pass 7 us (8 MB in, 13 out), keys for the backward pass 14 us (8
-// in, 18 out, and the norms), queries and errors of 16 heads 40 us (67 MB with
+// in, 18 out), queries and errors of 16 heads 40 us (67 MB with
 // o in, 105 out: 4.3 TB/s).
 #include "attn_image.h"
 
@@ -50,25 +50,6 @@ __device__ __forceinline__ void write_image(const uint8_t* lds, uint8_t* dst) {
     for (int i = threadIdx.x; i < BYTES / 16; i += kThreads)
         reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(lds)[i];
 }
-// Squared norm of 16 codes.
-__device__ __forceinline__ float norm16(uint4 w) {
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-    float n = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float x = fp8_to_f32<0>((v[i / 4] >> (8 * (i % 4))) & 0xFFu);
-        n = __builtin_fmaf(x, x, n);
-    }
-    return n;
-}
-__device__ __forceinline__ float block_max(float x, float* red) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-}
-
 // Orders the tiles of all sequences by their work, the longest first (a
 // counting sort over 256 classes), so that no long tile starts last: with
 // sequences of many lengths in one batch the order of the slots leaves the
@@ -174,41 +155,29 @@ __global__ __launch_bounds__(kThreads) void fwd_image_kernel(AttnArgs a) {
     write_image<I::kBytes>(lds, a.key_image + ((int64_t)hk * a.key_tiles + t) * I::kBytes);
 }
 
-// Also the largest squared norm of the values' finite rows, per workgroup, and
-// a zero for what the next kernel takes the maximum into.
 template <int DP, bool VEC>
 __global__ __launch_bounds__(kThreads) void key_image_kernel(AttnArgs a) {
     using I = KeyImage<DP>;
     constexpr int U = (I::N / 4) * (DP / 8), VU = I::N * (DP / 16) / kThreads;
     __shared__ __attribute__((aligned(16))) uint8_t lds[I::kBytes];
-    __shared__ float red[kThreads / 64];
     const int tid = threadIdx.x;
-    if (blockIdx.x == 0 && tid < 2) a.norms[tid] = 0.0f;
     if (a.row_order && blockIdx.x < 2) {
         if (blockIdx.x == 0) order_tiles<false, I::kBytes / 4>(a, a.row_order, lds);
         else order_tiles<true, I::kBytes / 4>(a, a.key_order, lds);
         return;
     }
-    if (a.key_tiles == 0) return;
     const int block = blockIdx.x - (a.row_order ? 2 : 0);
     const int hk = block % a.Hkv, t = block / a.Hkv;
     const int64_t t0 = (int64_t)t * I::N;
     uint32_t* noted = reinterpret_cast<uint32_t*>(lds + I::kNoted);
     if (tid < 4) noted[tid] = 0u;
-    float top = 0.0f;
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
         const int id = tid + u * kThreads, row = id / (DP / 16), col = id % (DP / 16) * 16;
-        const uint4 w = load_codes16<VEC>(a.v.p + (t0 + row) * a.v.ts + (int64_t)hk * a.v.hs, col, a.D,
-                                          t0 + row < a.Tk);
-        *reinterpret_cast<uint4*>(lds + I::kV + row * I::CT::kRow + col) = w;
-        float n = norm16(w);
-#pragma unroll
-        for (int d = DP / 32; d; d >>= 1) n += __shfl_xor(n, d);
-        if (n < INFINITY) top = fmaxf(top, n);
+        *reinterpret_cast<uint4*>(lds + I::kV + row * I::CT::kRow + col) = load_codes16<VEC>(
+            a.v.p + (t0 + row) * a.v.ts + (int64_t)hk * a.v.hs, col, a.D, t0 + row < a.Tk);
     }
-    top = block_max(top, red);
-    if (tid == 0) a.norms[4 + block] = top;
+    __syncthreads();
     uint2 w[4];
     if (tid < U) {
         load_unit<I::N, DP, VEC>(w, a.k, hk, t0, a.Tk, a.D, tid);
@@ -218,14 +187,12 @@ __global__ __launch_bounds__(kThreads) void key_image_kernel(AttnArgs a) {
     write_image<I::kBytes>(lds, a.key_image + ((int64_t)hk * a.key_tiles + t) * I::kBytes);
 }
 
-// Also delta = <e, o> of every row, and the largest squared norms of e's and
-// v's finite rows (maxima do not depend on the order of the atomics).
+// Also delta = <e, o> of every row; o has the 10 bits that it was stored with.
 template <int DP, bool VEC>
 __global__ __launch_bounds__(kThreads) void query_image_kernel(AttnArgs a, int vec_o) {
     using I = QueryImage<DP>;
     constexpr int U = (I::N / 4) * (DP / 8);
     __shared__ __attribute__((aligned(16))) uint8_t lds[I::kBytes];
-    __shared__ float red[kThreads / 64];
     const int tid = threadIdx.x, hq = blockIdx.x % a.Hq, t = blockIdx.x / a.Hq;
     const int64_t t0 = (int64_t)t * I::N;
     uint32_t* noted = reinterpret_cast<uint32_t*>(lds + I::kNoted);
@@ -240,7 +207,6 @@ __global__ __launch_bounds__(kThreads) void query_image_kernel(AttnArgs a, int v
     }
     __syncthreads();
     // 16 lanes per row, 8 entries each
-    float top = 0.0f;
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
         const int row = pass * 16 + tid / 16, d0 = tid % 16 * 8;
@@ -262,19 +228,14 @@ __global__ __launch_bounds__(kThreads) void query_image_kernel(AttnArgs a, int v
                     if (d0 + i < a.D) oc[i / 2] |= (uint32_t)o[d0 + i] << (16 * (i % 2));
             }
         }
-        float s = 0.0f, n = 0.0f;
+        float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float e = fp8_to_f32<0>(((i < 4 ? w.x : w.y) >> (8 * (i % 4))) & 0xFFu);
             s = __builtin_fmaf(e, fp16_to_f32((oc[i / 2] >> (16 * (i % 2))) & 0xFFFFu), s);
-            n = __builtin_fmaf(e, e, n);
         }
 #pragma unroll
-        for (int d = 8; d; d >>= 1) {
-            s += __shfl_xor(s, d);
-            n += __shfl_xor(n, d);
-        }
-        if (n < INFINITY) top = fmaxf(top, n);
+        for (int d = 8; d; d >>= 1) s += __shfl_xor(s, d);
         if (tid % 16 == 0) {
             float l = INFINITY;                             // no such row, or one that sees nothing: p = 0
             if (live) {
@@ -286,25 +247,13 @@ __global__ __launch_bounds__(kThreads) void query_image_kernel(AttnArgs a, int v
             *reinterpret_cast<float*>(lds + I::delta(row / 4) + 4 * (row % 4)) = live ? -s : 0.0f;
         }
     }
-    top = block_max(top, red);
-    // non-negative floats order as their bits; most workgroups find that their
-    // maximum is no news and leave the one address alone
-    auto raise = [&](int k, float x) {
-        uint32_t* p = reinterpret_cast<uint32_t*>(a.norms) + k;
-        const uint32_t u = __float_as_uint(x);
-        if (u > __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(p, u);
-    };
-    if (tid == 0) raise(0, top);
-    const int64_t nv = a.key_tiles * a.Hkv, i = (int64_t)blockIdx.x * kThreads + tid;
-    for (int64_t j = i; j < nv; j += (int64_t)gridDim.x * kThreads) raise(1, a.norms[4 + j]);
     write_image<I::kBytes>(lds, a.query_image + ((int64_t)hq * a.query_tiles + t) * I::kBytes);
 }
 
 template <int DP, bool VEC>
 void launch_bwd(const AttnArgs& a, bool vec_o, hipStream_t stream) {
     const int64_t nk = a.key_tiles * a.Hkv + (a.row_order ? 2 : 0);
-    hipLaunchKernelGGL((key_image_kernel<DP, VEC>), dim3((unsigned)(nk ? nk : 1)), dim3(kThreads), 0,
-                       stream, a);
+    if (nk) hipLaunchKernelGGL((key_image_kernel<DP, VEC>), dim3((unsigned)nk), dim3(kThreads), 0, stream, a);
     if (a.query_tiles)
         hipLaunchKernelGGL((query_image_kernel<DP, VEC>), dim3((unsigned)(a.query_tiles * a.Hq)),
                            dim3(kThreads), 0, stream, a, (int)vec_o);
