@@ -33,9 +33,11 @@ struct DistillArgs {
     float to2, tau, grad_scale;        // to2 = log2(e) / tau
 };
 
-// Exponents are kept in base 2: with c = RN(m to2), m the row's maximum, an
-// entry's is fma(z, to2, -c): one rounding of a small number.  The rounding of
-// c itself cancels between an entry and the sum.
+// An entry's exponent is that of its distance from the row's maximum m, in base
+// 2: (x - m) to2.  The distance is exact or off by 2^-24 of itself, whatever m
+// is -- x to2 - m to2 would overflow, or lose the distance, where every logit of
+// a row is a mask's.
+__device__ __forceinline__ float exponent(float x, float m, float to2) { return (x - m) * to2; }
 
 // Two reductions at once over the workgroup's T threads.
 template <int T, typename OP>
@@ -172,12 +174,12 @@ __global__ __launch_bounds__(T, T / 256) void distill_kernel(DistillArgs a) {
 #pragma unroll
             for (int i = 1; i < 8; ++i) top8 = fmaxf(top8, x[i]);
             if (!(top8 <= m.x)) {
-                if (m.x != -INFINITY) s *= exp2f(m.x * to2 - top8 * to2);
+                if (m.x != -INFINITY) s *= exp2f(exponent(m.x, top8, to2));
                 m.x = top8;
             }
-            const float c = m.x == -INFINITY ? 0.0f : m.x * to2;
+            const float c = m.x == -INFINITY ? 0.0f : m.x;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], to2, -c));
+            for (int i = 0; i < 8; ++i) s += __builtin_amdgcn_exp2f(exponent(x[i], c, to2));
         }
     }
     const float own = m.x;
@@ -190,7 +192,6 @@ __global__ __launch_bounds__(T, T / 256) void distill_kernel(DistillArgs a) {
         }
         return;
     }
-    const float c = m.x * to2, ct = m.y * to2;
     float2 sum = make_float2(0.0f, 0.0f);
     if constexpr (NV > 0) {
 #pragma unroll
@@ -199,32 +200,33 @@ __global__ __launch_bounds__(T, T / 256) void distill_kernel(DistillArgs a) {
             float x[8];
             values_of<FZ>(raw[i], special, x);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum.x += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], to2, -c));
+            for (int j = 0; j < 8; ++j) sum.x += __builtin_amdgcn_exp2f(exponent(x[j], m.x, to2));
         }
     } else {
-        // c's rounding as the second reading will have it
-        if (own == own && own != -INFINITY) s *= exp2f(own * to2 - c);
+        if (own == own && own != -INFINITY) s *= exp2f(exponent(own, m.x, to2));
         sum.x = m.x == -INFINITY || m.x != m.x ? NAN : s;
     }
     for (int i = tid; i < a.k; i += T)
-        if (at[i] >= 0) sum.y += exp2f(__builtin_fmaf(q[i], to2, -ct));
+        if (at[i] >= 0) sum.y += exp2f(exponent(q[i], m.y, to2));
     sum = block_both<T>(sum, red, Sum());
     const float log_s = log2f(sum.x), log_st = log2f(sum.y), inv = 1.0f / sum.x;
 
+    // the loss's terms in natural logarithms: a target on a logit at the type's
+    // lowest value has a finite one
     float2 kl = make_float2(0.0f, 0.0f);
     for (int i = tid; i < a.k; i += T) {
-        float qi = 0.0f, xi = 0.0f;
+        float qi = 0.0f, pi = 0.0f;
         if (at[i] >= 0) {
-            const float lq = __builtin_fmaf(q[i], to2, -ct) - log_st;
+            const float lq = exponent(q[i], m.y, to2) - log_st;
             qi = exp2f(lq);
-            xi = __builtin_fmaf(xt[i], to2, -c);
-            if (qi != 0.0f) kl.x += qi * (lq - (xi - log_s));
+            pi = exp2f(exponent(xt[i], m.x, to2)) * inv;
+            if (qi != 0.0f) kl.x += qi * ((lq + log_s) * kLn2 - (xt[i] - m.x) / a.tau);
         }
         q[i] = qi;
-        xt[i] = exp2f(xi) * inv;
+        xt[i] = pi;
     }
     kl = block_both<T>(kl, red, Sum());
-    if (tid == 0 && a.loss) a.loss[n] = w * (a.tau * a.tau) * (kl.x * kLn2);
+    if (tid == 0 && a.loss) a.loss[n] = w * (a.tau * a.tau) * kl.x;
     if (!g) return;
     const float f = w * (a.tau * a.grad_scale), fi = f * inv;
     // every |g| is at most |f|
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(T, T / 256) void distill_kernel(DistillArgs a) {
         float x[8];
         values_of<FZ>(e, odd, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], to2, -c)) * fi;
+        for (int j = 0; j < 8; ++j) x[j] = __builtin_amdgcn_exp2f(exponent(x[j], m.x, to2)) * fi;
         store_eight<FG>(g, v, a.V, x, plain);
     };
     if constexpr (NV > 0) {
