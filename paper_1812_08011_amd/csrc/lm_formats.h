@@ -46,17 +46,19 @@ __device__ __forceinline__ uint32_t fp16_nonfinite(uint32_t w) {
     return (w & 0x7E007E00u) + 0x02000200u;
 }
 
-// Two FP16 codes of finite values below FP16's largest, rounded to nearest
-// even: the values times 2^-96 have FP16's exponent in a float's exponent
-// field, so 14 bits are rounded off.  (Below 2^-30 that product itself rounds,
-// at 2^-14 of FP16's step.)
+// Two FP16 codes of values below 2^31 in magnitude, rounded to nearest even once:
+// with E the value's power of two, but at least 2^-30 (below, FP16's step stays
+// what it is there), the sum |x| + 2^14 E has FP16's step at x, and what it
+// passes 2^14 E by is the significand; it carries into the exponent by itself.
 __device__ __forceinline__ uint32_t fp16_pair(float a, float b) {
     uint32_t r[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        uint32_t u = __float_as_uint((i ? b : a) * 0x1p-96f);
-        u += 0x1FFFu + ((u >> 14) & 1u);
-        r[i] = ((u >> 14) & 0x7FFFu) | ((u >> 16) & 0x8000u);
+        const float x = i ? b : a;
+        const uint32_t u = __float_as_uint(x), e0 = 97u << 23, e = max(u & 0x7F800000u, e0);
+        const float sum = __builtin_fabsf(x) + __uint_as_float(e + (14u << 23));
+        const uint32_t code = __float_as_uint(sum) - e + (e >> 14) - ((14u << 23) + (e0 >> 14));
+        r[i] = code | ((u >> 16) & 0x8000u);
     }
     return r[0] | (r[1] << 16);
 }
