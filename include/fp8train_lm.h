@@ -61,8 +61,8 @@ int fp16_dequantize(const uint16_t* src, float scale, void* dst, int dst_format,
  *
  * inverse = 1 is the gradient: with y = rotary_embed(x) and an error e of y,
  * the error of x is rotary_embed(e) with inverse = 1 and the same mscale.
- * The angle is reduced in double precision, so positions of any size keep
- * float accuracy.  freqs: R/2 doubles on the device; scaling for long
+ * The angle is reduced exactly enough that positions of any size keep float
+ * accuracy (frequencies up to 2^16).  freqs: R/2 doubles on the device; scaling for long
  * contexts is in the table (and mscale).  positions: T int64, any sign.
  *
  * x: T x H x D in x_format with strides x_ts (tokens) and x_hs (heads), the D

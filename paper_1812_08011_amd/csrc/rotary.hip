@@ -32,15 +32,35 @@ struct RotaryArgs {
     int tokens;                        // per workgroup (gridDim.y > 1: one)
 };
 
+// The fraction of a turn, in [-1/2, 1/2], of position * freq where the product in
+// double precision has lost it: freq / (2 pi) in two doubles, the position in
+// two parts of 32 bits, each product with its rounding error.  Off by 2^-44 of a
+// turn and of freq.
+__device__ __forceinline__ float far_fraction(int64_t position, double freq) {
+    constexpr double kHi = 0x1.45f306dc9c883p-3, kLo = -0x1.6b01ec5417056p-57;   // 1 / (2 pi)
+    const double g = freq * kHi, g2 = __builtin_fma(freq, kHi, -g) + freq * kLo;
+    const int64_t low = (int64_t)((uint64_t)position & 0xFFFFFFFFu);
+    const double part[2] = {(double)(position - low), (double)low};              // both exact
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const double t = part[i] * g, e = __builtin_fma(part[i], g, -t) + part[i] * g2;
+        sum += (t - __builtin_rint(t)) + (e - __builtin_rint(e));
+    }
+    return (float)(sum - __builtin_rint(sum));
+}
+
 // cos and sin of position * freq: the angle in turns is reduced in double
 // precision (a float angle of 10^5 radians is off by 0.004), its fraction in
-// [-1/2, 1/2] holds float accuracy whatever the position.
+// [-1/2, 1/2] holds float accuracy.  Up to 2^20 turns one product is off by
+// 2^-31 of a turn at most.
 // The nearest quarter turn is taken off; on the eighth of a turn that is left,
 // either way, the Taylor series to the 9th and 8th power are off by less than
 // 3e-8, half a step of FP32 at 1.
 __device__ __forceinline__ float2 turn(int64_t position, double freq, float m, int inverse) {
     const double turns = (double)position * (freq * 0.15915494309189533577);
-    const float f = (float)(turns - __builtin_rint(turns));
+    float f = (float)(turns - __builtin_rint(turns));
+    if (__builtin_expect(!(__builtin_fabs(turns) <= 0x1p20), 0)) f = far_fraction(position, freq);
     const float k = __builtin_rintf(4.0f * f), r = __builtin_fmaf(k, -0.25f, f), r2 = r * r;
     float s = __builtin_fmaf(r2, 42.0586939f, -76.7058598f);
     s = __builtin_fmaf(r2, s, 81.6052493f);
