@@ -146,6 +146,8 @@ size_t attn_fwd_fp8_workspace_size(int64_t S, int64_t Tq, int64_t Tk, int64_t ma
  * as q, k, v's.  Rows that see no key have dq = +0; keys that no query sees
  * have dK = dV = +0.
  * o (FP16 codes) and lse are attn_fwd_fp8's results for the same arguments.
+ * p_j carries lse's rounding: it is off by up to 2^-22 max |s| of itself, so
+ * gradients want scores below some 2^15 (attn_fwd_fp8 takes any).
  * The two products with p_j and dS_j use them as IEEE half: p_j times 2^15 (dV
  * loses up to 2^-40 of each error e), dS_j times a power of two that the row
  * (for dq) or the key (for dK) finds for itself, whatever other rows, keys and

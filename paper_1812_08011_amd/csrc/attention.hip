@@ -1,4 +1,7 @@
 // Attention over packed sequences (attn_fwd_fp8, attn_bwd_fp8): host side.
+#include <float.h>
+#include <math.h>
+
 #include "attn_bwd.h"
 #include "attn_fwd.h"
 
@@ -74,7 +77,7 @@ extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     a.causal = causal;
     a.Tq = Tq;
     a.Tk = Tk;
-    a.c2 = sm_scale * kAttnLog2e;
+    a.c2 = fminf(sm_scale * kAttnLog2e, FLT_MAX);
     a.sm_scale = sm_scale;
     a.o = o;
     a.o_ts = o_ts;
@@ -143,7 +146,7 @@ extern "C" int attn_bwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     a.causal = causal;
     a.Tq = Tq;
     a.Tk = Tk;
-    a.c2 = sm_scale * kAttnLog2e;
+    a.c2 = fminf(sm_scale * kAttnLog2e, FLT_MAX);
     a.sm_scale = sm_scale;
     a.o = const_cast<uint16_t*>(o);
     a.o_ts = o_ts;

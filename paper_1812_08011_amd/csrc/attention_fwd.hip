@@ -21,6 +21,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kBase = 7.0f;         // p is held times 2^7 (relative to the row's reference)
 constexpr float kRoom = 15.0f;        // and may grow to 2^15 before the reference moves
+// Beyond this an exponent S c2 - reference, one FMA, is off by the rounding of
+// the reference, 2^-4 and more of a power of two, for all keys alike: halves
+// overflow, or underflow to 0.  A row's scores are then taken from a score.
+constexpr float kFar = 0x1p20f;
 
 struct Fmax { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 struct Add { __device__ float operator()(float a, float b) const { return a + b; } };
@@ -99,6 +103,8 @@ struct FwdRows {
     v8h qf[NC][2];
     v16f o[ND];
     float ref, mu, l, c2;              // reference; the same, 0 before the first key; sum; scale
+    float base;                        // the score that the others are taken from
+    bool far;                          // some row's is not 0
     uint32_t noted_any;                // keys with values that are not finite came by
 
     template <bool VEC>
@@ -115,7 +121,8 @@ struct FwdRows {
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
         ref = -INFINITY;
-        mu = l = 0.0f;
+        mu = l = base = 0.0f;
+        far = false;
         noted_any = 0;
     }
 
@@ -150,6 +157,7 @@ struct FwdRows {
                     if ((uint32_t)(key + 32 * kt + 8 * (r / 4) + r % 4) >= (uint32_t)lim)
                         st[kt][r] = -INFINITY;
         }
+        if (__builtin_expect(far, 0)) lower(st, base);
         float mx = -INFINITY;
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt)
@@ -157,6 +165,7 @@ struct FwdRows {
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kt][r]);
         mx = both_halves(mx, Fmax()) * c2;
         if (__any(mx - ref > kRoom)) {
+            if (__builtin_expect(__any(__builtin_fabsf(mx) > kFar && mx - kBase > ref), 0)) mx = take_base(st, mx);
             const float nref = fmaxf(ref, mx - kBase);
             const float f = nref == ref ? 1.0f : exp2f(ref - nref);
             ref = nref;
@@ -185,6 +194,32 @@ struct FwdRows {
         }
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt) noted_any |= noted[kt];
+    }
+
+    __device__ __forceinline__ void lower(v16f* st, float by) {
+        asm volatile("" : "+v"(by));                        // a branch, as above
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st[kt][r] -= by;
+    }
+    // Rows whose largest score is a far one, and moves their reference, take it
+    // for the score that the others are taken from: that of the tile's exponents
+    // is 0 then.
+    __device__ __forceinline__ float take_base(v16f* st, float mx) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, st[kt][r]);
+        top = both_halves(top, Fmax());
+        const bool moves = __builtin_fabsf(mx) > kFar && mx - kBase > ref && __builtin_fabsf(top) < INFINITY;
+        const float by = moves ? top : 0.0f;
+        far = true;
+        base += by;
+        if (moves) ref = __builtin_fmaf(-by, c2, ref);
+        lower(st, by);
+        return moves ? 0.0f : mx;
     }
 
     // The values that are not finite of the keys noted in `bits`, from key j0
@@ -251,16 +286,21 @@ struct FwdTile {
     }
 };
 
+__device__ __forceinline__ float row_lse(const AttnArgs& a, float base, float ref, float l) {
+    return __builtin_fmaf(base, a.sm_scale, kAttnLn2 * (ref + log2f(l)));
+}
+
 // xs: kRowsOut bytes of LDS of the wave's own.
 template <int DP, int N, int BM, bool SPLIT>
 __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& sp,
                                             const FwdTile<BM, BM == 128 ? 32 : 0>& t,
-                                            const FwdRows<DP, N>& x, float ref, float l, int lane, void* xs) {
+                                            const FwdRows<DP, N>& x, float base, float ref, float l, int lane,
+                                            void* xs) {
     const int h = lane >> 5;
     if constexpr (SPLIT) {
         const int64_t part = (int64_t)blockIdx.y * gridDim.x + (int64_t)t.slot * a.Hkv + t.hk;
         const int64_t pr = part * BM + (t.row - t.row0);
-        if (h == 0 && t.live) sp.ml[pr] = make_float2(ref, l);
+        if (h == 0 && t.live) sp.ml[pr] = make_float4(base, ref, l, 0.0f);
         if constexpr (BM == 32) {                           // few of the rows are there
             if (!t.live) return;
             float* po = sp.o + pr * DP + 4 * h;
@@ -278,7 +318,7 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
         }
     } else {
         if (a.lse && h == 0 && t.live)
-            a.lse[(int64_t)t.hq * a.Tq + t.tq] = t.lim > 0 ? kAttnLn2 * (ref + log2f(l)) : -INFINITY;
+            a.lse[(int64_t)t.hq * a.Tq + t.tq] = t.lim > 0 ? row_lse(a, base, ref, l) : -INFINITY;
         if (!a.o && !a.o8) return;
         // a row that sees nothing has sums of +0
         const float inv = t.lim > 0 ? 1.0f / l : 1.0f;
@@ -351,7 +391,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_image_kernel(AttnArgs a,
     }
     const float l = both_halves(x.l, Add());
     __syncthreads();                                        // the buffers are free
-    finish_rows<DP, N, 128, SPLIT>(a, sp, t, x, x.ref, l, lane, lds + wave * kRowsOut);
+    finish_rows<DP, N, 128, SPLIT>(a, sp, t, x, x.base, x.ref, l, lane, lds + wave * kRowsOut);
 }
 
 // KW = 1: 128 rows, 32 per wave, every wave walks all key tiles (shared in
@@ -460,7 +500,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
                    });
         }
     }
-    float l = both_halves(x.l, Add()), ref = x.ref;
+    float l = both_halves(x.l, Add()), base = x.base, ref = x.ref;
     // A value that is not finite in a tile that every row sees has made its
     // column's sums Inf, or NaN where its p underflowed (0 x Inf): they start
     // again from 0.
@@ -486,21 +526,28 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
 
     if constexpr (KW > 1) {
         // join the waves: references first, then the scaled sums
-        __shared__ float refs[KW][32], ls[KW][32];
+        __shared__ float bases[KW][32], refs[KW][32], ls[KW][32];
         __syncthreads();
         if (h == 0) {
+            bases[wave][l31] = base;
             refs[wave][l31] = ref;
             ls[wave][l31] = l;
         }
         __syncthreads();
-        float m = refs[0][l31];
+        float bm = bases[0][l31], m = refs[0][l31];
 #pragma unroll
-        for (int v = 1; v < KW; ++v) m = fmaxf(m, refs[v][l31]);
+        for (int v = 1; v < KW; ++v) {
+            const float bv = bases[v][l31], rv = refs[v][l31];
+            if (part_above(bv, rv, bm, m, a.c2) > 0.0f) {
+                bm = bv;
+                m = rv;
+            }
+        }
         l = 0.0f;
 #pragma unroll
         for (int v = 0; v < KW; ++v)
-            l += refs[v][l31] == m ? ls[v][l31] : ls[v][l31] * exp2f(refs[v][l31] - m);
-        const float f = part_weight(ref, m);
+            l += ls[v][l31] * part_weight(bases[v][l31], refs[v][l31], bm, m, a.c2);
+        const float f = part_weight(base, ref, bm, m, a.c2);
         float* xs = reinterpret_cast<float*>(vs);           // [wave - 1][register][lane]
         if (wave) {
 #pragma unroll
@@ -519,10 +566,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnS
                 for (int v = 0; v < KW - 1; ++v) y += xs[((v * ND + d) * 16 + r) * 64 + lane];
                 x.o[d][r] = y;
             }
+        base = bm;
         ref = m;
     }
     // KW = 1: the last step ended at a barrier; KW = 4: one wave is left
-    finish_rows<DP, kBN, BM, SPLIT>(a, sp, w, x, ref, l, lane, lds + (KW == 1 ? wave * kRowsOut : 0));
+    finish_rows<DP, kBN, BM, SPLIT>(a, sp, w, x, base, ref, l, lane, lds + (KW == 1 ? wave * kRowsOut : 0));
 }
 
 // Joins the partial results of a tile's key ranges, in their order: a wave per
@@ -544,13 +592,21 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSpl
     // without a key has neither; one whose scores are all NaN has a sum of NaN,
     // which has to come through.
     const int64_t stride = (int64_t)gridDim.x * BM, first = (int64_t)blockIdx.x * BM + rr;
-    const float2 ml = lane < sp.n ? sp.ml[lane * stride + first] : make_float2(-INFINITY, 0.0f);
-    const bool some = ml.x != -INFINITY || ml.y != 0.0f;
-    float m = ml.x;
+    const float4 ml = lane < sp.n ? sp.ml[lane * stride + first] : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+    const bool some = ml.y != -INFINITY || ml.z != 0.0f;
+    float bm = ml.x, m = ml.y;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    const float f = part_weight(ml.x, m);
-    float l = some ? ml.y * f : 0.0f;
+    for (int d = 32; d; d >>= 1) {
+        const float bv = __shfl_xor(bm, d), rv = __shfl_xor(m, d);
+        if (part_above(bv, rv, bm, m, a.c2) > 0.0f) {
+            bm = bv;
+            m = rv;
+        }
+    }
+    bm = __shfl(bm, 0);                                     // of equal ones the same for all
+    m = __shfl(m, 0);
+    const float f = part_weight(ml.x, ml.y, bm, m, a.c2);
+    float l = some ? ml.z * f : 0.0f;
 #pragma unroll
     for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
     float o[2] = {0.0f, 0.0f};
@@ -573,7 +629,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSpl
         if (a.o8) a.o8[t * a.o8_ts + hq * a.o8_hs + d] = (uint8_t)f32_to_fp8(x * a.o8_scale);
     }
     if (a.lse && lane == 0)
-        a.lse[(int64_t)hq * a.Tq + t] = lim > 0 ? kAttnLn2 * (m + log2f(l)) : -INFINITY;
+        a.lse[(int64_t)hq * a.Tq + t] = lim > 0 ? row_lse(a, bm, m, l) : -INFINITY;
 }
 
 template <int DP, bool VEC>
@@ -648,7 +704,7 @@ AttnFwdPlan attn_fwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
              (!p.image || image_tiles(Tk, attn_keys(p.DP)) * Hkv < kAttnGrid);
     p.image_bytes = (size_t)image + (p.order ? (p.slots * 4 + 15) / 16 * 16 : 0);
     p.bytes = p.image_bytes +
-              (p.splits > 1 ? (size_t)p.splits * p.slots * Hkv * p.BM * (p.DP * 4 + 8) : 0);
+              (p.splits > 1 ? (size_t)p.splits * p.slots * Hkv * p.BM * (p.DP * 4 + sizeof(float4)) : 0);
     return p;
 }
 
@@ -661,7 +717,7 @@ void attn_fwd_launch(AttnArgs a, const AttnFwdPlan& p, bool vec, void* workspace
     if (p.splits > 1) {
         const int64_t rows = (int64_t)p.splits * p.slots * a.Hkv * p.BM;
         sp.o = reinterpret_cast<float*>(a.key_image + p.image_bytes);
-        sp.ml = reinterpret_cast<float2*>(sp.o + rows * p.DP);
+        sp.ml = reinterpret_cast<float4*>(sp.o + rows * p.DP);
         sp.n = p.splits;
         sp.per = p.per;
     }

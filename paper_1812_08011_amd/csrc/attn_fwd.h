@@ -13,9 +13,9 @@ struct AttnFwdPlan {
     size_t image_bytes, bytes;         // workspace: images and order first, then partial results
 };
 
-struct AttnSplit {                     // partial results: rows x DP sums, (reference, sum)
+struct AttnSplit {                     // partial results: rows x DP sums, (base, reference, sum)
     float* o;
-    float2* ml;
+    float4* ml;
     int n, per;
 };
 

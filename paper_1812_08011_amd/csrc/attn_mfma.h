@@ -171,11 +171,18 @@ __device__ __forceinline__ float fp8_nonfinite(uint32_t c) {
     return __uint_as_float(((c & 0x80u) << 24) | kF32Inf | ((c & 3u) << 21));
 }
 
-// The weight, against the largest reference m, of sums held relative to `ref`.
-// It does not underflow to 0: an infinity that a seen value has left in the
-// sums stays one, and finite sums times 2^-126 are lost in any other rounding.
-__device__ __forceinline__ float part_weight(float ref, float m) {
-    return ref == m ? 1.0f : fmaxf(exp2f(ref - m), 0x1p-126f);
+// How far, in powers of two, sums of one part of the keys are held above those
+// of another: a part's exponents are taken from the score `base` and then from
+// the reference `ref` (base 2; -Inf before its first key).
+__device__ __forceinline__ float part_above(float base, float ref, float base0, float ref0, float c2) {
+    return __builtin_fmaf(base - base0, c2, ref - ref0);
+}
+// A part's weight against the part that is held highest.  It does not underflow
+// to 0: an infinity that a seen value has left in the sums stays one, and finite
+// sums times 2^-126 are lost in any other rounding.
+__device__ __forceinline__ float part_weight(float base, float ref, float base0, float ref0, float c2) {
+    return base == base0 && ref == ref0 ? 1.0f
+                                        : fmaxf(exp2f(part_above(base, ref, base0, ref0, c2)), 0x1p-126f);
 }
 
 // Entries that are not finite, of the rows noted in `bits` (row 0 of them is
