@@ -162,7 +162,7 @@ inline bool rows_apart(int64_t T, int64_t H, int64_t D, int64_t ts, int64_t hs) 
     if (T > 1 && ts < D) return false;
     if (H > 1 && hs < D) return false;
     if (T <= 1 || H <= 1) return true;
-    return ts / H >= hs || ts - D >= (H - 1) * hs || hs / T >= ts || hs - D >= (T - 1) * ts;
+    return (ts - D) / (H - 1) >= hs || (hs - D) / (T - 1) >= ts;   // no product: it may pass 64 bits
 }
 
 }  // namespace fp8t
