@@ -13,13 +13,16 @@
 // its key finds for itself (kDsFirst).  Sums are FP32.
 //
 // The three products of dq and the four of dk and dv bound them: with 8192
-// causal tokens, 16 heads of 128 and 4 key heads 412 GFLOP in 397 us (1038
-// TFLOP/s) and 550 GFLOP in 640 us (859 TFLOP/s), of 1138 that a large product
-// reaches.  D 64, mixed lengths: 69 GFLOP in 92 us and 92 GFLOP in 140 us, the
-// exponentials' share twice as large.  Both keep 2 waves per SIMD: the sums
-// take 64 registers of a lane in dq and 128 in dk and dv (64 keys a wave
-// spilled: 26 ms for the pass over those 8192 tokens), and read their tiles from
-// images, since transposing them in the loop spilled too (9 ms).
+// causal tokens, 16 heads of 128 and 4 key heads 412 GFLOP in 406 us (1015
+// TFLOP/s) and 550 GFLOP in 680 us (809 TFLOP/s), of 1138 that a large product
+// reaches.  D 64, mixed lengths: 69 GFLOP in 98 us and 92 GFLOP in 149 us; the
+// vector ALUs are busy for 58% and 44% of it, the matrix cores for 32% and 28%
+// (D 128: 53% and 35%, 48% and 36%).  With D above 64 both keep 2 waves per SIMD
+// (244 and 252 registers): the sums take 64 registers of a lane in dq and 128 in
+// dk and dv (64 keys a wave spilled: 26 ms for the pass over those 8192 tokens),
+// and read their tiles from images, since transposing them in the loop spilled
+// too (9 ms).  D up to 64 takes 160 and 165 registers, 3 waves.  Looking for the
+// largest dS takes 10 instructions per 32 x 32 scores, 4 to 5% of these times.
 #include "attn_bwd.h"
 #include "attn_image.h"
 
@@ -451,8 +454,10 @@ AttnBwdPlan attn_bwd_plan(int64_t S, int64_t Tq, int64_t Tk, int64_t max_q, int6
     p.parts = p.key_order + (S > 1 ? up(slots(S, Tk, 1, kAttnDkvKeys) * 4) : 0);
     // The steps of a key tile are shared out where the tiles leave CUs idle,
     // until there are 4 workgroups per CU, with 16 steps of 32 queries each at
-    // least.  8192 causal tokens, 4 key heads: 640 us and 25 for the join; with
-    // 2 per CU 835 and 15 (the causal tiles differ in length), with 8 560 and 51.
+    // least.  8192 causal tokens, 16 heads of 128, 4 key heads, forward and
+    // gradients: 1416 us with 4; with 2 1614 (the causal tiles differ in length);
+    // with 8 1375, for twice the partial results: 268 MB of workspace more than
+    // none in place of 134.
     const int64_t tiles = slots(S, Tk, 1, kAttnDkvKeys);
     const int64_t some = S * ((max_k + kAttnDkvKeys - 1) / kAttnDkvKeys), groups = (tiles < some ? tiles : some) * Hkv;
     const int64_t steps = (max_q + 31) / 32 * G, want = 4 * (int64_t)device_cus();

@@ -11,7 +11,9 @@
 // the FP8 matrix instructions, twice as fast, cut products to 13 bits, which
 // moved the log-sum-exps by 3e-5.  p is rounded to a half of its own row's
 // scale (2^-12 relative at the largest, absolutely 2^-30 of it): what leaves is
-// rounded to 10 bits or 3.  Sums, reference and statistics stay FP32.
+// rounded to 10 bits or 3.  Sums, reference and statistics stay FP32.  Where a
+// row's scores are so large that FP32 exponents lose their fraction, they are
+// taken from one of them first (kFar).
 #include "attn_fwd.h"
 #include "attn_image.h"
 
@@ -343,12 +345,13 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
 // LDS, one tile ahead.
 //
 // Bound by the matrix cores: 550 GFLOP (16384 causal tokens, 8 heads of 128, 2
-// key heads) in 558 us, 985 TFLOP/s, where a large half-precision product
+// key heads) in 565 us, 973 TFLOP/s, where a large half-precision product
 // reaches 1138; without the softmax's instructions between them the same matrix
-// instructions took 470 us.  275 GFLOP over 8192 tokens: 286 us.  D 64: 46
-// GFLOP of mixed lengths in 73 us, bound by the exponentials (one for 256
-// operations).  A row tile of 128 keeps 2 waves per SIMD (200 registers a lane);
-// a third wave spills.  A third buffer in LDS changed nothing.
+// instructions took 470 us.  275 GFLOP over 8192 tokens: 284 us.  D 64: 46
+// GFLOP of mixed lengths in 75 us, the vector ALUs busy for 61% of it and the
+// matrix cores for 28% (D 128: 55% and 48%).  With D above 64 a row tile of 128
+// keeps 2 waves per SIMD (190 registers a lane), a third spills; with D up to 64
+// it is 3 (166).  A third buffer in LDS changed nothing.
 template <int DP, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_image_kernel(AttnArgs a, AttnSplit sp) {
     using I = FwdImage<DP>;
@@ -406,7 +409,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_image_kernel(AttnArgs a,
 // the join; a copy of that size would take 9 us) and by the latency of a
 // workgroup's start, first loads and join: 11 us where there is one key.  Many
 // short sequences (24 of up to 96 tokens, 16 heads of 64) take 10 us, nearly
-// all of it that latency.
+// all of it that latency.  KW = 4 with D above 64 takes all 256 registers and 72
+// to 92 bytes of scratch a lane: the next tile's keys and values are in flight
+// beside the queries and 64 sums.
 template <int DP, int KW, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnArgs a, AttnSplit sp) {
     constexpr int NT = kThreads / KW, BM = 128 / KW, kBN = KW == 1 ? attn_keys(DP) : attn_keys(DP) / 2;

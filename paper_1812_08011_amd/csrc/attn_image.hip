@@ -2,9 +2,9 @@
 // LDS and writes it out 16 bytes a thread.
 //
 // Bound by what they read and write.  8192 tokens of 128: keys of 4 heads for
-// the forward pass 7 us (8 MB in, 13 out), keys for the backward pass 14 us (8
-// in, 18 out), queries and errors of 16 heads 40 us (67 MB with
-// o in, 105 out: 4.3 TB/s).
+// the forward pass 7 us (8 MB in, 13 out), keys for the backward pass 11 us (8
+// in, 18 out), queries and errors of 16 heads 35 us (67 MB with o in, 105 out:
+// 4.9 TB/s).
 #include "attn_image.h"
 
 namespace fp8t {
