@@ -77,7 +77,9 @@ extern "C" int attn_fwd_fp8(const uint8_t* q, int64_t q_ts, int64_t q_hs, const 
     a.causal = causal;
     a.Tq = Tq;
     a.Tk = Tk;
-    a.c2 = fminf(sm_scale * kAttnLog2e, FLT_MAX);
+    // scores, multiples of 2^-32 below 2^39: with any larger factor too one key
+    // takes a row, and 2^86 times a distance stays finite
+    a.c2 = fminf(sm_scale * kAttnLog2e, 0x1p86f);
     a.sm_scale = sm_scale;
     a.o = o;
     a.o_ts = o_ts;

@@ -159,15 +159,24 @@ struct FwdRows {
                     if ((uint32_t)(key + 32 * kt + 8 * (r / 4) + r % 4) >= (uint32_t)lim)
                         st[kt][r] = -INFINITY;
         }
-        if (__builtin_expect(far, 0)) lower(st, base);
-        float mx = -INFINITY;
+        float top = -INFINITY;
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kt][r]);
-        mx = both_halves(mx, Fmax()) * c2;
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, st[kt][r]);
+        top = both_halves(top, Fmax());
+        float mx = (top - base) * c2;
         if (__any(mx - ref > kRoom)) {
-            if (__builtin_expect(__any(__builtin_fabsf(mx) > kFar && mx - kBase > ref), 0)) mx = take_base(st, mx);
+            // rows whose reference moves to a far score are taken from that
+            const bool moves = __builtin_fabsf(mx) > kFar && mx - kBase > ref && mx < INFINITY;
+            if (__builtin_expect(__any(moves), 0)) {
+                if (moves) {
+                    ref = __builtin_fmaf(base - top, c2, ref);
+                    base = top;
+                    mx = 0.0f;
+                }
+                far = true;
+            }
             const float nref = fmaxf(ref, mx - kBase);
             const float f = nref == ref ? 1.0f : exp2f(ref - nref);
             ref = nref;
@@ -177,6 +186,14 @@ struct FwdRows {
             for (int d = 0; d < ND; ++d)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= f;
+        }
+        if (__builtin_expect(far, 0)) {
+            float by = base;
+            asm volatile("" : "+v"(by));                    // a branch, as above
+#pragma unroll
+            for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[kt][r] -= by;
         }
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt) {
@@ -196,32 +213,6 @@ struct FwdRows {
         }
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt) noted_any |= noted[kt];
-    }
-
-    __device__ __forceinline__ void lower(v16f* st, float by) {
-        asm volatile("" : "+v"(by));                        // a branch, as above
-#pragma unroll
-        for (int kt = 0; kt < NK; ++kt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) st[kt][r] -= by;
-    }
-    // Rows whose largest score is a far one, and moves their reference, take it
-    // for the score that the others are taken from: that of the tile's exponents
-    // is 0 then.
-    __device__ __forceinline__ float take_base(v16f* st, float mx) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int kt = 0; kt < NK; ++kt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, st[kt][r]);
-        top = both_halves(top, Fmax());
-        const bool moves = __builtin_fabsf(mx) > kFar && mx - kBase > ref && __builtin_fabsf(top) < INFINITY;
-        const float by = moves ? top : 0.0f;
-        far = true;
-        base += by;
-        if (moves) ref = __builtin_fmaf(-by, c2, ref);
-        lower(st, by);
-        return moves ? 0.0f : mx;
     }
 
     // The values that are not finite of the keys noted in `bits`, from key j0
