@@ -36,34 +36,33 @@ constexpr int kThreads = 256;
 // depend on any other.  It starts so large that any dS that reaches a result
 // has all 11 bits of a half, and goes down when one of the sum passes kDsRoom
 // (the largest half is 65504), the sums so far with it: the first steps of a
-// wave do that, later ones seldom.  The largest then lies in [2^11, 2^12) --
-// nearer to the largest half the sums went down more often, 2% of the time -- so
-// that a dS down to 2^-25 of it keeps all 11 bits, with steps of 2^-35 below.
+// wave do that, later ones seldom.  The largest then lies in [2^11, 2^12) (one
+// power of two higher the sums go down more often, 1 to 2% of the time), so that
+// a dS down to 2^-25 of it keeps all 11 bits, with steps of 2^-35 below.
 constexpr float kDsFirst = 0x1p64f;    // |<e, v>| and |delta| stay below 2^56: no overflow
 constexpr float kDsRoom = 61440.0f;
-__device__ __forceinline__ bool ds_passes(const float* ds) {
-    // two chains; a NaN passes nothing: its row's or its key's result is NaN
-    float a = 0.0f, b = 0.0f;
+// A lane's largest, NaN if one is: its row's or its key's result is NaN then.
+__device__ __forceinline__ float ds_top(const float* ds) {
+    float a = 0.0f, b = 0.0f;                               // two chains
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
         a = maximum3_abs(a, ds[r], ds[r + 1]);
         b = maximum3_abs(b, ds[r + 2], ds[r + 3]);
     }
-    return __any(maximum3_abs(kDsRoom, a, b) > kDsRoom);
+    return maximum3_abs(0.0f, a, b);
 }
 // The factor that brings the largest finite one down; ds times it.
-__device__ __forceinline__ float ds_down(float* ds) {
-    float top = 0.0f;
+__device__ __forceinline__ float ds_down(float* ds, float top) {
+    if (__builtin_expect(__any(!(top < INFINITY)), 0)) {
+        top = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const float x = __builtin_fabsf(ds[r]);
-        top = fmaxf(top, x < INFINITY ? x : 0.0f);
+        for (int r = 0; r < 16; ++r) {
+            const float x = __builtin_fabsf(ds[r]);
+            top = fmaxf(top, x < INFINITY ? x : 0.0f);
+        }
     }
     top = both_halves(top, [](float a, float b) { return fmaxf(a, b); });
-    if (!(top > kDsRoom)) return 1.0f;
-    int e;
-    (void)__builtin_frexpf(top, &e);                        // top < 2^e
-    const float f = __builtin_ldexpf(1.0f, 12 - e);
+    const float f = top > kDsRoom ? __builtin_ldexpf(1.0f, 12 - __builtin_amdgcn_frexp_expf(top)) : 1.0f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) ds[r] *= f;
     return f;
@@ -169,8 +168,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(AttnArgs a) {
                 for (int r = 0; r < 16; ++r)
                     if ((uint32_t)(key + 8 * (r / 4) + r % 4) >= (uint32_t)lim) ds[r] = 0.0f;
             }
-            if (__builtin_expect(ds_passes(ds), 0)) {
-                const float f = ds_down(ds);
+            const float top = ds_top(ds);
+            if (__builtin_expect(__any(top > kDsRoom), 0)) {
+                const float f = ds_down(ds, top);
                 sigma *= f;
                 delta *= f;
 #pragma unroll
@@ -320,8 +320,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dkv_kernel(AttnArgs a) {
             for (int r = 0; r < 16; ++r)
                 if ((uint32_t)(i + 8 * (r / 4) + r % 4) >= seen_by) p[r] = ds[r] = 0.0f;
         }
-        if (__builtin_expect(ds_passes(ds), 0)) {
-            const float f = ds_down(ds);
+        const float top = ds_top(ds);
+        if (__builtin_expect(__any(top > kDsRoom), 0)) {
+            const float f = ds_down(ds, top);
             sg *= f;
 #pragma unroll
             for (int d = 0; d < ND; ++d)
