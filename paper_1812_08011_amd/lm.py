@@ -52,8 +52,10 @@ def rotary_freqs(R, base=10000.0, scaling=None, factor=1.0, original_length=4096
         raise ValueError("rotary_freqs: R must be even and positive")
     if scaling not in (None, "linear", "base", "by_parts"):
         raise ValueError(f"rotary_freqs: unknown scaling {scaling!r}")
-    if scaling is not None and factor < 1.0:
-        raise ValueError("rotary_freqs: factor must be at least 1")
+    if scaling is not None and not 1.0 <= factor < math.inf:
+        raise ValueError("rotary_freqs: factor must be at least 1 and finite")
+    if scaling == "by_parts" and not slow_turns < fast_turns:
+        raise ValueError("rotary_freqs: slow_turns must be below fast_turns")
     if scaling == "base" and R > 2:
         base = base * factor ** (R / (R - 2.0))
     freqs = base ** (-np.arange(0, R, 2, dtype=np.float64) / R)
