@@ -287,6 +287,9 @@ __device__ __forceinline__ float row_lse(const AttnArgs& a, float base, float re
     return __builtin_fmaf(base, a.sm_scale, kAttnLn2 * ((ref + kBase) + log2f(__builtin_ldexpf(l, -(int)kBase))));
 }
 
+// A row whose scores are all -Inf is 0 / 0 throughout, its infinite values too.
+__device__ __forceinline__ float row_inverse(float l) { return l == 0.0f ? NAN : 1.0f / l; }
+
 // xs: kRowsOut bytes of LDS of the wave's own.
 template <int DP, int N, int BM, bool SPLIT>
 __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& sp,
@@ -318,7 +321,7 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
             a.lse[(int64_t)t.hq * a.Tq + t.tq] = t.lim > 0 ? row_lse(a, base, ref, l) : -INFINITY;
         if (!a.o && !a.o8) return;
         // a row that sees nothing has sums of +0
-        const float inv = t.lim > 0 ? 1.0f / l : 1.0f;
+        const float inv = t.lim > 0 ? row_inverse(l) : 1.0f;
         const int64_t o = t.tq * a.o_ts + (int64_t)t.hq * a.o_hs;
         const int64_t o8 = t.tq * a.o8_ts + (int64_t)t.hq * a.o8_hs;
         rows_out<DP>(static_cast<float*>(xs), x.o, inv, lane, [&](int r, int col, const float* v) {
@@ -619,7 +622,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, AttnSpl
     }
     const int64_t t = sq.q0 + i;
     const int hq = hk * a.G + row - i * a.G;
-    const float inv = 1.0f / l;
+    const float inv = row_inverse(l);
 #pragma unroll
     for (int u = 0; u < DP / 64; ++u) {
         const int d = 64 * u + lane;
