@@ -10,8 +10,9 @@
  *
  * Results are functions of the arguments alone on a given device (no atomics
  * whose order could change them); attention's size hints and workspace choose
- * the order of its sums, so a call with others may differ in the last bits.  Sums, softmax statistics and log-sum-exps
- * are FP32; every result is rounded once, from FP32, to its storage format.
+ * the order of its sums, so a call with others may differ in the last bits.
+ * Sums, softmax statistics and log-sum-exps are FP32; every result is rounded
+ * once, from FP32, to its storage format.
  */
 #ifndef FP8TRAIN_LM_H
 #define FP8TRAIN_LM_H
@@ -189,7 +190,8 @@ size_t attn_bwd_fp8_workspace_size(int64_t S, int64_t Tq, int64_t Tk, int64_t ma
  * or floats).  w: per-row weights (1 / rows of a batch mean; 0 for padding),
  * NULL for 1.  A row with w = 0, without a used entry, or with no used
  * teacher logit above -Inf has loss +0 and g +0, whatever z holds.  An
- * entry that occurs twice counts twice.  Terms with q_i = 0 add 0.
+ * entry that occurs twice counts twice.  Terms with q_i = 0 add 0.  Powers are
+ * taken of a logit's distance from the row's largest; below 2^-126 they are 0.
  *
  * z: N x V in z_format (F32 or FP16), row stride z_ld >= V; idx (int64) and
  * t (t_format F32 or FP16): N x k contiguous, 0 <= k <= 4096; w, loss: N

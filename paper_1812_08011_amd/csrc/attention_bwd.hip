@@ -13,15 +13,15 @@
 // its key finds for itself (kDsFirst).  Sums are FP32.
 //
 // The three products of dq and the four of dk and dv bound them: with 8192
-// causal tokens, 16 heads of 128 and 4 key heads 412 GFLOP in 406 us (1015
-// TFLOP/s) and 550 GFLOP in 680 us (809 TFLOP/s), of 1138 that a large product
-// reaches.  D 64, mixed lengths: 69 GFLOP in 98 us and 92 GFLOP in 149 us; the
+// causal tokens, 16 heads of 128 and 4 key heads 412 GFLOP in 398 us (1035
+// TFLOP/s) and 550 GFLOP in 673 us (817 TFLOP/s), of 1138 that a large product
+// reaches.  D 64, mixed lengths: 69 GFLOP in 98 us and 92 GFLOP in 148 us; the
 // vector ALUs are busy for 58% and 44% of it, the matrix cores for 32% and 28%
-// (D 128: 53% and 35%, 48% and 36%).  With D above 64 both keep 2 waves per SIMD
-// (244 and 252 registers): the sums take 64 registers of a lane in dq and 128 in
+// (D 128: 52% and 35%, 48% and 36%).  With D above 64 both keep 2 waves per SIMD
+// (246 and 254 registers): the sums take 64 registers of a lane in dq and 128 in
 // dk and dv (64 keys a wave spilled: 26 ms for the pass over those 8192 tokens),
 // and read their tiles from images, since transposing them in the loop spilled
-// too (9 ms).  D up to 64 takes 160 and 165 registers, 3 waves.  Looking for the
+// too (9 ms).  D up to 64 takes 162 and 168 registers, 3 waves.  Looking for the
 // largest dS takes 10 instructions per 32 x 32 scores, 4 to 5% of these times.
 #include "attn_bwd.h"
 #include "attn_image.h"

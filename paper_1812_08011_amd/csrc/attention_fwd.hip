@@ -343,10 +343,10 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnSplit& 
 // LDS, one tile ahead.
 //
 // Bound by the matrix cores: 550 GFLOP (16384 causal tokens, 8 heads of 128, 2
-// key heads) in 565 us, 973 TFLOP/s, where a large half-precision product
+// key heads) in 551 us, 998 TFLOP/s, where a large half-precision product
 // reaches 1138; without the softmax's instructions between them the same matrix
-// instructions took 470 us.  275 GFLOP over 8192 tokens: 284 us.  D 64: 46
-// GFLOP of mixed lengths in 75 us, the vector ALUs busy for 61% of it and the
+// instructions took 470 us.  275 GFLOP over 8192 tokens: 282 us.  D 64: 46
+// GFLOP of mixed lengths in 77 us, the vector ALUs busy for 60% of it and the
 // matrix cores for 28% (D 128: 55% and 48%).  With D above 64 a row tile of 128
 // keeps 2 waves per SIMD (190 registers a lane), a third spills; with D up to 64
 // it is 3 (166).  A third buffer in LDS changed nothing.
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_image_kernel(AttnArgs a,
 // the join; a copy of that size would take 9 us) and by the latency of a
 // workgroup's start, first loads and join: 11 us where there is one key.  Many
 // short sequences (24 of up to 96 tokens, 16 heads of 64) take 10 us, nearly
-// all of it that latency.  KW = 4 with D above 64 takes all 256 registers and 72
+// all of it that latency.  KW = 4 with D above 64 takes all 256 registers and 64
 // to 92 bytes of scratch a lane: the next tile's keys and values are in flight
 // beside the queries and 64 sums.
 template <int DP, int KW, bool VEC, bool SPLIT>
