@@ -1,4 +1,4 @@
-"""Python binding of libfp8train (include/fp8train.h, include/fp8train_lm.h).
+"""Python binding of libfp8train (include/fp8train.h, fp8train_lm.h, fp8train_tokens.h).
 
 Argument marshalling only: every step runs in the HIP library.  Arrays are
 torch tensors on the GPU (uint8 for FP8 codes, uint16 for FP16 codes, float32
@@ -17,6 +17,7 @@ SRC_F32, SRC_FP16 = 0, 1
 EXACT, FAST = 0, 1
 FMT_F32, FMT_FP16, FMT_FP8, FMT_HALF = 0, 1, 2, 3
 ATTN_MAX_D = 128
+MAX_TOP, EMBED_MAX_V = 128, 1 << 24
 
 _lib = None
 
@@ -104,6 +105,28 @@ def lib():
         L.distill_loss.restype = i32
         L.distill_loss.argtypes = [vp, i32, i64, vp, vp, i32, i64, vp, i64, i64, f32, f32, vp, vp,
                                    i32, i64, vp]
+        L.embed_fwd.restype = i32
+        L.embed_fwd.argtypes = [vp, i64, vp, i32, i64, i64, i64, f32, vp, i32, i64, vp]
+        L.embed_bwd.restype = i32
+        L.embed_bwd.argtypes = [vp, i64, vp, i32, i64, i64, i64, f32, vp, i32, i64, vp, sz, vp]
+        L.embed_bwd_workspace_size.restype = sz
+        L.embed_bwd_workspace_size.argtypes = [i64, i64, i64]
+        L.rms_norm_fwd.restype = i32
+        L.rms_norm_fwd.argtypes = [vp, i32, i64, vp, vp, i64, vp, i32, i64, i64, f32, vp, i32, i64,
+                                   vp, i32, i64, f32, vp, vp, vp]
+        L.rms_norm_bwd.restype = i32
+        L.rms_norm_bwd.argtypes = [vp, i32, i64, vp, i32, vp, vp, i32, i64, vp, i64, i64, i64, vp,
+                                   i32, i64, vp, i64, f32, vp, i32, vp, sz, vp]
+        L.rms_norm_bwd_workspace_size.restype = sz
+        L.rms_norm_bwd_workspace_size.argtypes = [i64, i64]
+        L.token_logprobs.restype = i32
+        L.token_logprobs.argtypes = [vp, i32, i64, vp, i64, i64, i64, f32, vp, vp, vp, i64, vp, vp,
+                                     vp, sz, vp]
+        L.token_logprobs_workspace_size.restype = sz
+        L.token_logprobs_workspace_size.argtypes = [i64, i64, i64]
+        L.token_logprobs_bwd.restype = i32
+        L.token_logprobs_bwd.argtypes = [vp, i32, i64, vp, i64, vp, vp, vp, vp, i64, i64, f32, f32,
+                                         vp, i32, i64, vp]
         L.fp8t_status_string.restype = ctypes.c_char_p
         L.fp8t_status_string.argtypes = [i32]
         _lib = L
@@ -462,4 +485,185 @@ def distill_loss(z, idx, t, w, tau, grad_scale, loss, g, stream=None):
         float(grad_scale), None if loss is None else _dense(fn, loss, (N,), torch.float32),
         *((None, FMT_F32, 0) if g is None else matrix(g, (FMT_F32, FMT_FP16, FMT_FP8))),
         _stream(stream)))
+    return g
+
+
+# ---- operators on tokens and rows (include/fp8train_tokens.h) ------------------------
+#
+# Matrices may be any views whose rows are contiguous.  Tensors have to be on the
+# current device: an address that the GPU cannot reach would end the process.
+
+_ANY, _FLOATS = (FMT_F32, FMT_FP16, FMT_FP8), (FMT_F32, FMT_FP16)
+
+
+def _here(fn, *tensors):
+    """All on one GPU, the current one."""
+    import torch
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+            raise ValueError(f"{fn}: a tensor on {t.device} is not on the current GPU")
+
+
+def _matrix(fn, t, rows, cols, allowed):
+    """(address, format, row stride) of a rows x cols tensor."""
+    fmt = _format(fn, t, allowed)
+    if t.shape != (rows, cols):
+        raise ValueError(f"{fn}: shape {tuple(t.shape)} where {(rows, cols)} is needed")
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1 and rows > 0:
+        raise ValueError(f"{fn}: rows must be contiguous")
+    return t.data_ptr(), fmt, ld if rows > 1 else max(ld, cols)
+
+
+def _vector(fn, t, n, allowed):
+    """(address, format) of n contiguous elements; (None, FMT_F32) of None."""
+    if t is None:
+        return None, FMT_F32
+    fmt = _format(fn, t, allowed)
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{fn}: {n} contiguous elements are needed")
+    return t.data_ptr(), fmt
+
+
+def _floats(fn, t, *shape):
+    import torch
+    return None if t is None else _dense(fn, t, shape, torch.float32)
+
+
+def _i64(fn, t, *shape):
+    import torch
+    return None if t is None else _dense(fn, t, shape, torch.int64)
+
+
+def _space(fn, workspace, workspace_bytes):
+    if workspace is not None and not isinstance(workspace, int):
+        if workspace_bytes > workspace.numel() * workspace.element_size():
+            raise ValueError(f"{fn}: the workspace holds fewer than {workspace_bytes} bytes")
+        _here(fn, workspace)
+    return _ptr(workspace), int(workspace_bytes)
+
+
+def embed_fwd(tokens, table, y, scale=1.0, stream=None):
+    """y (T x W) = rows of the table (V x W) by tokens (T int64), times scale;
+    each float32, FP16 or FP8 codes.  Tokens outside [0, V) give rows of 0."""
+    fn = "embed_fwd"
+    T, (V, W) = tokens.numel(), table.shape
+    tp, tf, t_ld = _matrix(fn, table, V, W, _ANY)
+    yp, yf, y_ld = _matrix(fn, y, T, W, _ANY)
+    at = _i64(fn, tokens, T)
+    _here(fn, tokens, table, y)
+    _check(fn, lib().embed_fwd(at, T, tp, tf, t_ld, V, W, float(scale), yp, yf, y_ld,
+                               _stream(stream)))
+    return y
+
+
+def embed_bwd_workspace_size(tokens, e, g):
+    return int(lib().embed_bwd_workspace_size(tokens.numel(), *g.shape))
+
+
+def embed_bwd(tokens, e, g, scale=1.0, workspace=None, workspace_bytes=0, stream=None):
+    """g (V x W): the sum of scale * e[t] over the t with tokens[t] = v, for
+    every v; e: T x W."""
+    fn = "embed_bwd"
+    T, (V, W) = tokens.numel(), g.shape
+    ep, ef, e_ld = _matrix(fn, e, T, W, _ANY)
+    gp, gf, g_ld = _matrix(fn, g, V, W, _ANY)
+    at = _i64(fn, tokens, T)
+    ws = _space(fn, workspace, workspace_bytes)
+    _here(fn, tokens, e, g)
+    _check(fn, lib().embed_bwd(at, T, ep, ef, e_ld, V, W, float(scale), gp, gf, g_ld, *ws,
+                               _stream(stream)))
+    return g
+
+
+def rms_norm_fwd(x, r, w, eps, h, y, y_scale=1.0, y_row_scale=None, rstd=None, x_row_scale=None,
+                 stream=None):
+    """h = x + r (T x W, float32 or FP16 codes; r and h of one type) and y =
+    h / rms(h) w times y_scale, or times a scale of each row's own that brings
+    its largest result to y_scale and is written to y_row_scale.  r, w, h, y and
+    the float32 vectors may be None; h may be r or x itself."""
+    fn = "rms_norm_fwd"
+    T, W = x.shape
+    xp, xf, x_ld = _matrix(fn, x, T, W, _FLOATS)
+    rp, rf, r_ld = (None, None, 0) if r is None else _matrix(fn, r, T, W, _FLOATS)
+    hp, hf, h_ld = (None, None, 0) if h is None else _matrix(fn, h, T, W, _FLOATS)
+    if r is not None and h is not None and rf != hf:
+        raise TypeError(f"{fn}: r and h have different types")
+    yp, yf, y_ld = (None, FMT_FP8, 0) if y is None else _matrix(fn, y, T, W, _ANY)
+    wp, wf = _vector(fn, w, W, _FLOATS)
+    xs, ys, rs = _floats(fn, x_row_scale, T), _floats(fn, y_row_scale, T), _floats(fn, rstd, T)
+    _here(fn, x, r, w, h, y, x_row_scale, y_row_scale, rstd)
+    _check(fn, lib().rms_norm_fwd(xp, xf, x_ld, xs, rp, r_ld, wp, wf, T, W, float(eps), hp,
+                                  FMT_F32 if rf is hf is None else hf if rf is None else rf, h_ld,
+                                  yp, yf, y_ld, float(y_scale), ys, rs, _stream(stream)))
+    return h if y is None else y
+
+
+def rms_norm_bwd_workspace_size(h):
+    return int(lib().rms_norm_bwd_workspace_size(*h.shape))
+
+
+def rms_norm_bwd(h, w, rstd, dy, dr, dx, dx8=None, dx8_scale=1.0, dw=None, workspace=None,
+                 workspace_bytes=0, stream=None):
+    """Gradients of rms_norm_fwd from its h and rstd and the error dy of the
+    normed rows: dx (of h, with dr, the error that reaches h past the norm, of
+    the same type; may be dr), dx8 (the same in FP8 times dx8_scale) and dw."""
+    fn = "rms_norm_bwd"
+    T, W = h.shape
+    hp, hf, h_ld = _matrix(fn, h, T, W, _FLOATS)
+    yp, yf, y_ld = _matrix(fn, dy, T, W, _ANY)
+    rp, rf, r_ld = (None, None, 0) if dr is None else _matrix(fn, dr, T, W, _FLOATS)
+    xp, xf, x_ld = (None, None, 0) if dx is None else _matrix(fn, dx, T, W, _FLOATS)
+    if dr is not None and dx is not None and rf != xf:
+        raise TypeError(f"{fn}: dr and dx have different types")
+    x8p, _, x8_ld = (None, None, 0) if dx8 is None else _matrix(fn, dx8, T, W, (FMT_FP8,))
+    wp, wf = _vector(fn, w, W, _FLOATS)
+    dwp, dwf = _vector(fn, dw, W, _FLOATS)
+    rs = _floats(fn, rstd, T)
+    ws = _space(fn, workspace, workspace_bytes)
+    _here(fn, h, w, rstd, dy, dr, dx, dx8, dw)
+    _check(fn, lib().rms_norm_bwd(hp, hf, h_ld, wp, wf, rs, yp, yf, y_ld, rp, r_ld, T, W, xp,
+                                  FMT_F32 if rf is xf is None else xf if rf is None else rf, x_ld,
+                                  x8p, x8_ld, float(dx8_scale), dwp, dwf, *ws, _stream(stream)))
+    return dx
+
+
+def token_logprobs_workspace_size(z, k):
+    return int(lib().token_logprobs_workspace_size(*z.shape, int(k)))
+
+
+def token_logprobs(z, idx, tau=1.0, logp=None, entropy=None, stats=None, top_idx=None,
+                   top_logp=None, workspace=None, workspace_bytes=0, stream=None):
+    """Log probabilities logp (N x m) of the tokens idx (N x m int64) under
+    softmax(z / tau), z: N x V float32 or FP16 codes; entropy (N), stats (N x 2:
+    what token_logprobs_bwd takes) and the likeliest tokens top_idx (N x k
+    int64) with their top_logp (N x k).  Results that are None are not formed."""
+    fn = "token_logprobs"
+    N, V = z.shape
+    zp, zf, z_ld = _matrix(fn, z, N, V, _FLOATS)
+    m = 0 if idx is None else idx.shape[1]
+    k = 0 if top_idx is None and top_logp is None else (top_logp if top_idx is None else top_idx).shape[1]
+    args = (_i64(fn, idx, N, m), m, N, V, float(tau), _floats(fn, logp, N, m),
+            _floats(fn, entropy, N), _floats(fn, stats, N, 2), k, _i64(fn, top_idx, N, k),
+            _floats(fn, top_logp, N, k))
+    ws = _space(fn, workspace, workspace_bytes)
+    _here(fn, z, idx, logp, entropy, stats, top_idx, top_logp)
+    _check(fn, lib().token_logprobs(zp, zf, z_ld, *args, *ws, _stream(stream)))
+    return logp
+
+
+def token_logprobs_bwd(z, idx, tau, stats, entropy, d_logp, d_entropy, grad_scale, g, stream=None):
+    """g (N x V: float32, FP16 or FP8 codes; may be z): the logits' gradient
+    times grad_scale from those of token_logprobs' logp (N x m) and entropy (N),
+    either None, and its stats and entropy."""
+    fn = "token_logprobs_bwd"
+    N, V = z.shape
+    zp, zf, z_ld = _matrix(fn, z, N, V, _FLOATS)
+    gp, gf, g_ld = _matrix(fn, g, N, V, _ANY)
+    m = 0 if idx is None else idx.shape[1]
+    args = (_i64(fn, idx, N, m), m, _floats(fn, stats, N, 2), _floats(fn, entropy, N),
+            _floats(fn, d_logp, N, m), _floats(fn, d_entropy, N))
+    _here(fn, z, idx, stats, entropy, d_logp, d_entropy, g)
+    _check(fn, lib().token_logprobs_bwd(zp, zf, z_ld, *args, N, V, float(tau), float(grad_scale),
+                                        gp, gf, g_ld, _stream(stream)))
     return g

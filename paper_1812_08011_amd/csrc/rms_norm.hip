@@ -1,0 +1,283 @@
+// rms_norm_fwd: a residual sum and its root-mean-square norm, in one pass.
+//
+// HBM-bound.  T threads own a row and keep it in registers, NV times eight
+// elements each, between the sum of squares and the result: every element is
+// read once and written once.  Rows wider than kWidest are read again.
+#include "row_ops.h"
+
+namespace fp8t {
+namespace {
+
+constexpr int64_t kAcross = 1 << 20;   // workgroups along a grid's first dimension
+constexpr int64_t kWidest = 1024 * 16;
+
+struct NormArgs {
+    const void* x;
+    const float* x_row_scale;
+    const void* r;
+    const void* w;
+    void* h;
+    void* y;
+    float* y_row_scale;
+    float* rstd;
+    int64_t x_ld, r_ld, h_ld, y_ld, T, W;
+    int w_format, y_format;
+    bool sum;                          // u is rounded to the stream's format
+    float eps, y_scale;
+};
+
+// 1 / sqrt(mean + eps) of a row whose squares add up to `ss`; the squares of
+// finite floats can pass FP32's largest: then `again` gives their sum times
+// 2^-160.  eps >= 2^-100 hides what squares lose below 2^-126.
+template <typename AGAIN>
+__device__ __forceinline__ float inverse_rms(float ss, int64_t W, float eps, AGAIN again) {
+    if (__builtin_expect(ss == INFINITY, 0)) {
+        const float s = again() / (float)W + (eps * 0x1p-80f) * 0x1p-80f;
+        return 0x1p-80f / sqrtf(s);                         // Inf in the row: 0
+    }
+    return 1.0f / sqrtf(ss / (float)W + eps);
+}
+__device__ __forceinline__ float row_scale(float top, float y_scale) {
+    return top > 0.0f && top < INFINITY ? fminf(y_scale / top, 0x1p126f) : 1.0f;
+}
+
+template <int FX, int FS>
+struct NormRow {
+    const NormArgs& a;
+    const fmt_t<FX>* x;
+    const fmt_t<FS>* r;
+    fmt_t<FS>* h;
+    float div;
+    __device__ __forceinline__ NormRow(const NormArgs& a_, int64_t t) : a(a_) {
+        x = static_cast<const fmt_t<FX>*>(a.x) + t * a.x_ld;
+        r = a.r ? static_cast<const fmt_t<FS>*>(a.r) + t * a.r_ld : nullptr;
+        h = a.h ? static_cast<fmt_t<FS>*>(a.h) + t * a.h_ld : nullptr;
+        div = a.x_row_scale ? a.x_row_scale[t] : 1.0f;
+    }
+    // u of elements c .. c + 7 from what was loaded
+    __device__ __forceinline__ void sum(const Eight<FX>& ex, const Eight<FS>& er, float* u) const {
+        values8<FX>(ex, u);
+        if (a.x_row_scale) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = u[i] / div;
+        }
+        if (r) {
+            float v[8];
+            values8<FS>(er, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] += v[i];
+        }
+        if (FS != FP8T_FMT_F32 && a.sum) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = through<FS>(u[i]);
+        }
+    }
+    __device__ __forceinline__ Eight<FS> residual(int64_t c) const {
+        return r ? load8<FS>(r, c, a.W) : Eight<FS>{};
+    }
+};
+
+// NV = 0: a row wider than the registers, read again for each of its sums.
+template <int FX, int FS, int T, int NV>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a) {
+    constexpr int kRows = T < 256 ? 256 / T : 1;            // rows of a workgroup
+    __shared__ float red[2][T < 256 ? 1 : T / 64];
+    const int tid = threadIdx.x % T;
+    const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + threadIdx.x / T;
+    if (t >= a.T) return;                                   // a wave or the workgroup
+    const NormRow<FX, FS> row(a, t);
+    float u[NV ? NV : 1][8], w[NV ? NV : 1][8];
+    float ss = 0.0f;
+    if constexpr (NV > 0) {
+        Eight<FX> ex[NV];
+        Eight<FS> er[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = (int64_t)(v * T + tid) * 8;
+            ex[v] = Eight<FX>{};
+            er[v] = Eight<FS>{};
+            if (c < a.W) {
+                ex[v] = load8<FX>(row.x, c, a.W);
+                er[v] = row.residual(c);
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = (int64_t)(v * T + tid) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[v][i] = 1.0f;
+            if (a.w && c < a.W) load_values8(a.w, a.w_format, c, a.W, w[v]);
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = (int64_t)(v * T + tid) * 8;
+            row.sum(ex[v], er[v], u[v]);
+            if (c >= a.W) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[v][i] = 0.0f;
+            } else if (row.h) {
+                store_some<FS>(row.h + c, left8(c, a.W), u[v]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss += u[v][i] * u[v][i];
+        }
+    } else {
+        for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
+            row.sum(load8<FX>(row.x, c, a.W), row.residual(c), u[0]);
+            if (row.h) store_some<FS>(row.h + c, left8(c, a.W), u[0]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss += u[0][i] * u[0][i];
+        }
+    }
+    // u of a wide row once more: h may have taken r's or x's place
+    auto reload = [&](int64_t c, float* v) {
+        if (row.h) values8<FS>(load8<FS>(row.h, c, a.W), v);
+        else row.sum(load8<FX>(row.x, c, a.W), row.residual(c), v);
+    };
+    ss = row_reduce<T>(ss, red[0], RowSum());
+    const float rstd = inverse_rms(ss, a.W, a.eps, [&]() {
+        float s = 0.0f;
+        auto add = [&](const float* v) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += (v[i] * 0x1p-80f) * (v[i] * 0x1p-80f);
+        };
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) add(u[v]);
+        } else {
+            for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
+                reload(c, u[0]);
+                add(u[0]);
+            }
+        }
+        return row_reduce<T>(s, red[1], RowSum());
+    });
+    if (a.rstd && tid == 0) a.rstd[t] = rstd;
+    if (!a.y) return;
+    float scale = a.y_scale;
+    auto norm = [&](float* v, const float* wv) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * wv[i];
+    };
+    auto weights = [&](int64_t c, float* wv) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wv[i] = 1.0f;
+        if (a.w) load_values8(a.w, a.w_format, c, a.W, wv);
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) norm(u[v], w[v]);
+    }
+    if (a.y_row_scale) {
+        float top = 0.0f;
+        auto most = [&](const float* v) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) top = maximum3_abs(top, v[i], v[i + 1]);
+        };
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) most(u[v]);
+        } else {
+            for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
+                reload(c, u[0]);
+                weights(c, w[0]);
+                norm(u[0], w[0]);
+                most(u[0]);
+            }
+        }
+        if constexpr (T > 64) __syncthreads();              // red[1] may be in use
+        scale = row_scale(row_reduce<T>(top, red[1], RowMax()), a.y_scale);
+        if (tid == 0) a.y_row_scale[t] = scale;
+    }
+    uint8_t* y = static_cast<uint8_t*>(a.y) +
+                 t * a.y_ld * (a.y_format == FP8T_FMT_F32 ? 4 : a.y_format == FP8T_FMT_FP16 ? 2 : 1);
+    auto out = [&](int64_t c, float* v) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= scale;
+        store_values8(y, a.y_format, c, left8(c, a.W), v);
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = (int64_t)(v * T + tid) * 8;
+            if (c < a.W) out(c, u[v]);
+        }
+    } else {
+        for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
+            reload(c, u[0]);
+            weights(c, w[0]);
+            norm(u[0], w[0]);
+            out(c, u[0]);
+        }
+    }
+}
+
+template <int FX, int FS, int T, int NV>
+void launch_rows(const NormArgs& a, hipStream_t stream) {
+    constexpr int kRows = T < 256 ? 256 / T : 1;
+    const int64_t n = (a.T + kRows - 1) / kRows, across = n < kAcross ? n : kAcross;
+    hipLaunchKernelGGL((rms_norm_kernel<FX, FS, T, NV>),
+                       dim3((unsigned)across, (unsigned)((n + across - 1) / across)), dim3(T < 256 ? 256 : T), 0,
+                       stream, a);
+}
+
+template <int FX, int FS>
+void launch(const NormArgs& a, hipStream_t stream) {
+    if (a.W <= 64 * 8) launch_rows<FX, FS, 64, 1>(a, stream);
+    else if (a.W <= 64 * 16) launch_rows<FX, FS, 64, 2>(a, stream);
+    else if (a.W <= 256 * 8) launch_rows<FX, FS, 256, 1>(a, stream);
+    else if (a.W <= 256 * 16) launch_rows<FX, FS, 256, 2>(a, stream);
+    else if (a.W <= 1024 * 8) launch_rows<FX, FS, 1024, 1>(a, stream);
+    else if (a.W <= kWidest) launch_rows<FX, FS, 1024, 2>(a, stream);
+    else launch_rows<FX, FS, 1024, 0>(a, stream);
+}
+
+}  // namespace
+}  // namespace fp8t
+
+using namespace fp8t;
+
+extern "C" int rms_norm_fwd(const void* x, int x_format, int64_t x_ld, const float* x_row_scale,
+                            const void* r, int64_t r_ld, const void* w, int w_format, int64_t T,
+                            int64_t W, float eps, void* h, int s_format, int64_t h_ld, void* y,
+                            int y_format, int64_t y_ld, float y_scale, float* y_row_scale,
+                            float* rstd, hipStream_t stream) {
+    if (T < 0 || W < 0 || T > kMaxGemmDim || W > kMaxGemmDim || !float_or_16(x_format) ||
+        !float_or_16(s_format) || !float_or_16(w_format) || !storage_format(y_format) ||
+        !(eps >= 0x1p-100f) || !(eps <= 0x1p100f))
+        return FP8T_EINVAL;
+    if (T == 0 || W == 0) return FP8T_OK;
+    if ((!h && !y && !rstd) || !matrix_ok(x, x_ld, T, W) || (r && r_ld < W) || (h && h_ld < W) ||
+        (y && y_ld < W))
+        return FP8T_EINVAL;
+    if (y_row_scale && (!y || !(y_scale > 0.0f) || !(y_scale <= 3.4028234e38f))) return FP8T_EINVAL;
+    NormArgs a;
+    a.x = x;
+    a.x_row_scale = x_row_scale;
+    a.r = r;
+    a.w = w;
+    a.h = h;
+    a.y = y;
+    a.y_row_scale = y_row_scale;
+    a.rstd = rstd;
+    a.x_ld = x_ld;
+    a.r_ld = r_ld;
+    a.h_ld = h_ld;
+    a.y_ld = y_ld;
+    a.T = T;
+    a.W = W;
+    a.w_format = w_format;
+    a.y_format = y_format;
+    a.sum = r || h;
+    a.eps = eps;
+    a.y_scale = y_scale;
+    const bool f32 = s_format == FP8T_FMT_F32;
+    if (x_format == FP8T_FMT_F32) {
+        if (f32) launch<FP8T_FMT_F32, FP8T_FMT_F32>(a, stream);
+        else launch<FP8T_FMT_F32, FP8T_FMT_FP16>(a, stream);
+    } else {
+        if (f32) launch<FP8T_FMT_FP16, FP8T_FMT_F32>(a, stream);
+        else launch<FP8T_FMT_FP16, FP8T_FMT_FP16>(a, stream);
+    }
+    return launch_status();
+}

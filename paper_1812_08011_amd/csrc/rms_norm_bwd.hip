@@ -1,0 +1,353 @@
+// rms_norm_bwd: gradients of the root-mean-square norm.
+//
+// HBM-bound, one pass.  A workgroup owns a range of rows; the T threads of a
+// row keep it in registers (NV times eight elements each) between the mean and
+// the gradient, and their columns' sums of dw over the rows.  Those go to the
+// workspace, one row of sums for each workgroup, and a second kernel adds them
+// in order.  Rows wider than kWidest are read twice, and dw has a kernel of its
+// own.
+#include "row_ops.h"
+
+namespace fp8t {
+namespace {
+
+constexpr int64_t kAcross = 1 << 20;
+constexpr int64_t kWidest = 1024 * 16;
+constexpr int kDwThreads = 256, kJoinThreads = 1024;
+
+struct NormGradArgs {
+    const void* h;
+    const void* w;
+    const float* rstd;
+    const void* dy;
+    const void* dr;
+    void* dx;
+    uint8_t* dx8;
+    float* parts;                      // workgroups x W (null: no dw)
+    int64_t h_ld, dy_ld, dr_ld, dx_ld, dx8_ld, T, W;
+    int64_t share, blocks;             // rows of a group of T threads; workgroups
+    int w_format;
+    float dx8_scale;
+};
+
+template <int FD>
+__device__ __forceinline__ void put(const NormGradArgs& a, int64_t t, int64_t c, float* d) {
+    const int n = left8(c, a.W);
+    if (a.dx) store_some<FD>(static_cast<fmt_t<FD>*>(a.dx) + t * a.dx_ld + c, n, d);
+    if (a.dx8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] *= a.dx8_scale;
+        store_some<FP8T_FMT_FP8>(a.dx8 + t * a.dx8_ld + c, n, d);
+    }
+}
+
+template <int FH, int FY, int FD, int T, int NV>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGradArgs a) {
+    constexpr int kGroups = T < 256 ? 256 / T : 1;          // of a workgroup
+    __shared__ float red[2][T < 256 ? 1 : T / 64];
+    __shared__ float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? T * NV * 8 : 1];
+    const int tid = threadIdx.x % T, sub = threadIdx.x / T;
+    const int64_t t0 = ((int64_t)blockIdx.x * kGroups + sub) * a.share;
+    const int64_t t1 = t0 + a.share < a.T ? t0 + a.share : a.T;
+    float w[NV][8], dw[NV][8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int64_t c = (int64_t)(v * T + tid) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w[v][i] = 1.0f;
+            dw[v][i] = 0.0f;
+        }
+        if (a.w && c < a.W) load_values8(a.w, a.w_format, c, a.W, w[v]);
+    }
+    int turn = 0;
+    for (int64_t t = t0; t < t1; ++t) {
+        Eight<FH> eh[NV];
+        Eight<FY> ey[NV];
+        Eight<FD> er[NV];
+        const fmt_t<FH>* h = static_cast<const fmt_t<FH>*>(a.h) + t * a.h_ld;
+        const fmt_t<FY>* dy = static_cast<const fmt_t<FY>*>(a.dy) + t * a.dy_ld;
+        const fmt_t<FD>* dr = a.dr ? static_cast<const fmt_t<FD>*>(a.dr) + t * a.dr_ld : nullptr;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = (int64_t)(v * T + tid) * 8;
+            eh[v] = Eight<FH>{};
+            ey[v] = Eight<FY>{};
+            er[v] = Eight<FD>{};
+            if (c < a.W) {
+                eh[v] = load8<FH>(h, c, a.W);
+                ey[v] = load8<FY>(dy, c, a.W);
+                if (dr) er[v] = load8<FD>(dr, c, a.W);
+            }
+        }
+        const float rstd = a.rstd[t];
+        float n[NV][8], g[NV][8], dot = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            values8<FH>(eh[v], n[v]);
+            values8<FY>(ey[v], g[v]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[v][i] *= rstd;
+                dw[v][i] += g[v][i] * n[v][i];
+                g[v][i] *= w[v][i];
+                dot += g[v][i] * n[v][i];
+            }
+        }
+        const float m = row_reduce<T>(dot, red[turn], RowSum()) / (float)a.W;
+        turn ^= 1;
+        if (!a.dx && !a.dx8) continue;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = (int64_t)(v * T + tid) * 8;
+            if (c >= a.W) continue;
+            float d[8];
+            values8<FD>(er[v], d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float own = rstd * (g[v][i] - n[v][i] * m);
+                d[i] = dr ? d[i] + own : own;
+            }
+            put<FD>(a, t, c, d);
+        }
+    }
+    if (!a.parts) return;
+    if constexpr (kGroups > 1) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums[sub][(v * T + tid) * 8 + i] = dw[v][i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.W; c += 256) {
+            float s = sums[0][c];
+#pragma unroll
+            for (int g = 1; g < kGroups; ++g) s += sums[g][c];
+            a.parts[(int64_t)blockIdx.x * a.W + c] = s;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = (int64_t)(v * T + tid) * 8;
+            if (c < a.W)
+                store_some<FP8T_FMT_F32>(a.parts + (int64_t)blockIdx.x * a.W + c, left8(c, a.W), dw[v]);
+        }
+    }
+}
+
+// Wide rows: one row per workgroup, read twice.
+template <int FH, int FY, int FD>
+__global__ __launch_bounds__(1024) void rms_norm_bwd_wide_kernel(NormGradArgs a) {
+    __shared__ float red[16];
+    const int64_t t = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (t >= a.T) return;
+    const fmt_t<FH>* h = static_cast<const fmt_t<FH>*>(a.h) + t * a.h_ld;
+    const fmt_t<FY>* dy = static_cast<const fmt_t<FY>*>(a.dy) + t * a.dy_ld;
+    const fmt_t<FD>* dr = a.dr ? static_cast<const fmt_t<FD>*>(a.dr) + t * a.dr_ld : nullptr;
+    const float rstd = a.rstd[t];
+    float n[8], g[8], w[8], dot = 0.0f;
+    auto load = [&](int64_t c) {
+        values8<FH>(load8<FH>(h, c, a.W), n);
+        values8<FY>(load8<FY>(dy, c, a.W), g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 1.0f;
+        if (a.w) load_values8(a.w, a.w_format, c, a.W, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            n[i] *= rstd;
+            g[i] *= w[i];
+        }
+    };
+    for (int64_t c = (int64_t)threadIdx.x * 8; c < a.W; c += 8192) {
+        load(c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dot += g[i] * n[i];
+    }
+    const float m = row_reduce<1024>(dot, red, RowSum()) / (float)a.W;
+    for (int64_t c = (int64_t)threadIdx.x * 8; c < a.W; c += 8192) {
+        load(c);
+        float d[8];
+        if (dr) values8<FD>(load8<FD>(dr, c, a.W), d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float own = rstd * (g[i] - n[i] * m);
+            d[i] = dr ? d[i] + own : own;
+        }
+        put<FD>(a, t, c, d);
+    }
+}
+
+// dw of wide rows: a thread owns eight columns and a range of rows.
+template <int FH, int FY>
+__global__ __launch_bounds__(kDwThreads) void rms_norm_dw_kernel(NormGradArgs a) {
+    const int64_t c = ((int64_t)blockIdx.x * kDwThreads + threadIdx.x) * 8;
+    if (c >= a.W) return;
+    const int64_t t0 = blockIdx.y * a.share, t1 = t0 + a.share < a.T ? t0 + a.share : a.T;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int64_t t = t0; t < t1; ++t) {
+        float n[8], g[8];
+        values8<FH>(load8<FH>(static_cast<const fmt_t<FH>*>(a.h) + t * a.h_ld, c, a.W), n);
+        values8<FY>(load8<FY>(static_cast<const fmt_t<FY>*>(a.dy) + t * a.dy_ld, c, a.W), g);
+        const float rstd = a.rstd[t];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += g[i] * (n[i] * rstd);
+    }
+    store_some<FP8T_FMT_F32>(a.parts + blockIdx.y * a.W + c, left8(c, a.W), sum);
+}
+
+// dw = the sum of the workgroups' rows: a lane owns a column, each wave a range
+// of the rows, in order; the waves' sums are added in order.
+__global__ __launch_bounds__(kJoinThreads) void rms_norm_join_kernel(const float* parts, int64_t blocks,
+                                                                     int64_t W, void* dw, int dw_format) {
+    constexpr int kWaves = kJoinThreads / 64;
+    __shared__ float sums[kWaves][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t share = (blocks + kWaves - 1) / kWaves;
+    const int64_t g0 = wave * share, g1 = g0 + share < blocks ? g0 + share : blocks;
+    float sum = 0.0f;
+    if (c < W) {
+        constexpr int kAhead = 16;
+        for (int64_t g = g0; g < g1; g += kAhead) {
+            float x[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) x[u] = g + u < g1 ? parts[(g + u) * W + c] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) sum += x[u];
+        }
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave > 0 || c >= W) return;
+    sum = sums[0][lane];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) sum += sums[i][lane];
+    if (dw_format == FP8T_FMT_F32) static_cast<float*>(dw)[c] = sum;
+    else static_cast<uint16_t*>(dw)[c] = f32_to_fp16_rn(sum);
+}
+
+// Rows of a group of T threads, and workgroups (rows of partial sums).
+struct NormGradPlan {
+    int64_t share, blocks;
+};
+NormGradPlan norm_grad_plan(int64_t T, int64_t W) {
+    const int64_t threads = W <= 64 * 16 ? 64 : W <= 256 * 16 ? 256 : 1024;
+    const int64_t groups = threads < 256 ? 256 / threads : 1;
+    int64_t cus = device_cus();
+    if (cus <= 0) cus = 256;
+    // as many as run at a time, but two rows for each group at least
+    int64_t most = W > kWidest ? 64 : cus * 1024 / (threads * groups) * groups;
+    const int64_t pairs = (T + 1) / 2;
+    if (most > pairs) most = pairs;
+    if (most < 1) most = 1;
+    NormGradPlan p;
+    p.share = (T + most - 1) / most;
+    if (p.share < 1) p.share = 1;
+    const int64_t rows = W > kWidest ? p.share : p.share * groups;
+    p.blocks = (T + rows - 1) / rows;
+    return p;
+}
+
+template <int FH, int FY, int FD, int T, int NV>
+void launch_rows(const NormGradArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL((rms_norm_bwd_kernel<FH, FY, FD, T, NV>), dim3((unsigned)a.blocks),
+                       dim3(T < 256 ? 256 : T), 0, stream, a);
+}
+
+template <int FH, int FY, int FD>
+void launch(const NormGradArgs& a, hipStream_t stream) {
+    if (a.W <= 64 * 8) launch_rows<FH, FY, FD, 64, 1>(a, stream);
+    else if (a.W <= 64 * 16) launch_rows<FH, FY, FD, 64, 2>(a, stream);
+    else if (a.W <= 256 * 8) launch_rows<FH, FY, FD, 256, 1>(a, stream);
+    else if (a.W <= 256 * 16) launch_rows<FH, FY, FD, 256, 2>(a, stream);
+    else if (a.W <= 1024 * 8) launch_rows<FH, FY, FD, 1024, 1>(a, stream);
+    else if (a.W <= kWidest) launch_rows<FH, FY, FD, 1024, 2>(a, stream);
+    else {
+        if (a.dx || a.dx8) {
+            const int64_t across = a.T < kAcross ? a.T : kAcross;
+            hipLaunchKernelGGL((rms_norm_bwd_wide_kernel<FH, FY, FD>),
+                               dim3((unsigned)across, (unsigned)((a.T + across - 1) / across)), dim3(1024), 0,
+                               stream, a);
+        }
+        if (a.parts)
+            hipLaunchKernelGGL((rms_norm_dw_kernel<FH, FY>),
+                               dim3((unsigned)((a.W + 8 * kDwThreads - 1) / (8 * kDwThreads)),
+                                    (unsigned)a.blocks),
+                               dim3(kDwThreads), 0, stream, a);
+    }
+}
+
+template <int FH, int FD>
+void launch_dy(const NormGradArgs& a, int dy_format, hipStream_t stream) {
+    if (dy_format == FP8T_FMT_F32) launch<FH, FP8T_FMT_F32, FD>(a, stream);
+    else if (dy_format == FP8T_FMT_FP16) launch<FH, FP8T_FMT_FP16, FD>(a, stream);
+    else launch<FH, FP8T_FMT_FP8, FD>(a, stream);
+}
+
+bool norm_sizes_ok(int64_t T, int64_t W) {
+    return T >= 0 && W >= 0 && T <= kMaxGemmDim && W <= kMaxGemmDim;
+}
+
+}  // namespace
+}  // namespace fp8t
+
+using namespace fp8t;
+
+extern "C" size_t rms_norm_bwd_workspace_size(int64_t T, int64_t W) {
+    if (!norm_sizes_ok(T, W) || T == 0 || W == 0) return 0;
+    return sizeof(float) * (size_t)norm_grad_plan(T, W).blocks * (size_t)W;
+}
+
+extern "C" int rms_norm_bwd(const void* h, int h_format, int64_t h_ld, const void* w, int w_format,
+                            const float* rstd, const void* dy, int dy_format, int64_t dy_ld,
+                            const void* dr, int64_t dr_ld, int64_t T, int64_t W, void* dx,
+                            int d_format, int64_t dx_ld, uint8_t* dx8, int64_t dx8_ld,
+                            float dx8_scale, void* dw, int dw_format, void* workspace,
+                            size_t workspace_bytes, hipStream_t stream) {
+    if (!norm_sizes_ok(T, W) || !float_or_16(h_format) || !float_or_16(w_format) ||
+        !storage_format(dy_format) || !float_or_16(d_format) || !float_or_16(dw_format) ||
+        (!workspace && workspace_bytes))
+        return FP8T_EINVAL;
+    if (W == 0) return FP8T_OK;
+    if (!dx && !dx8 && !dw) return FP8T_EINVAL;
+    if (!matrix_ok(h, h_ld, T, W) || !matrix_ok(dy, dy_ld, T, W) || (T > 0 && !rstd) ||
+        (dr && dr_ld < W) || (dx && dx_ld < W) || (dx8 && dx8_ld < W) || !aligned(workspace, 16))
+        return FP8T_EINVAL;
+    const NormGradPlan p = norm_grad_plan(T, W);
+    if (dw && T > 0 && workspace_bytes < rms_norm_bwd_workspace_size(T, W)) return FP8T_EWORKSPACE;
+    NormGradArgs a;
+    a.h = h;
+    a.w = w;
+    a.rstd = rstd;
+    a.dy = dy;
+    a.dr = dr;
+    a.dx = dx;
+    a.dx8 = dx8;
+    a.parts = dw ? static_cast<float*>(workspace) : nullptr;
+    a.h_ld = h_ld;
+    a.dy_ld = dy_ld;
+    a.dr_ld = dr_ld;
+    a.dx_ld = dx_ld;
+    a.dx8_ld = dx8_ld;
+    a.T = T;
+    a.W = W;
+    a.share = p.share;
+    a.blocks = p.blocks;
+    a.w_format = w_format;
+    a.dx8_scale = dx8_scale;
+    if (T > 0) {
+        const bool f32 = d_format == FP8T_FMT_F32;
+        if (h_format == FP8T_FMT_F32) {
+            if (f32) launch_dy<FP8T_FMT_F32, FP8T_FMT_F32>(a, dy_format, stream);
+            else launch_dy<FP8T_FMT_F32, FP8T_FMT_FP16>(a, dy_format, stream);
+        } else {
+            if (f32) launch_dy<FP8T_FMT_FP16, FP8T_FMT_F32>(a, dy_format, stream);
+            else launch_dy<FP8T_FMT_FP16, FP8T_FMT_FP16>(a, dy_format, stream);
+        }
+    }
+    if (dw) {
+        const int64_t n = T > 0 ? p.blocks : 0;
+        hipLaunchKernelGGL(rms_norm_join_kernel, dim3((unsigned)((W + 63) / 64)), dim3(kJoinThreads), 0, stream,
+                           a.parts, n, W, dw, dw_format);
+    }
+    return launch_status();
+}

@@ -1,0 +1,115 @@
+// Rows of codes or floats at any address, eight elements at a time, and
+// reductions over the threads of a row.
+#pragma once
+
+#include "fp8train_tokens.h"
+#include "lm_formats.h"
+
+namespace fp8t {
+
+// Elements c .. c + 7 of a row of W as they are stored, 0 past its end.
+template <int FMT>
+__device__ __forceinline__ Eight<FMT> load8(const fmt_t<FMT>* row, int64_t c, int64_t W) {
+    if (c + 8 <= W) return *reinterpret_cast<const Eight<FMT>*>(row + c);
+    Eight<FMT> e;
+    if constexpr (FMT == FP8T_FMT_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e.a[i] = c + i < W ? row[c + i] : 0.0f;
+            e.b[i] = c + 4 + i < W ? row[c + 4 + i] : 0.0f;
+        }
+    } else if constexpr (FMT == FP8T_FMT_FP16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = c + 2 * i < W ? row[c + 2 * i] : 0;
+            const uint32_t hi = c + 2 * i + 1 < W ? row[c + 2 * i + 1] : 0;
+            e.a[i] = lo | (hi << 16);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + 4 * i + j < W) w |= (uint32_t)row[c + 4 * i + j] << (8 * j);
+            e.a[i] = w;
+        }
+    }
+    return e;
+}
+
+template <int FMT>
+__device__ __forceinline__ void values8(const Eight<FMT>& e, float* x) {
+    if constexpr (FMT == FP8T_FMT_FP8) {
+        // E5M2 to FP32, exact, specials included
+        typedef float v2f __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const v2f lo = __builtin_amdgcn_cvt_pk_f32_bf8((int)e.a[i], false);
+            const v2f hi = __builtin_amdgcn_cvt_pk_f32_bf8((int)e.a[i], true);
+            x[4 * i] = lo[0];
+            x[4 * i + 1] = lo[1];
+            x[4 * i + 2] = hi[0];
+            x[4 * i + 3] = hi[1];
+        }
+    } else {
+        values_of<FMT>(e, special_in<FMT>(e), x);
+    }
+}
+
+// Eight values of a row in a format that is known at run time only (uniform).
+__device__ __forceinline__ void load_values8(const void* row, int fmt, int64_t c, int64_t W, float* x) {
+    if (fmt == FP8T_FMT_F32)
+        values8<FP8T_FMT_F32>(load8<FP8T_FMT_F32>(static_cast<const float*>(row), c, W), x);
+    else
+        values8<FP8T_FMT_FP16>(load8<FP8T_FMT_FP16>(static_cast<const uint16_t*>(row), c, W), x);
+}
+
+// n <= 8 results (n > 0) to elements c .. of a row.
+__device__ __forceinline__ void store_values8(void* row, int fmt, int64_t c, int n, const float* x) {
+    if (fmt == FP8T_FMT_F32) store_some<FP8T_FMT_F32>(static_cast<float*>(row) + c, n, x);
+    else if (fmt == FP8T_FMT_FP16) store_some<FP8T_FMT_FP16>(static_cast<uint16_t*>(row) + c, n, x);
+    else store_some<FP8T_FMT_FP8>(static_cast<uint8_t*>(row) + c, n, x);
+}
+
+// A float as its nearest value in a stream's format.
+template <int FMT>
+__device__ __forceinline__ float through(float x) {
+    return FMT == FP8T_FMT_FP16 ? fp16_to_f32(f32_to_fp16_rn(x)) : x;
+}
+
+__device__ __forceinline__ int left8(int64_t c, int64_t W) {
+    return W - c < 8 ? (int)(W - c) : 8;
+}
+
+// A reduction over the T threads of a row (T 64: a wave; else the workgroup),
+// every thread gets the same bits.  red: T / 64 floats, free before the call.
+template <int T, typename OP>
+__device__ __forceinline__ float row_reduce(float x, float* red, OP op) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x = op(x, __shfl_xor(x, d));
+    if constexpr (T > 64) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = red[0];
+#pragma unroll
+        for (int i = 1; i < T / 64; ++i) x = op(x, red[i]);
+    }
+    return x;
+}
+struct RowSum {
+    __device__ float operator()(float a, float b) const { return a + b; }
+};
+// NaN wins.
+struct RowMax {
+    __device__ float operator()(float a, float b) const { return a > b || a != a ? a : b; }
+};
+
+inline bool float_or_16(int f) { return f == FP8T_FMT_F32 || f == FP8T_FMT_FP16; }
+inline bool storage_format(int f) { return f >= FP8T_FMT_F32 && f <= FP8T_FMT_FP8; }
+// The row of W elements with stride ld that a call may read or write.
+inline bool matrix_ok(const void* p, int64_t ld, int64_t rows, int64_t W) {
+    return rows == 0 || W == 0 || (p && ld >= W);
+}
+
+}  // namespace fp8t
