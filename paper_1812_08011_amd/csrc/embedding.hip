@@ -10,11 +10,13 @@
 //             twice: first it counts each row's tokens per wave and those below
 //             its rows (that is where its part of the sorted list begins), then
 //             every wave places its own tokens in order.
-//   sum    -- a group of lanes takes the runs (equal tokens) that begin in a
-//             piece of kPiece sorted tokens.  A run of more than kLong is cut
-//             at the pieces' borders, and the parts' sums go to the workspace.
-//             Other workgroups write the rows that no token names.
-//   join   -- adds the parts of the long runs in their order.
+//   sum    -- a workgroup takes a piece of the sorted tokens, each of its groups
+//             of lanes the runs (equal tokens) that begin in a share of
+//             kShare tokens.  A run of more than kLong is cut at the shares'
+//             borders: the parts' sums meet in LDS, in order, and those of runs
+//             that leave the piece go to the workspace.  Other workgroups write
+//             the rows that no token names.
+//   join   -- adds the parts of such runs in their order.
 #include "row_ops.h"
 
 namespace fp8t {
@@ -84,8 +86,9 @@ void launch_fwd(const EmbedArgs& a, hipStream_t stream) {
 
 constexpr int kIndexThreads = 1024, kWaves = kIndexThreads / 64, kMaxRows = 512;
 constexpr int kSeen = 192;             // tokens of its rows that a wave of the index kernel keeps
-constexpr int kPiece = 32, kLong = 64; // sorted tokens per piece; the longest run that is not cut
-static_assert(kLong >= kPiece, "a run longer than kLong passes a border of its piece");
+constexpr int kShare = 16, kLong = 32; // sorted tokens per group of lanes; the longest run that is not cut
+constexpr int kZeroRows = 16;          // rows that a wave looks at for those without a token
+static_assert(kLong >= kShare, "a run longer than kLong passes a border of its share");
 
 struct GradArgs {
     const int64_t* tokens;
@@ -96,8 +99,8 @@ struct GradArgs {
     int R;                             // vocabulary rows per index workgroup
     int log_lanes;                     // lanes of a row of errors, eight columns each
     int slabs;                         // column slabs of 8 << log_lanes
-    int pieces;
-    int64_t piece_blocks, zero_blocks;
+    int piece;                         // sorted tokens of a workgroup: its groups' shares
+    int64_t pieces, piece_blocks, zero_blocks;
     int* start;                        // V + 1: a row's first sorted token
     int2* list;                        // T: (token, position), sorted
     float* parts;                      // pieces x 2 x W: sums of cut runs
@@ -221,13 +224,11 @@ template <int FE, int FG>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (block >= a.piece_blocks) {
-        // rows without a token: 64 a wave, of one slab
-        const int64_t z = block - a.piece_blocks, rows = 64;
+        // rows without a token: among kZeroRows a wave
+        const int64_t z = block - a.piece_blocks;
         const int lane = threadIdx.x & 63;
-        const int64_t v0 = (z * (kThreads / 64) + (threadIdx.x >> 6)) * rows;
-        if (v0 >= a.V) return;
-        const int64_t v = v0 + lane;
-        const bool none = v < a.V && a.start[v] == a.start[v + 1];
+        const int64_t v0 = (z * (kThreads / 64) + (threadIdx.x >> 6)) * kZeroRows, v = v0 + lane;
+        const bool none = lane < kZeroRows && v < a.V && a.start[v] == a.start[v + 1];
         uint64_t todo = __ballot(none);
         const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         while (todo) {
@@ -238,60 +239,112 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
         }
         return;
     }
-    const int lanes = 1 << a.log_lanes, per = kThreads >> a.log_lanes;
-    const int64_t unit = block * per + (threadIdx.x >> a.log_lanes);
-    const int64_t p = unit / a.slabs;
-    const int64_t c = ((unit % a.slabs) * lanes + (threadIdx.x & (lanes - 1))) * 8;
+    const int per = kThreads >> a.log_lanes, group = threadIdx.x >> a.log_lanes;
+    const int lane = threadIdx.x & ((1 << a.log_lanes) - 1);
+    const int64_t p = block / a.slabs;
+    const int64_t c = ((block % a.slabs << a.log_lanes) + lane) * 8;
     const int n = a.start[a.V];
-    if (p * kPiece >= n || c >= a.W) return;
-    const int from = (int)p * kPiece, to = from + kPiece < n ? from + kPiece : n;
-    const fmt_t<FE>* e = static_cast<const fmt_t<FE>*>(a.e);
-    // runs that began before this piece: whose they are unless they are long
-    int i = from;
-    int2 at = a.list[i];
-    int begin = a.start[at.x], end = a.start[at.x + 1];
-    if (begin < from && end - begin <= kLong) {
-        i = end;                                            // the piece where it began sums it
-        if (i >= to) return;
-        at = a.list[i];
-        begin = i;
-        end = a.start[at.x + 1];
-    }
-    while (i < to) {
-        const bool cut = end - begin > kLong;
-        const int stop = cut && end > to ? to : end;
+    if (p * a.piece >= n) return;
+    // what a group leaves of cut runs: [0] of one that began before its share,
+    // [1] of one that begins there (whole workgroups' worth: 256 x 8 floats each)
+    __shared__ float4 part[2][2][kThreads];
+    __shared__ int left[2][kThreads];                       // their tokens, -1: none
+    const int from = (int)p * a.piece + group * kShare, to = from + kShare < n ? from + kShare : n;
+    if (lane == 0) left[0][group] = left[1][group] = -1;
+    if (from < n) {
+        const fmt_t<FE>* e = static_cast<const fmt_t<FE>*>(a.e) + c;
+        const int64_t room = a.W - c;                       // <= 0: columns past the row's end
+        const int head = a.list[from].x, tail = a.list[to - 1].x;
+        const int head_begin = a.start[head], head_end = a.start[head + 1];
+        const int tail_begin = a.start[tail], tail_end = a.start[tail + 1];
+        int i = from, last = to;
+        const bool cut_head = head_begin < from && head_end - head_begin > kLong;
+        const bool cut_tail = tail_begin >= from && tail_end - tail_begin > kLong;
+        if (head_begin < from && !cut_head) i = head_end;   // the share where it began sums it
+        if (tail_begin >= i && !cut_tail && tail_end > to) last = tail_end;
+        if (lane == 0 && cut_head) left[0][group] = head;
+        if (lane == 0 && cut_tail) left[1][group] = tail;
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        const int v = at.x;
+        int v = i < last ? a.list[i].x : -1;
+        auto flush = [&]() {
+            if ((v == head && cut_head) || (v == tail && cut_tail)) {
+                const int at = v == head && cut_head ? 0 : 1;
+                part[at][0][threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                part[at][1][threadIdx.x] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+            } else if (room > 0) {
+                grad_out<FG>(a, v, c, sum);
+            }
+        };
         constexpr int kAhead = 8;
-        for (int j = i; j < stop; j += kAhead) {
-            Eight<FE> x[kAhead] = {};
+        int2 next[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (j + u < stop) x[u] = load8<FE>(e + (int64_t)a.list[j + u].y * a.e_ld, c, a.W);
+        for (int u = 0; u < kAhead; ++u) next[u] = a.list[i + u < last ? i + u : from];
+        for (int j = i; j < last; j += kAhead) {
+            Eight<FE> x[kAhead] = {};
+            int tok[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
+                tok[u] = next[u].x;
+                if (j + u < last && room > 0) x[u] = load8<FE>(e + (int64_t)next[u].y * a.e_ld, 0, room);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                next[u] = a.list[j + kAhead + u < last ? j + kAhead + u : from];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (j + u >= last) break;
+                if (tok[u] != v) {
+                    flush();
+                    v = tok[u];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+                }
                 float w[8];
                 values8<FE>(x[u], w);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum[k] += w[k];
             }
         }
-        if (cut) {
-            float* part = a.parts + (p * 2 + (begin >= from)) * a.W + c;
-            store_some<FP8T_FMT_F32>(part, left8(c, a.W), sum);
-        } else {
-            grad_out<FG>(a, v, c, sum);
-        }
-        i = stop;
-        if (i < to) {
-            at = a.list[i];
-            begin = i;
-            end = a.start[at.x + 1];
-        }
+        if (i < last) flush();
     }
+    __syncthreads();
+    // the first group joins the parts of cut runs in their order; a run that
+    // began before the piece or goes on behind it leaves a part of its own
+    if (group > 0 || c >= a.W) return;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    int v = -1;
+    bool inside = false;                                    // the run began in this piece
+    auto done = [&](bool more) {
+        if (v < 0) return;
+        if (inside && !more) grad_out<FG>(a, v, c, sum);
+        else store_some<FP8T_FMT_F32>(a.parts + (p * 2 + inside) * a.W + c, left8(c, a.W), sum);
+    };
+    for (int g = 0; g < per; ++g)
+#pragma unroll
+        for (int at = 0; at < 2; ++at) {
+            if (left[at][g] < 0) continue;
+            if (left[at][g] != v) {
+                done(false);
+                v = left[at][g];
+                inside = at == 1;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+            }
+            const int from_lane = (g << a.log_lanes) + lane;
+            const float4 lo = part[at][0][from_lane], hi = part[at][1][from_lane];
+            sum[0] += lo.x;
+            sum[1] += lo.y;
+            sum[2] += lo.z;
+            sum[3] += lo.w;
+            sum[4] += hi.x;
+            sum[5] += hi.y;
+            sum[6] += hi.z;
+            sum[7] += hi.w;
+        }
+    done(v >= 0 && a.start[v + 1] > (p + 1) * a.piece);
 }
 
-// The long run that begins in piece p, if one does: it passes p's end.
+// The cut run that begins in piece p and goes on behind it, if one does.
 template <int FG>
 __global__ __launch_bounds__(kThreads) void embed_join_kernel(GradArgs a) {
     const int lanes = 1 << a.log_lanes, per = kThreads >> a.log_lanes;
@@ -300,19 +353,18 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(GradArgs a) {
     const int64_t p = unit / a.slabs;
     const int64_t c = ((unit % a.slabs) * lanes + (threadIdx.x & (lanes - 1))) * 8;
     const int n = a.start[a.V];
-    if ((p + 1) * kPiece > n || c >= a.W) return;
-    const int v = a.list[(p + 1) * kPiece - 1].x, begin = a.start[v], end = a.start[v + 1];
-    if (begin < p * kPiece || end - begin <= kLong) return;
-    const int last = (end - 1) / kPiece;
-    const int w = left8(c, a.W);
+    if ((p + 1) * a.piece >= n || c >= a.W) return;
+    const int v = a.list[(p + 1) * a.piece - 1].x, begin = a.start[v], end = a.start[v + 1];
+    if (begin < p * a.piece || end <= (p + 1) * a.piece || end - begin <= kLong) return;
+    const int64_t last = (end - 1) / a.piece;
     float sum[8];
-    for (int k = 0; k < 8; ++k) sum[k] = k < w ? a.parts[(p * 2 + 1) * a.W + c + k] : 0.0f;
+    values8<FP8T_FMT_F32>(load8<FP8T_FMT_F32>(a.parts + (p * 2 + 1) * a.W, c, a.W), sum);
     constexpr int kAhead = 8;
-    for (int q = (int)p + 1; q <= last; q += kAhead) {
+    for (int64_t q = p + 1; q <= last; q += kAhead) {
         Eight<FP8T_FMT_F32> x[kAhead] = {};
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (q + u <= last) x[u] = load8<FP8T_FMT_F32>(a.parts + (int64_t)(q + u) * 2 * a.W, c, a.W);
+            if (q + u <= last) x[u] = load8<FP8T_FMT_F32>(a.parts + (q + u) * 2 * a.W, c, a.W);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             float y[8];
@@ -325,7 +377,8 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(GradArgs a) {
 }
 
 struct GradPlan {
-    int R, log_lanes, slabs, pieces;
+    int R, log_lanes, slabs, piece;
+    int64_t pieces;
     size_t list, parts, bytes;         // offsets into the workspace: start, list, parts
 };
 
@@ -335,11 +388,12 @@ GradPlan grad_plan(int64_t T, int64_t V, int64_t W) {
     p.R = (int)(r < 16 ? 16 : r > kMaxRows ? kMaxRows : r);
     p.log_lanes = log_lanes(W, 64);
     p.slabs = (int)((W + (8 << p.log_lanes) - 1) / (8 << p.log_lanes));
-    p.pieces = (int)((T + kPiece - 1) / kPiece);
+    p.piece = kShare * (kThreads >> p.log_lanes);
+    p.pieces = (T + p.piece - 1) / p.piece;
     auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };
     p.list = up(sizeof(int) * (size_t)(V + 1));
     p.parts = p.list + up(sizeof(int2) * (size_t)T);
-    p.bytes = p.parts + (T > kLong ? sizeof(float) * 2 * (size_t)W * (size_t)p.pieces : 0);
+    p.bytes = p.parts + (p.pieces > 1 ? sizeof(float) * 2 * (size_t)W * (size_t)p.pieces : 0);
     return p;
 }
 
@@ -353,13 +407,14 @@ void launch_bwd(GradArgs a, hipStream_t stream) {
     const size_t lds = sizeof(int) * kWaves * (size_t)a.R;
     hipLaunchKernelGGL(embed_index_kernel, dim3((unsigned)((a.V + a.R - 1) / a.R)), dim3(kIndexThreads), lds,
                        stream, a);
-    const int64_t per = kThreads >> a.log_lanes;
-    const int64_t blocks = ((int64_t)a.pieces * a.slabs + per - 1) / per;
-    a.piece_blocks = blocks;
-    a.zero_blocks = (a.V + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL((embed_sum_kernel<FE, FG>), grid_of(blocks + a.zero_blocks), dim3(kThreads), 0, stream, a);
-    if (a.T > kLong)
-        hipLaunchKernelGGL((embed_join_kernel<FG>), grid_of(blocks), dim3(kThreads), 0, stream, a);
+    a.piece_blocks = a.pieces * a.slabs;
+    a.zero_blocks = (a.V + kThreads / 64 * kZeroRows - 1) / (kThreads / 64 * kZeroRows);
+    hipLaunchKernelGGL((embed_sum_kernel<FE, FG>), grid_of(a.piece_blocks + a.zero_blocks), dim3(kThreads), 0, stream, a);
+    if (a.pieces > 1) {
+        const int64_t per = kThreads >> a.log_lanes;
+        hipLaunchKernelGGL((embed_join_kernel<FG>), grid_of((a.piece_blocks + per - 1) / per), dim3(kThreads), 0,
+                           stream, a);
+    }
 }
 
 bool grad_sizes_ok(int64_t T, int64_t V, int64_t W) {
@@ -438,6 +493,7 @@ extern "C" int embed_bwd(const int64_t* tokens, int64_t T, const void* e, int e_
     a.R = p.R;
     a.log_lanes = p.log_lanes;
     a.slabs = p.slabs;
+    a.piece = p.piece;
     a.pieces = p.pieces;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     a.start = reinterpret_cast<int*>(ws);

@@ -78,18 +78,21 @@ def test_gradient_formats(e, g):
     bwd(rng.integers(-1, 60, 300), draw(rng, (300, 100), e), 57, g, 3.25)
 
 
-@pytest.mark.parametrize("T", [0, 1, 2, 31, 32, 33, 63, 64, 65, 129, 1000])
-def test_gradient_run_lengths(T):
+@pytest.mark.parametrize("W", [3, 24, 260, 520, 1030])
+@pytest.mark.parametrize("T", [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 129, 1000, 5000])
+def test_gradient_run_lengths(T, W):
     """One token for all: runs that end before, at and behind the borders of
-    the pieces and of what is not cut; with other tokens before and behind."""
+    the pieces, of their shares and of what is not cut; with other tokens, and
+    long runs of theirs, before and behind."""
     rng = np.random.default_rng(53)
-    e = draw(rng, (T, 24), F16)
+    e = draw(rng, (T, W), F16)
     bwd(np.full(T, 5), e, 9, F32, 1.0)
-    for before in (1, 16, 31, 32, 33):
-        tok = np.full(T + before + 40, 5)
-        tok[:before], tok[T + before:] = 2, np.arange(40) % 3 + 6
+    for before in (1, 15, 16, 31, 33, 64, 200):
+        tok = np.full(T + before + 140, 5)
+        tok[:before], tok[T + before:] = 2, np.arange(140) % 3 + 6
+        tok[T + before + 60:] = 8
         rng.shuffle(tok)
-        bwd(tok, draw(rng, (len(tok), 24), F16), 9, F32, 1.0)
+        bwd(tok, draw(rng, (len(tok), W), F16), 9, F32, 1.0)
 
 
 @pytest.mark.parametrize("W", [1, 5, 8, 17, 64, 512, 513, 1024, 1500])
