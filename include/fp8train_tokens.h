@@ -154,7 +154,7 @@ size_t rms_norm_bwd_workspace_size(int64_t T, int64_t W);
  * workspace: token_logprobs_workspace_size bytes for the fastest plan, or none
  * (workspace_bytes == 0, then a plan that needs none); it holds the partial
  * results of parts of rows that several workgroups share.
- * Errors: FP8T_EINVAL (negative size, N above 2^31 - 4097, V above 2^31 - 16385, V = 0
+ * Errors: FP8T_EINVAL (negative size, N above 2^31 - 4097, V above 2^31 - 131073, V = 0
  * with N > 0, m > 4096, k > FP8T_MAX_TOP, tau not from 2^-30 to 2^30, unknown
  * format, a stride below V, NULL pointer for non-empty data, no result, NULL
  * workspace with workspace_bytes > 0, or one that is not 16-byte aligned where

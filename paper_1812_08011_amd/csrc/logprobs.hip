@@ -6,16 +6,19 @@
 // ln S - (sum of d e^d) / S, both terms of one sign each, so that nothing
 // cancels.
 //
-// The k largest: the threads' maxima, 128 or 256 groups of them, hold at least
-// k different elements, so their k-th largest is a bound below which nothing
-// can be among the row's k.  Only threads whose own maximum reaches it read
-// their elements again (from the caches) and keep what reaches it too; those
-// few are ranked by (order of the value, lowest index first).  Where ties or an
-// order of the row let more reach it than there is room for, the row is walked
-// in tiles, and the bound is raised after each.
+// The k largest: on the way, the maximum of every block of 64 elements (eight
+// where rows are short) goes to LDS.  The maxima of 256 groups of blocks are 256
+// different elements, so their k-th largest is a bound below which nothing can
+// be among the row's k.  Only blocks that reach it, little more than k, are read
+// again -- whole lines -- and what reaches it too is kept; those few are ranked
+// by (order of the value, lowest index first).  Where ties or an order of the
+// row let more reach it than there is room for, the row is walked in tiles, and
+// the bound is raised after each.
 //
 // Where rows are few, several workgroups share one, each with the k largest of
 // its part, and a second kernel joins them.
+#include <type_traits>
+
 #include "row_ops.h"
 
 namespace fp8t {
@@ -23,7 +26,7 @@ namespace {
 
 constexpr int kMaxGiven = 4096;
 constexpr int64_t kAcross = 1 << 20;           // rows along a grid's first dimension
-constexpr int64_t kMaxV = INT32_MAX - 16384;   // a thread's positions stay in 32 bits
+constexpr int64_t kMaxV = INT32_MAX - 131072;  // a thread's next positions stay in 32 bits
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -98,14 +101,31 @@ __device__ __forceinline__ void sort_keys(uint64_t* keys, int n, int size) {
 // The k largest of keys[0, n) to the front, in order; n <= room.  All threads.
 template <int T>
 __device__ __forceinline__ void top_keys(uint64_t* keys, int n, int k) {
-    if (n <= T && n <= 256) {
-        // each key's place is the number of larger ones
-        const uint64_t mine = (int)threadIdx.x < n ? keys[threadIdx.x] : 0;
-        int place = 0;
-        if ((int)threadIdx.x < n)
-            for (int i = 0; i < n; ++i) place += keys[i] > mine;
+    if (n <= 256) {
+        // each key's place is the number of larger ones; the threads first take
+        // as many keys as they are, then the rest
+        constexpr int kOwn = T < 256 ? 256 / T : 1;
+        const int tid = threadIdx.x;
+        for (int i = n + tid; i < ((n + 7) & ~7); i += T) keys[i] = 0;
         __syncthreads();
-        if ((int)threadIdx.x < n && place < k) keys[place] = mine;
+        uint64_t mine[kOwn];
+        int place[kOwn];
+#pragma unroll
+        for (int s = 0; s < kOwn; ++s) {
+            if (s * T + tid >= n) break;
+            mine[s] = keys[s * T + tid];
+            place[s] = 0;
+            for (int i = 0; i < n; i += 8)
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(keys + i + j);
+                    place[s] += (int)(two.x > mine[s]) + (int)(two.y > mine[s]);
+                }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < kOwn; ++s)
+            if (s * T + tid < n && place[s] < k) keys[place[s]] = mine[s];
         __syncthreads();
         return;
     }
@@ -135,15 +155,122 @@ __device__ __forceinline__ Eight<FZ> load_logits(const fmt_t<FZ>* row, int v, in
     return e;
 }
 
+// Logits as the sums take them: times 2^-96 from FP16 (the codes' fields moved
+// into a float's, one instruction less), as they are from floats.  Values that
+// are not finite come out as finite FP16 ones of 2^32 and more.
+template <int FZ>
+struct Raw {
+    static constexpr float kUnit = FZ == FP8T_FMT_FP16 ? 0x1p96f : 1.0f;
+    __device__ static __forceinline__ void values(const Eight<FZ>& e, float* y) {
+        if constexpr (FZ == FP8T_FMT_F32) {
+            values8<FZ>(e, y);
+        } else {
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[2 * i] = __uint_as_float((uint32_t)((int32_t)(e.a[i] << 16) >> 2) & 0x9FFFC000u);
+                y[2 * i + 1] = __uint_as_float((uint32_t)((int32_t)e.a[i] >> 2) & 0x9FFFC000u);
+                top = max3_abs(top, y[2 * i], y[2 * i + 1]);
+            }
+            if (__builtin_expect(top >= 0x1p-64f, 0)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = fp16_to_f32((e.a[i / 2] >> (16 * (i % 2))) & 0xFFFFu) * 0x1p-96f;
+            }
+        }
+    }
+};
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+// N times eight logits more: y is what Raw gives; top: the largest of each eight,
+// of the same unit.
+template <int FZ, int N>
+__device__ __forceinline__ void add_logits(Soft& x, const float (&y)[N][8], float (&top)[N], float to2,
+                                           float floor2) {
+    constexpr float kUnit = Raw<FZ>::kUnit;
+    float all = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        top[u] = fmaxf(y[u][0], y[u][1]);
+#pragma unroll
+        for (int i = 2; i < 8; i += 2) top[u] = max3(top[u], y[u][i], y[u][i + 1]);
+        all = fmaxf(all, top[u]);
+    }
+    all *= kUnit;
+    if (all > x.m) move_to(x, all, to2);
+    const float m = x.m == -INFINITY ? 0.0f : x.m;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // the distance first, exact or rounded once
+            const float d = (FZ == FP8T_FMT_F32 ? y[u][i] - m : __builtin_fmaf(y[u][i], kUnit, -m)) * to2;
+            const float p = __builtin_amdgcn_exp2f(d);
+            x.s += p;
+            x.t = __builtin_fmaf(fmaxf(d, floor2), p, x.t);  // d = -Inf adds 0
+        }
+}
+
+// The largest of eight neighbouring lanes, in all of them.
+__device__ __forceinline__ float max_of_8_lanes(float x) {
+    auto other = [](float v, auto ctrl) {
+        return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    x = fmaxf(x, other(x, std::integral_constant<int, 0xB1>()));    // lanes 1 0 3 2
+    x = fmaxf(x, other(x, std::integral_constant<int, 0x4E>()));    // lanes 2 3 0 1
+    return fmaxf(x, other(x, std::integral_constant<int, 0x141>()));  // mirrored in eight
+}
+
+// Where a row's blocks lie: tiles of T x 8 elements, of each `in_tile` blocks of
+// 8 or 64 elements; blocks of 64 of 1 << shift tiles (0, or 2 and more) may be
+// one.  At most `most` of them.
+struct Blocks {
+    int in_tile, units, shift, n;      // blocks of a tile; eights of a block; all blocks
+    bool fine;
+    __device__ __forceinline__ Blocks(int length, int T, int most) {
+        const int tiles = (length + T * 8 - 1) / (T * 8);
+        fine = tiles <= most / T;
+        in_tile = fine ? T : T / 8;
+        shift = 0;
+        if (!fine && tiles > most / in_tile)
+            for (shift = 2; ((tiles - 1) >> shift) + 1 > most / in_tile;) ++shift;
+        units = (fine ? 1 : 8) << shift;
+        n = (((tiles - 1) >> shift) + 1) * in_tile;
+    }
+    // The first element of eight number u of block i, from the part's start; it
+    // may lie behind the part's end, by less than a tenth of its length (blocks of
+    // several tiles: at least 17 times their tiles are there), below 2^32.
+    __device__ __forceinline__ uint32_t element(int i, int u, int T) const {
+        const uint32_t tile = (i / in_tile << shift) + (fine ? 0 : u >> 3), at = i % in_tile;
+        return tile * T * 8 + (fine ? at * 8 : at * 64 + (u & 7) * 8);
+    }
+};
+
 // What a row's sums are once joined: ln S and the entropy.
 __device__ __forceinline__ float log_sum(const Soft& x) {
     // the largest is +Inf, NaN, or nothing was above -Inf
     return x.m == -INFINITY || x.m == INFINITY ? NAN : log2f(x.s) * kLn2;
 }
 
+// A given token's logit, on its way since the kernel's start.
+struct Given {
+    bool used;
+    float z;
+};
+template <int FZ>
+__device__ __forceinline__ Given load_given(const LogprobArgs& a, int64_t n, const fmt_t<FZ>* z, int i) {
+    Given r = {false, 0.0f};
+    if (a.logp && i < a.m) {
+        const int64_t v = a.idx[n * a.m + i];
+        r.used = v >= 0 && v < a.V;
+        if (r.used) r.z = fmt_value<FZ>(z[v]);
+    }
+    return r;
+}
+
 // Results of row n but for the top: all threads of the workgroup.
 template <int FZ, int T>
-__device__ __forceinline__ void row_results(const LogprobArgs& a, int64_t n, const fmt_t<FZ>* z, Soft x) {
+__device__ __forceinline__ void row_results(const LogprobArgs& a, int64_t n, const fmt_t<FZ>* z, const Soft& x,
+                                            Given first) {
     const float ls = log_sum(x);
     if (threadIdx.x == 0) {
         if (a.stats) {
@@ -154,9 +281,8 @@ __device__ __forceinline__ void row_results(const LogprobArgs& a, int64_t n, con
     }
     if (a.logp)
         for (int i = threadIdx.x; i < a.m; i += T) {
-            const int64_t v = a.idx[n * a.m + i];
-            const bool used = v >= 0 && v < a.V;
-            a.logp[n * a.m + i] = used ? (fmt_value<FZ>(z[v]) - x.m) / a.tau - ls : 0.0f;
+            const Given g = i == (int)threadIdx.x ? first : load_given<FZ>(a, n, z, i);
+            a.logp[n * a.m + i] = g.used ? (g.z - x.m) / a.tau - ls : 0.0f;
         }
 }
 
@@ -177,97 +303,168 @@ __device__ __forceinline__ void top_result(const LogprobArgs& a, int64_t n, int 
 
 template <int FZ, int T, bool SPLIT>
 __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
-    constexpr int kRoom = T * 8, kWaves = T / 64, kGroups = 256;
-    __shared__ uint64_t keys[kRoom];
+    constexpr int kWaves = T / 64, kGroups = 256;
+    constexpr int kBlocks = T < 256 ? T * 8 : T * 4, kRoom = kBlocks;
+    __shared__ __attribute__((aligned(16))) uint64_t keys[kRoom];
     __shared__ Soft red[kWaves];
+    __shared__ float most[kBlocks];
+    __shared__ uint16_t chosen[kBlocks];
     __shared__ uint32_t group[kGroups];
     __shared__ uint32_t bound_of;
-    __shared__ int count;
+    __shared__ int count, reached;
     const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (n >= a.N) return;
     const int tid = threadIdx.x, lane = tid & 63;
     const fmt_t<FZ>* z = static_cast<const fmt_t<FZ>*>(a.z) + n * a.z_ld;
     const int v0 = SPLIT ? blockIdx.z * a.per : 0;
     const int v1 = SPLIT && v0 + a.per < a.V ? v0 + a.per : a.V;
-    const float to2 = a.to2;
+    // in vector registers: instructions that read scalar ones issue at half rate
+    const float to2 = __uint_as_float(in_vgpr(__float_as_uint(a.to2)));
+    const float floor2 = __uint_as_float(in_vgpr(__float_as_uint(-160.0f)));
+    const Given given = SPLIT ? Given{false, 0.0f} : load_given<FZ>(a, n, z, tid);
     Soft x = {-INFINITY, 0.0f, 0.0f};
-    constexpr int kAhead = 4;
-    for (int v = v0 + tid * 8; v < v1; v += T * 8 * kAhead) {
+    constexpr int kAhead = 4, kTile = T * 8;              // kAhead divides four, the least tiles of a block of several
+    constexpr float kUnit = Raw<FZ>::kUnit;
+    const Blocks blocks(v1 - v0, T, kBlocks);
+    const int tiles = (v1 - v0 + kTile - 1) / kTile;
+    // the maxima of a batch's or a tile's blocks: whole blocks are written once,
+    // those of several tiles by the one lane that has them all
+    auto joined = [&](int tile, float top) {
+        if (lane & 7) return;
+        const int i = (tile >> blocks.shift) * (T / 8) + (tid >> 3);
+        most[i] = tile & ((1 << blocks.shift) - 1) ? fmaxf(most[i], top) : top;
+    };
+    int tile = 0;
+    if (v0 + kTile * kAhead <= v1) {
+        // whole batches of tiles, the next one on its way
+        const fmt_t<FZ>* at = z + v0 + tid * 8;
         Eight<FZ> e[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (v + u * T * 8 < v1) e[u] = load_logits<FZ>(z, v + u * T * 8, v1);
+        for (int u = 0; u < kAhead; ++u) e[u] = *reinterpret_cast<const Eight<FZ>*>(at + u * kTile);
+        for (; v0 + (tile + kAhead) * kTile <= v1; tile += kAhead) {
+            float y[kAhead][8], top[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (v + u * T * 8 >= v1) break;
-            float y[8];
-            values8<FZ>(e[u], y);
-            float top = y[0];
+            for (int u = 0; u < kAhead; ++u) Raw<FZ>::values(e[u], y[u]);
+            at += kTile * kAhead;
+            if (v0 + (tile + 2 * kAhead) * kTile <= v1) {
 #pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
-            if (top > x.m) move_to(x, top, to2);
-            const float m = x.m == -INFINITY ? 0.0f : x.m;
+                for (int u = 0; u < kAhead; ++u) e[u] = *reinterpret_cast<const Eight<FZ>*>(at + u * kTile);
+            }
+            add_logits<FZ, kAhead>(x, y, top, to2, floor2);
+            if (a.k == 0) continue;
+            if (blocks.fine) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = (y[i] - m) * to2, p = __builtin_amdgcn_exp2f(d);
-                x.s += p;
-                x.t += fmaxf(d, -160.0f) * p;               // d = -Inf adds 0
+                for (int u = 0; u < kAhead; ++u) most[(tile + u) * T + tid] = top[u] * kUnit;
+            } else if (blocks.shift == 0) {
+                // the first lanes of eight write one tile's each
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) top[u] = max_of_8_lanes(top[u]);
+                const int u = lane & 7;
+                float mine = top[0];
+#pragma unroll
+                for (int i = 1; i < kAhead; ++i) mine = u == i ? top[i] : mine;
+                if (u < kAhead) most[(tile + u) * (T / 8) + (tid >> 3)] = mine * kUnit;
+            } else {
+                float all = top[0];
+#pragma unroll
+                for (int u = 1; u < kAhead; ++u) all = fmaxf(all, top[u]);
+                joined(tile, max_of_8_lanes(all) * kUnit);
             }
         }
     }
-    const float own = x.m;
-    const bool odd = x.s != x.s;                            // a NaN, or +Inf, among this thread's
+    for (; tile < tiles; ++tile) {
+        float y[1][8], top[1];
+        const int v = v0 + tile * kTile + tid * 8;
+        Raw<FZ>::values(load_logits<FZ>(z, v, v1), y[0]);
+        add_logits<FZ, 1>(x, y, top, to2, floor2);
+        if (a.k == 0) continue;
+        if (blocks.fine) most[tile * T + tid] = top[0] * kUnit;
+        else joined(tile, max_of_8_lanes(top[0]) * kUnit);
+    }
 #pragma unroll
     for (int d = 32; d; d >>= 1) {
         Soft y = {__shfl_xor(x.m, d), __shfl_xor(x.s, d), __shfl_xor(x.t, d)};
         x = join(x, y, to2);
     }
     if (lane == 0) red[tid >> 6] = x;
-    if (a.k > 0) {
-        if (tid == 0) count = 0;
-        // the threads' maxima in groups of T / 256 neighbours
-        uint32_t o = order_of(own);                         // a NaN beside it is above
-#pragma unroll
-        for (int d = 1; d < T / kGroups; d <<= 1) o = max(o, (uint32_t)__shfl_xor((int)o, d));
-        if (tid % (T / kGroups) == 0) group[tid / (T / kGroups)] = o;
-    }
+    if (tid == 0) count = reached = 0;
     __syncthreads();
     x = red[0];
 #pragma unroll
     for (int i = 1; i < kWaves; ++i) x = join(x, red[i], to2);
-    if (!SPLIT) row_results<FZ, T>(a, n, z, x);
+    if (!SPLIT) row_results<FZ, T>(a, n, z, x, given);
     else if (tid == 0) a.part_sums[n * a.parts + blockIdx.z] = make_float4(x.m, x.s, x.t, 0.0f);
     if (a.k == 0) return;
+    for (int g = tid; g < kGroups; g += T) {
+        float top = -INFINITY;
+        for (int i = g; i < blocks.n; i += kGroups) top = fmaxf(top, most[i]);
+        group[g] = order_of(top);
+    }
+    __syncthreads();
     if (tid < 64) {
-        // a bound that k groups at least reach: its bits from the highest on
-        uint32_t g[kGroups / 64], bound = 0;
+        // a bound that k groups at least reach, and few more: its bits from the
+        // first one in which the groups differ
+        uint32_t g[kGroups / 64], hi = 0, lo = 0xFFFFFFFFu;
 #pragma unroll
-        for (int i = 0; i < kGroups / 64; ++i) g[i] = group[i * 64 + lane];
-        for (int b = 31; b >= 0; --b) {
+        for (int i = 0; i < kGroups / 64; ++i) {
+            g[i] = group[i * 64 + lane];
+            hi = max(hi, g[i]);
+            lo = min(lo, g[i]);
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) {
+            hi = max(hi, (uint32_t)__shfl_xor((int)hi, d));
+            lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
+        }
+        hi = __builtin_amdgcn_readfirstlane(hi);
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        int b = hi == lo ? -1 : 31 - __clz(hi ^ lo);
+        uint32_t bound = b < 0 ? lo : lo & ~((2u << b) - 1u);
+        for (; b >= 0; --b) {
             const uint32_t tried = bound | (1u << b);
             int reach = 0;
 #pragma unroll
             for (int i = 0; i < kGroups / 64; ++i) reach += __popcll(__ballot(g[i] >= tried));
             if (reach >= a.k) bound = tried;
-            if (reach == a.k) break;
+            if (reach >= a.k && reach <= a.k + a.k / 8) break;
         }
         if (lane == 0) bound_of = bound;
     }
     __syncthreads();
     uint32_t bound = bound_of;
-    // elements that reach the bound, of threads whose largest does
-    if (odd || order_of(own) >= bound) {
-        for (int v = v0 + tid * 8; v < v1; v += T * 8) {
-            float y[8];
-            values8<FZ>(load_logits<FZ>(z, v, v1), y);
+    // the blocks that reach the bound; all of them where a NaN, or +Inf, is about
+    const bool odd = x.s != x.s;
+    for (int i = tid; i < blocks.n; i += T)
+        if (odd || order_of(most[i]) >= bound) chosen[atomicAdd(&reached, 1)] = (uint16_t)i;
+    __syncthreads();
+    const int items = reached * blocks.units;
+    // below every value where there are fewer groups than k (a NaN's bits then)
+    const float least = value_of_order(bound);
+    constexpr int kItems = 4;
+    for (int i = tid; i < items; i += T * kItems) {
+        Eight<FZ> e[kItems];
+        int at[kItems];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t o = order_of(y[i]);
-                if (o >= bound && v + i < v1) {
-                    const int at = atomicAdd(&count, 1);    // the order is made below
-                    if (at < kRoom) keys[at] = key_of(o, v + i);
-                }
+        for (int u = 0; u < kItems; ++u) {
+            const int item = i + u * T, who = item / blocks.units;
+            at[u] = v1;
+            if (item < items) {
+                const uint32_t v = v0 + blocks.element(chosen[who], item - who * blocks.units, T);
+                if (v < (uint32_t)v1) at[u] = (int)v;
             }
+            if (at[u] < v1) e[u] = load_logits<FZ>(z, at[u], v1);
+        }
+#pragma unroll
+        for (int u = 0; u < kItems; ++u) {
+            if (at[u] >= v1) continue;
+            float y[8];
+            values8<FZ>(e[u], y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (!(y[j] < least) && at[u] + j < v1) {
+                    const int to = atomicAdd(&count, 1);    // the order is made below
+                    if (to < kRoom) keys[to] = key_of(order_of(y[j]), at[u] + j);
+                }
         }
     }
     __syncthreads();
@@ -278,14 +475,9 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
         if (tid == 0) count = 0;
         __syncthreads();
         for (int w = v0; w < v1; w += kRoom / 2) {
-            const int v = w + tid * 4;
-            for (int i = 0; i < 4; ++i) {
-                if (v + i >= v1) break;
-                const uint32_t o = order_of(fmt_value<FZ>(z[v + i]));
-                if (o >= bound) {
-                    const int at = atomicAdd(&count, 1);
-                    keys[at] = key_of(o, v + i);
-                }
+            for (int v = w + tid; v < v1 && v < w + kRoom / 2; v += T) {
+                const uint32_t o = order_of(fmt_value<FZ>(z[v]));
+                if (o >= bound) keys[atomicAdd(&count, 1)] = key_of(o, v);
             }
             __syncthreads();
             have = count;
@@ -304,31 +496,62 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
         __syncthreads();
     }
     top_keys<T>(keys, have, a.k);
-    if (tid < a.k) {
-        const uint64_t key = tid < have ? keys[tid] : 0;
-        if (SPLIT) a.part_top[(n * a.parts + blockIdx.z) * a.k + tid] = key;
-        else top_result(a, n, tid, key, x);
+    for (int j = tid; j < a.k; j += T) {
+        const uint64_t key = j < have ? keys[j] : 0;
+        if (SPLIT) a.part_top[(n * a.parts + blockIdx.z) * a.k + j] = key;
+        else top_result(a, n, j, key, x);
     }
 }
 
-// A row's parts joined: their sums, and the k largest of their tops.
+// A row's parts joined: their sums, and the k largest of their tops, which are
+// in order: lists are merged two by two, each key's place found by bisection in
+// the other list (2 x 128 keys of 32 parts: 7 readings for each of 16 keys of a
+// thread, then half as many).
 constexpr int kJoinThreads = 256;
 template <int FZ>
 __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobArgs a) {
-    extern __shared__ uint64_t keys[];                      // parts x k, up to a power of two
+    extern __shared__ uint64_t keys[];                      // twice parts x k
     const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (n >= a.N) return;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, k = a.k;
+    const fmt_t<FZ>* z = static_cast<const fmt_t<FZ>*>(a.z) + n * a.z_ld;
+    const Given given = load_given<FZ>(a, n, z, tid);
+    uint64_t *from = keys, *to = keys + a.parts * k;
+    for (int i = tid; i < a.parts * k; i += kJoinThreads) from[i] = a.part_top[n * a.parts * k + i];
     const float4* sums = a.part_sums + n * a.parts;
-    Soft x = {sums[0].x, sums[0].y, sums[0].z};
-    for (int i = 1; i < a.parts; ++i) x = join(x, Soft{sums[i].x, sums[i].y, sums[i].z}, a.to2);
-    row_results<FZ, kJoinThreads>(a, n, static_cast<const fmt_t<FZ>*>(a.z) + n * a.z_ld, x);
-    if (a.k == 0) return;
-    const int all = a.parts * a.k;
-    for (int i = tid; i < all; i += kJoinThreads) keys[i] = a.part_top[n * all + i];
+    // every wave joins the parts' sums: lane i has part i's
+    const int lane = tid & 63;
+    const float4 own = lane < a.parts ? sums[lane] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+    Soft x = {own.x, own.y, own.z};
+#pragma unroll
+    for (int d = 32; d; d >>= 1)
+        x = join(x, Soft{__shfl_xor(x.m, d), __shfl_xor(x.s, d), __shfl_xor(x.t, d)}, a.to2);
+    row_results<FZ, kJoinThreads>(a, n, z, x, given);
+    if (k == 0) return;
     __syncthreads();
-    top_keys<kJoinThreads>(keys, all, a.k);
-    if (tid < a.k) top_result(a, n, tid, keys[tid], x);
+    for (int lists = a.parts; lists > 1; lists = (lists + 1) / 2) {
+        for (int i = tid; i < lists * k; i += kJoinThreads) {
+            const int l = i / k, j = i - l * k, other = l ^ 1;
+            const uint64_t mine = from[i];
+            int before = 0;                                 // of the other list; an equal one of the first list too
+            if (other < lists) {
+                const uint64_t* list = from + other * k;
+                int lo = 0, hi = k;
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (list[mid] > mine || (list[mid] == mine && (l & 1))) lo = mid + 1;
+                    else hi = mid;
+                }
+                before = lo;
+            }
+            if (j + before < k) to[l / 2 * k + j + before] = mine;
+        }
+        __syncthreads();
+        uint64_t* swap = from;
+        from = to;
+        to = swap;
+    }
+    if (tid < k) top_result(a, n, tid, from[tid], x);
 }
 
 struct LogprobPlan {
@@ -348,7 +571,12 @@ LogprobPlan logprob_plan(int64_t N, int64_t V, int64_t k) {
     parts = (V + per - 1) / per;
     p.parts = (int)parts;
     p.per = (int)per;
-    p.threads = per <= 16384 ? 256 : per <= 65536 ? 512 : 1024;
+    // The fewest threads whose sums are not the longer part of a row's time: each
+    // row waits for its sums, its bound and its few elements again, and more rows
+    // at a time hide that.  k 20, T 64, 128, 256, 512: 20000 x 1000 FP16 45, 55,
+    // 98, 206 us; 8192 x 8192 51, 46, 56, 103; 4096 x 32768 92, 75, 69, 75; 512 x
+    // 131072 87, 59, 36, 36 (with k 64 132, 75, 44, 38).
+    p.threads = per <= 2048 ? 64 : per <= 8192 ? 128 : per <= 65536 ? 256 : 512;
     p.top = sizeof(float4) * (size_t)N * (size_t)parts;
     p.bytes = parts > 1 ? p.top + sizeof(uint64_t) * (size_t)N * (size_t)parts * (size_t)k : 0;
     return p;
@@ -368,15 +596,13 @@ void launch_rows(const LogprobArgs& a, hipStream_t stream) {
 }
 template <int FZ>
 void launch(const LogprobArgs& a, int threads, hipStream_t stream) {
-    if (threads == 256) launch_rows<FZ, 256>(a, stream);
-    else if (threads == 512) launch_rows<FZ, 512>(a, stream);
-    else launch_rows<FZ, 1024>(a, stream);
-    if (a.parts > 1) {
-        int size = 2;
-        while (size < a.parts * a.k) size <<= 1;
+    if (threads == 64) launch_rows<FZ, 64>(a, stream);
+    else if (threads == 128) launch_rows<FZ, 128>(a, stream);
+    else if (threads == 256) launch_rows<FZ, 256>(a, stream);
+    else launch_rows<FZ, 512>(a, stream);
+    if (a.parts > 1)
         hipLaunchKernelGGL((logprob_join_kernel<FZ>), grid_of(a.N, 1), dim3(kJoinThreads),
-                           sizeof(uint64_t) * (size_t)size, stream, a);
-    }
+                           2 * sizeof(uint64_t) * (size_t)(a.parts * a.k), stream, a);
 }
 
 // ---- backward ----------------------------------------------------------------------------
@@ -513,7 +739,7 @@ extern "C" int token_logprobs(const void* z, int z_format, int64_t z_ld, const i
     if (p.bytes && workspace_bytes && !aligned(workspace, 16)) return FP8T_EINVAL;
     if (p.bytes && !workspace_bytes) {
         p.parts = 1;
-        p.threads = 1024;
+        p.threads = 512;
     }
     LogprobArgs a;
     a.z = z;
