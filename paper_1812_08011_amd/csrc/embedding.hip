@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
                 const bool used = (uint64_t)tok[r] < (uint64_t)a.V;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = used ? x[i] * a.scale : 0.0f;
-                store_some<FY>(static_cast<fmt_t<FY>*>(a.y) + t * a.y_ld + c, left8(c, a.W), x);
+                store_eight<FY>(static_cast<fmt_t<FY>*>(a.y) + t * a.y_ld + c, left8(c, a.W), x);
             }
         }
     }
@@ -217,7 +217,7 @@ __device__ __forceinline__ void grad_out(const GradArgs& a, int64_t v, int64_t c
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = sum[i] * a.scale;
-    store_some<FG>(static_cast<fmt_t<FG>*>(a.g) + v * a.g_ld + c, left8(c, a.W), y);
+    store_eight<FG>(static_cast<fmt_t<FG>*>(a.g) + v * a.g_ld + c, left8(c, a.W), y);
 }
 
 template <int FE, int FG>
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
             const int64_t at = v0 + __ffsll((unsigned long long)todo) - 1;
             todo &= todo - 1;
             for (int64_t c = lane * 8; c < a.W; c += 512)
-                store_some<FG>(static_cast<fmt_t<FG>*>(a.g) + at * a.g_ld + c, left8(c, a.W), zero);
+                store_eight<FG>(static_cast<fmt_t<FG>*>(a.g) + at * a.g_ld + c, left8(c, a.W), zero);
         }
         return;
     }

@@ -644,7 +644,7 @@ __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradAr
         const int v = v0 + (u * kGradThreads + tid) * 8;
         if (v < v1) e[u] = load_logits<FZ>(z, v, v1);
     }
-    const float top = a.stats[2 * n], ls2 = a.stats[2 * n + 1] * kLog2e;
+    const float top = a.stats[2 * n], ls = a.stats[2 * n + 1];
     const float dh = a.d_entropy ? a.d_entropy[n] : 0.0f;
     const float H = a.d_entropy ? a.entropy[n] : 0.0f;
     // the given tokens, their sum, and whether one of them is not 0
@@ -664,21 +664,26 @@ __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradAr
         sum = row_reduce<kGradThreads>(sum, red, RowSum());
         some = __syncthreads_or(some);
     }
-    auto gradient = [&](float x, float both) {
-        // the exponent is that of the distance from the row's largest, base 2
-        const float l = (x - top) * a.to2 - ls2, p = __builtin_amdgcn_exp2f(l);
-        const float f = sum + dh * (fmaxf(l, -160.0f) * kLn2 + H);
-        return a.scale * (both - p * f);
+    // p (D + dh (l + H)) = 2^d (c1 d + c0), d the distance from the row's largest
+    // in base 2: the row's factors are taken once, and no power of a sum
+    const float inv = a.scale * exp2f(-ls * kLog2e);
+    auto vgpr = [](float x) { return __uint_as_float(in_vgpr(__float_as_uint(x))); };
+    const float c0 = vgpr(-inv * (sum + dh * (H - ls))), c1 = vgpr(-inv * dh * kLn2);
+    const float to2 = vgpr(a.to2), floor2 = vgpr(-160.0f), m = vgpr(top);
+    auto gradient = [&](float distance) {
+        const float d = distance * to2;
+        return __builtin_amdgcn_exp2f(d) * __builtin_fmaf(c1, fmaxf(d, floor2), c0);
     };
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
         const int v = v0 + (u * kGradThreads + tid) * 8;
         if (v >= v1) break;
         float x[8];
-        values8<FZ>(e[u], x);
+        Raw<FZ>::values(e[u], x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = some ? gradient(x[i], 0.0f) : 0.0f;
-        store_some<FG>(g + v, left8(v, v1), x);
+        for (int i = 0; i < 8; ++i)
+            x[i] = some ? gradient(FZ == FP8T_FMT_F32 ? x[i] - m : __builtin_fmaf(x[i], Raw<FZ>::kUnit, -m)) : 0.0f;
+        store_eight<FG>(g + v, left8(v, v1), x);
     }
     if (a.m == 0 || !some) return;
     // the given tokens of this chunk, each with the sum of its occurrences, by
@@ -694,7 +699,7 @@ __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradAr
                 first &= j >= i;
                 both += given[j];
             }
-        if (first) g[v] = fmt_code<FG>(gradient(logit[i], both));
+        if (first) g[v] = fmt_code<FG>(a.scale * both + gradient(logit[i] - top));
     }
 }
 

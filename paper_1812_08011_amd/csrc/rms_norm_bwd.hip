@@ -37,7 +37,7 @@ __device__ __forceinline__ void put(const NormGradArgs& a, int64_t t, int64_t c,
     if (a.dx8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] *= a.dx8_scale;
-        store_some<FP8T_FMT_FP8>(a.dx8 + t * a.dx8_ld + c, n, d);
+        store_eight<FP8T_FMT_FP8>(a.dx8 + t * a.dx8_ld + c, n, d);
     }
 }
 
