@@ -98,40 +98,112 @@ __device__ __forceinline__ void sort_keys(uint64_t* keys, int n, int size) {
     __syncthreads();
 }
 
-// The k largest of keys[0, n) to the front, in order; n <= room.  All threads.
-template <int T>
-__device__ __forceinline__ void top_keys(uint64_t* keys, int n, int k) {
-    if (n <= 256) {
-        // each key's place is the number of larger ones; the threads first take
-        // as many keys as they are, then the rest
-        constexpr int kOwn = T < 256 ? 256 / T : 1;
-        const int tid = threadIdx.x;
-        for (int i = n + tid; i < ((n + 7) & ~7); i += T) keys[i] = 0;
-        __syncthreads();
-        uint64_t mine[kOwn];
-        int place[kOwn];
+// What the selection of a row's top keeps in LDS.
+constexpr int kFew = 256;
+template <int ROOM, int GROUPS>
+struct Selection {
+    static constexpr int kRoom = ROOM, kGroups = GROUPS;
+    __attribute__((aligned(16))) uint64_t keys[ROOM];
+    __attribute__((aligned(16))) uint64_t few[kFew];
+    uint64_t top[FP8T_MAX_TOP];
+    uint32_t group[GROUPS];
+    uint32_t bound;
+    int count, kept;
+};
+
+// A bound that at least k of the groups' maxima reach, and few more (below all
+// of them where there are fewer): its bits from the first one in which the
+// groups differ.  All threads; group is complete before the call.
+template <int T, typename S>
+__device__ __forceinline__ uint32_t find_bound(S& s, int k) {
+    __syncthreads();
+    constexpr int kGroups = S::kGroups;
+    const int lane = threadIdx.x & 63;
+    if (threadIdx.x < 64) {
+        uint32_t g[kGroups / 64], hi = 0, lo = 0xFFFFFFFFu;
 #pragma unroll
-        for (int s = 0; s < kOwn; ++s) {
-            if (s * T + tid >= n) break;
-            mine[s] = keys[s * T + tid];
-            place[s] = 0;
-            for (int i = 0; i < n; i += 8)
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(keys + i + j);
-                    place[s] += (int)(two.x > mine[s]) + (int)(two.y > mine[s]);
-                }
+        for (int i = 0; i < kGroups / 64; ++i) {
+            g[i] = s.group[i * 64 + lane];
+            hi = max(hi, g[i]);
+            lo = min(lo, g[i]);
         }
-        __syncthreads();
 #pragma unroll
-        for (int s = 0; s < kOwn; ++s)
-            if (s * T + tid < n && place[s] < k) keys[place[s]] = mine[s];
-        __syncthreads();
-        return;
+        for (int d = 32; d; d >>= 1) {
+            hi = max(hi, (uint32_t)__shfl_xor((int)hi, d));
+            lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
+        }
+        hi = __builtin_amdgcn_readfirstlane(hi);
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        int b = hi == lo ? -1 : 31 - __clz(hi ^ lo);
+        uint32_t bound = b < 0 ? lo : lo & ~((2u << b) - 1u);
+        for (; b >= 0; --b) {
+            const uint32_t tried = bound | (1u << b);
+            int reach = 0;
+#pragma unroll
+            for (int i = 0; i < kGroups / 64; ++i) reach += __popcll(__ballot(g[i] >= tried));
+            if (reach >= k) bound = tried;
+            if (reach >= k && reach <= k + k / 8) break;
+        }
+        if (lane == 0) s.bound = bound;
     }
-    int size = 2;
+    __syncthreads();
+    return s.bound;
+}
+
+// The k largest of keys[0, n) to top, each to the place that is the number of
+// larger ones.
+template <int T>
+__device__ __forceinline__ void rank_keys(uint64_t* keys, int n, uint64_t* top, int k) {
+    for (int i = n + threadIdx.x; i < ((n + 7) & ~7); i += T) keys[i] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int own = threadIdx.x; own < n; own += T) {
+        const uint64_t mine = keys[own];
+        int place = 0;
+#pragma unroll 1
+        for (int i = 0; i < n; i += 8)
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(keys + i + j);
+                place += (int)(two.x > mine) + (int)(two.y > mine);
+            }
+        if (place < k) top[place] = mine;
+    }
+    __syncthreads();
+}
+
+// Where the k largest of s.keys[0, n) then are, in order; n <= S::kRoom.  All
+// threads.
+template <int T, typename S>
+__device__ __forceinline__ const uint64_t* top_keys(S& s, int n, int k) {
+    constexpr int kGroups = S::kGroups;
+    const int tid = threadIdx.x;
+    if (n <= 128 || n <= k + k / 2) {                       // ranking costs n squared
+        rank_keys<T>(s.keys, n, s.top, k);
+        return s.top;
+    }
+    // fewer first: those that reach the k-th largest of the groups
+    for (int g = tid; g < kGroups; g += T) {
+        uint32_t top = 0;
+        for (int i = g; i < n; i += kGroups) top = max(top, (uint32_t)(s.keys[i] >> 32));
+        s.group[g] = top;
+    }
+    if (tid == 0) s.kept = 0;
+    const uint32_t bound = find_bound<T>(s, k);
+    for (int i = tid; i < n; i += T)
+        if ((uint32_t)(s.keys[i] >> 32) >= bound) {
+            const int at = atomicAdd(&s.kept, 1);
+            if (at < kFew) s.few[at] = s.keys[i];
+        }
+    __syncthreads();
+    if (s.kept <= kFew) {
+        rank_keys<T>(s.few, s.kept, s.top, k);
+        return s.top;
+    }
+    int size = 2;                                           // ties
     while (size < n) size <<= 1;
-    sort_keys<T>(keys, n, size);
+    sort_keys<T>(s.keys, n, size);
+    return s.keys;
 }
 
 template <int FZ>
@@ -301,17 +373,144 @@ __device__ __forceinline__ void top_result(const LogprobArgs& a, int64_t n, int 
     }
 }
 
+// The top of a part whose s.count keys that reach the bound are in s.keys, or
+// too many for it; written to row n's results or the part's place in the
+// workspace.
+template <int FZ, int T, bool SPLIT, typename S>
+__device__ __forceinline__ void finish_top(const LogprobArgs& a, S& s, int64_t n, const fmt_t<FZ>* z, int v0, int v1,
+                                           uint32_t bound, const Soft& x) {
+    constexpr int ROOM = S::kRoom;
+    const int tid = threadIdx.x;
+    __syncthreads();
+    int have = s.count;
+    if (have > ROOM) {
+        // too many: tiles of half the room, the k largest so far in front
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        for (int w = v0; w < v1; w += ROOM / 2) {
+            for (int v = w + tid; v < v1 && v < w + ROOM / 2; v += T) {
+                const uint32_t o = order_of(fmt_value<FZ>(z[v]));
+                if (o >= bound) s.keys[atomicAdd(&s.count, 1)] = key_of(o, v);
+            }
+            __syncthreads();
+            have = s.count;
+            __syncthreads();
+            if (have > ROOM / 2 - FP8T_MAX_TOP) {
+                const uint64_t* top = top_keys<T>(s, have, a.k);
+                have = have < a.k ? have : a.k;
+                if (top != s.keys)
+                    for (int i = tid; i < have; i += T) s.keys[i] = top[i];
+                // what comes later loses against an equal one
+                const uint32_t last = have == a.k ? (uint32_t)(top[a.k - 1] >> 32) : 0u;
+                if (have == a.k) bound = last == 0xFFFFFFFFu ? last : last + 1;
+                if (tid == 0) s.count = have;
+                __syncthreads();
+            }
+        }
+        have = s.count;
+        __syncthreads();
+    }
+    const uint64_t* top = top_keys<T>(s, have, a.k);
+    for (int j = tid; j < a.k; j += T) {
+        const uint64_t key = j < have ? top[j] : 0;
+        if (SPLIT) a.part_top[(n * a.parts + blockIdx.z) * a.k + j] = key;
+        else top_result(a, n, j, key, x);
+    }
+}
+
+// The sums of all threads.  red: T / 64 of them, free before the call.
+template <int T>
+__device__ __forceinline__ Soft block_join(Soft x, Soft* red, float to2) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        Soft y = {__shfl_xor(x.m, d), __shfl_xor(x.s, d), __shfl_xor(x.t, d)};
+        x = join(x, y, to2);
+    }
+    if constexpr (T > 64) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = red[0];
+#pragma unroll
+        for (int i = 1; i < T / 64; ++i) x = join(x, red[i], to2);
+    }
+    return x;
+}
+
+// Rows, or parts, of 2048 elements at most: one wave keeps them in registers, and
+// nothing is read again.  A group is half the eight elements of a load, so that
+// there are as many as alternatives but for the shortest rows, whose elements
+// all have room.
+constexpr int kShort = 2048;
+template <int FZ, bool SPLIT>
+__global__ __launch_bounds__(64) void logprob_short_kernel(LogprobArgs a) {
+    constexpr int T = 64, U = kShort / (T * 8), kTile = T * 8, kRoom = 512, kGroups = 2 * T * U;
+    __shared__ Selection<kRoom, kGroups> s;
+    const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (n >= a.N) return;
+    const int tid = threadIdx.x;
+    const fmt_t<FZ>* z = static_cast<const fmt_t<FZ>*>(a.z) + n * a.z_ld;
+    const int v0 = SPLIT ? blockIdx.z * a.per : 0;
+    const int v1 = SPLIT && v0 + a.per < a.V ? v0 + a.per : a.V;
+    const float to2 = __uint_as_float(in_vgpr(__float_as_uint(a.to2)));
+    const float floor2 = __uint_as_float(in_vgpr(__float_as_uint(-160.0f)));
+    Eight<FZ> e[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (v0 + u * kTile < v1) e[u] = load_logits<FZ>(z, v0 + u * kTile + tid * 8, v1);
+    const Given given = SPLIT ? Given{false, 0.0f} : load_given<FZ>(a, n, z, tid);
+    Soft x = {-INFINITY, 0.0f, 0.0f};
+    float top[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float half[2] = {-INFINITY, -INFINITY};
+        if (v0 + u * kTile < v1) {                          // the same for all
+            float y[1][8], most[1];
+            Raw<FZ>::values(e[u], y[0]);
+            add_logits<FZ, 1>(x, y, most, to2, floor2);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                half[h] = max3(fmaxf(y[0][4 * h], y[0][4 * h + 1]), y[0][4 * h + 2], y[0][4 * h + 3]) * Raw<FZ>::kUnit;
+        }
+        top[u] = fmaxf(half[0], half[1]);
+        if (a.k > 0) {
+            s.group[u * T + tid] = order_of(half[0]);
+            s.group[(U + u) * T + tid] = order_of(half[1]);
+        }
+    }
+    const bool odd = x.s != x.s;                            // a NaN, or +Inf, among this thread's
+    if (tid == 0) s.count = 0;
+    x = block_join<T>(x, nullptr, to2);
+    if (!SPLIT) row_results<FZ, T>(a, n, z, x, given);
+    else if (tid == 0) a.part_sums[n * a.parts + blockIdx.z] = make_float4(x.m, x.s, x.t, 0.0f);
+    if (a.k == 0) return;
+    const uint32_t bound = find_bound<T>(s, a.k);
+    // below every value where there are fewer groups than k (a NaN's bits then)
+    const float least = value_of_order(bound);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int v = v0 + u * kTile + tid * 8;
+        if (v >= v1 || (!odd && top[u] < least)) continue;
+        float y[8];
+        values8<FZ>(e[u], y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!(y[j] < least) && v + j < v1) {
+                const int to = atomicAdd(&s.count, 1);      // the order is made below
+                if (to < kRoom) s.keys[to] = key_of(order_of(y[j]), v + j);
+            }
+    }
+    finish_top<FZ, T, SPLIT>(a, s, n, z, v0, v1, bound, x);
+}
+
 template <int FZ, int T, bool SPLIT>
 __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
-    constexpr int kWaves = T / 64, kGroups = 256;
-    constexpr int kBlocks = T < 256 ? T * 8 : T * 4, kRoom = kBlocks;
-    __shared__ __attribute__((aligned(16))) uint64_t keys[kRoom];
-    __shared__ Soft red[kWaves];
+    constexpr int kBlocks = T < 256 ? T * 8 : T * 4, kRoom = T < 256 ? 512 : T * 4, kGroups = 256;
+    __shared__ Selection<kRoom, kGroups> s;
+    __shared__ Soft red[T / 64];
     __shared__ float most[kBlocks];
     __shared__ uint16_t chosen[kBlocks];
-    __shared__ uint32_t group[kGroups];
-    __shared__ uint32_t bound_of;
-    __shared__ int count, reached;
+    __shared__ int reached;
     const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (n >= a.N) return;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -323,7 +522,7 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
     const float floor2 = __uint_as_float(in_vgpr(__float_as_uint(-160.0f)));
     const Given given = SPLIT ? Given{false, 0.0f} : load_given<FZ>(a, n, z, tid);
     Soft x = {-INFINITY, 0.0f, 0.0f};
-    constexpr int kAhead = 4, kTile = T * 8;              // kAhead divides four, the least tiles of a block of several
+    constexpr int kAhead = 2, kTile = T * 8;              // kAhead divides four, the least tiles of a block of several
     constexpr float kUnit = Raw<FZ>::kUnit;
     const Blocks blocks(v1 - v0, T, kBlocks);
     const int tiles = (v1 - v0 + kTile - 1) / kTile;
@@ -381,57 +580,17 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
         if (blocks.fine) most[tile * T + tid] = top[0] * kUnit;
         else joined(tile, max_of_8_lanes(top[0]) * kUnit);
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        Soft y = {__shfl_xor(x.m, d), __shfl_xor(x.s, d), __shfl_xor(x.t, d)};
-        x = join(x, y, to2);
-    }
-    if (lane == 0) red[tid >> 6] = x;
-    if (tid == 0) count = reached = 0;
-    __syncthreads();
-    x = red[0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) x = join(x, red[i], to2);
+    if (tid == 0) s.count = reached = 0;
+    x = block_join<T>(x, red, to2);
     if (!SPLIT) row_results<FZ, T>(a, n, z, x, given);
     else if (tid == 0) a.part_sums[n * a.parts + blockIdx.z] = make_float4(x.m, x.s, x.t, 0.0f);
     if (a.k == 0) return;
     for (int g = tid; g < kGroups; g += T) {
         float top = -INFINITY;
         for (int i = g; i < blocks.n; i += kGroups) top = fmaxf(top, most[i]);
-        group[g] = order_of(top);
+        s.group[g] = order_of(top);
     }
-    __syncthreads();
-    if (tid < 64) {
-        // a bound that k groups at least reach, and few more: its bits from the
-        // first one in which the groups differ
-        uint32_t g[kGroups / 64], hi = 0, lo = 0xFFFFFFFFu;
-#pragma unroll
-        for (int i = 0; i < kGroups / 64; ++i) {
-            g[i] = group[i * 64 + lane];
-            hi = max(hi, g[i]);
-            lo = min(lo, g[i]);
-        }
-#pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            hi = max(hi, (uint32_t)__shfl_xor((int)hi, d));
-            lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
-        }
-        hi = __builtin_amdgcn_readfirstlane(hi);
-        lo = __builtin_amdgcn_readfirstlane(lo);
-        int b = hi == lo ? -1 : 31 - __clz(hi ^ lo);
-        uint32_t bound = b < 0 ? lo : lo & ~((2u << b) - 1u);
-        for (; b >= 0; --b) {
-            const uint32_t tried = bound | (1u << b);
-            int reach = 0;
-#pragma unroll
-            for (int i = 0; i < kGroups / 64; ++i) reach += __popcll(__ballot(g[i] >= tried));
-            if (reach >= a.k) bound = tried;
-            if (reach >= a.k && reach <= a.k + a.k / 8) break;
-        }
-        if (lane == 0) bound_of = bound;
-    }
-    __syncthreads();
-    uint32_t bound = bound_of;
+    const uint32_t bound = find_bound<T>(s, a.k);
     // the blocks that reach the bound; all of them where a NaN, or +Inf, is about
     const bool odd = x.s != x.s;
     for (int i = tid; i < blocks.n; i += T)
@@ -462,45 +621,12 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (!(y[j] < least) && at[u] + j < v1) {
-                    const int to = atomicAdd(&count, 1);    // the order is made below
-                    if (to < kRoom) keys[to] = key_of(order_of(y[j]), at[u] + j);
+                    const int to = atomicAdd(&s.count, 1);  // the order is made below
+                    if (to < kRoom) s.keys[to] = key_of(order_of(y[j]), at[u] + j);
                 }
         }
     }
-    __syncthreads();
-    int have = count;
-    if (have > kRoom) {
-        // too many: tiles of half the room, the k largest so far in front
-        __syncthreads();
-        if (tid == 0) count = 0;
-        __syncthreads();
-        for (int w = v0; w < v1; w += kRoom / 2) {
-            for (int v = w + tid; v < v1 && v < w + kRoom / 2; v += T) {
-                const uint32_t o = order_of(fmt_value<FZ>(z[v]));
-                if (o >= bound) keys[atomicAdd(&count, 1)] = key_of(o, v);
-            }
-            __syncthreads();
-            have = count;
-            __syncthreads();
-            if (have > kRoom / 2 - FP8T_MAX_TOP) {
-                top_keys<T>(keys, have, a.k);
-                have = have < a.k ? have : a.k;
-                // what comes later loses against an equal one
-                const uint32_t last = have == a.k ? (uint32_t)(keys[a.k - 1] >> 32) : 0u;
-                if (have == a.k) bound = last == 0xFFFFFFFFu ? last : last + 1;
-                if (tid == 0) count = have;
-                __syncthreads();
-            }
-        }
-        have = count;
-        __syncthreads();
-    }
-    top_keys<T>(keys, have, a.k);
-    for (int j = tid; j < a.k; j += T) {
-        const uint64_t key = j < have ? keys[j] : 0;
-        if (SPLIT) a.part_top[(n * a.parts + blockIdx.z) * a.k + j] = key;
-        else top_result(a, n, j, key, x);
-    }
+    finish_top<FZ, T, SPLIT>(a, s, n, z, v0, v1, bound, x);
 }
 
 // A row's parts joined: their sums, and the k largest of their tops, which are
@@ -555,7 +681,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobArgs 
 }
 
 struct LogprobPlan {
-    int threads, parts, per;
+    int parts, per;
     size_t top, bytes;                 // offset of the tops in the workspace; its size
 };
 LogprobPlan logprob_plan(int64_t N, int64_t V, int64_t k) {
@@ -571,12 +697,6 @@ LogprobPlan logprob_plan(int64_t N, int64_t V, int64_t k) {
     parts = (V + per - 1) / per;
     p.parts = (int)parts;
     p.per = (int)per;
-    // The fewest threads whose sums are not the longer part of a row's time: each
-    // row waits for its sums, its bound and its few elements again, and more rows
-    // at a time hide that.  k 20, T 64, 128, 256, 512: 20000 x 1000 FP16 45, 55,
-    // 98, 206 us; 8192 x 8192 51, 46, 56, 103; 4096 x 32768 92, 75, 69, 75; 512 x
-    // 131072 87, 59, 36, 36 (with k 64 132, 75, 44, 38).
-    p.threads = per <= 2048 ? 64 : per <= 8192 ? 128 : per <= 65536 ? 256 : 512;
     p.top = sizeof(float4) * (size_t)N * (size_t)parts;
     p.bytes = parts > 1 ? p.top + sizeof(uint64_t) * (size_t)N * (size_t)parts * (size_t)k : 0;
     return p;
@@ -595,11 +715,25 @@ void launch_rows(const LogprobArgs& a, hipStream_t stream) {
         hipLaunchKernelGGL((logprob_kernel<FZ, T, false>), grid_of(a.N, 1), dim3(T), 0, stream, a);
 }
 template <int FZ>
-void launch(const LogprobArgs& a, int threads, hipStream_t stream) {
-    if (threads == 64) launch_rows<FZ, 64>(a, stream);
-    else if (threads == 128) launch_rows<FZ, 128>(a, stream);
-    else if (threads == 256) launch_rows<FZ, 256>(a, stream);
-    else launch_rows<FZ, 512>(a, stream);
+void launch(const LogprobArgs& a, hipStream_t stream) {
+    // The fewest threads whose sums are not the longer part of a row's time: each
+    // row waits for its sums, its bound and its few elements again, and more rows
+    // at a time hide that.  k 20, T 128, 256 and 512: 8192 x 8192 FP16 51, 59 and
+    // 105 us; 4096 x 32768 75, 69 and 75; 512 x 131072 59, 36 and 36 (with k 64 75,
+    // 44 and 38).
+    const int length = a.parts > 1 ? a.per : a.V;
+    if (length <= kShort) {
+        if (a.parts > 1)
+            hipLaunchKernelGGL((logprob_short_kernel<FZ, true>), grid_of(a.N, a.parts), dim3(64), 0, stream, a);
+        else
+            hipLaunchKernelGGL((logprob_short_kernel<FZ, false>), grid_of(a.N, 1), dim3(64), 0, stream, a);
+    } else if (length <= 8192) {
+        launch_rows<FZ, 128>(a, stream);
+    } else if (length <= 65536) {
+        launch_rows<FZ, 256>(a, stream);
+    } else {
+        launch_rows<FZ, 512>(a, stream);
+    }
     if (a.parts > 1)
         hipLaunchKernelGGL((logprob_join_kernel<FZ>), grid_of(a.N, 1), dim3(kJoinThreads),
                            2 * sizeof(uint64_t) * (size_t)(a.parts * a.k), stream, a);
@@ -742,10 +876,7 @@ extern "C" int token_logprobs(const void* z, int z_format, int64_t z_ld, const i
     LogprobPlan p = logprob_plan(N, V, k);
     if (workspace_bytes && workspace_bytes < p.bytes) return FP8T_EWORKSPACE;
     if (p.bytes && workspace_bytes && !aligned(workspace, 16)) return FP8T_EINVAL;
-    if (p.bytes && !workspace_bytes) {
-        p.parts = 1;
-        p.threads = 512;
-    }
+    if (p.bytes && !workspace_bytes) p.parts = 1;
     LogprobArgs a;
     a.z = z;
     a.idx = idx;
@@ -765,8 +896,8 @@ extern "C" int token_logprobs(const void* z, int z_format, int64_t z_ld, const i
     a.to2 = kLog2e / tau;
     a.part_sums = static_cast<float4*>(workspace);
     a.part_top = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(workspace) + (p.parts > 1 ? p.top : 0));
-    if (z_format == FP8T_FMT_F32) launch<FP8T_FMT_F32>(a, p.threads, stream);
-    else launch<FP8T_FMT_FP16>(a, p.threads, stream);
+    if (z_format == FP8T_FMT_F32) launch<FP8T_FMT_F32>(a, stream);
+    else launch<FP8T_FMT_FP16>(a, stream);
     return launch_status();
 }
 
