@@ -54,12 +54,12 @@ struct NormRow {
         h = a.h ? static_cast<fmt_t<FS>*>(a.h) + t * a.h_ld : nullptr;
         div = a.x_row_scale ? a.x_row_scale[t] : 1.0f;
     }
-    // u of elements c .. c + 7 from what was loaded
-    __device__ __forceinline__ void sum(const Eight<FX>& ex, const Eight<FS>& er, float* u) const {
+    // u of elements c .. c + 7 from what was loaded; written to h
+    __device__ __forceinline__ void sum(const Eight<FX>& ex, const Eight<FS>& er, int64_t c, float* u) const {
         values8<FX>(ex, u);
         if (a.x_row_scale) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = u[i] / div;
+            for (int i = 0; i < 8; ++i) u[i] = c + i < a.W ? u[i] / div : 0.0f;
         }
         if (r) {
             float v[8];
@@ -67,9 +67,9 @@ struct NormRow {
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[i] += v[i];
         }
-        if (FS != FP8T_FMT_F32 && a.sum) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = through<FS>(u[i]);
+        if (a.sum) {
+            const Eight<FS> e = rounded8<FS>(u);
+            if (h && c < a.W) store_stored8<FS>(h + c, left8(c, a.W), e);
         }
     }
     __device__ __forceinline__ Eight<FS> residual(int64_t c) const {
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
     __shared__ float red[2][T < 256 ? 1 : T / 64];
     const int tid = threadIdx.x % T;
     const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + threadIdx.x / T;
-    if (t >= a.T) return;                                   // a wave or the workgroup
+    if (t >= a.T) return;                                   // all threads of a row
     const NormRow<FX, FS> row(a, t);
     float u[NV ? NV : 1][8], w[NV ? NV : 1][8];
     float ss = 0.0f;
@@ -111,20 +111,13 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int64_t c = (int64_t)(v * T + tid) * 8;
-            row.sum(ex[v], er[v], u[v]);
-            if (c >= a.W) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[v][i] = 0.0f;
-            } else if (row.h) {
-                store_some<FS>(row.h + c, left8(c, a.W), u[v]);
-            }
+            row.sum(ex[v], er[v], c, u[v]);                 // 0 past the row's end
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss += u[v][i] * u[v][i];
         }
     } else {
         for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
-            row.sum(load8<FX>(row.x, c, a.W), row.residual(c), u[0]);
-            if (row.h) store_some<FS>(row.h + c, left8(c, a.W), u[0]);
+            row.sum(load8<FX>(row.x, c, a.W), row.residual(c), c, u[0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss += u[0][i] * u[0][i];
         }
@@ -132,7 +125,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
     // u of a wide row once more: h may have taken r's or x's place
     auto reload = [&](int64_t c, float* v) {
         if (row.h) values8<FS>(load8<FS>(row.h, c, a.W), v);
-        else row.sum(load8<FX>(row.x, c, a.W), row.residual(c), v);
+        else row.sum(load8<FX>(row.x, c, a.W), row.residual(c), c, v);
     };
     ss = row_reduce<T>(ss, red[0], RowSum());
     const float rstd = inverse_rms(ss, a.W, a.eps, [&]() {
@@ -223,7 +216,10 @@ void launch_rows(const NormArgs& a, hipStream_t stream) {
 
 template <int FX, int FS>
 void launch(const NormArgs& a, hipStream_t stream) {
-    if (a.W <= 64 * 8) launch_rows<FX, FS, 64, 1>(a, stream);
+    if (a.W <= 8 * 8) launch_rows<FX, FS, 8, 1>(a, stream);
+    else if (a.W <= 16 * 8) launch_rows<FX, FS, 16, 1>(a, stream);
+    else if (a.W <= 32 * 8) launch_rows<FX, FS, 32, 1>(a, stream);
+    else if (a.W <= 64 * 8) launch_rows<FX, FS, 64, 1>(a, stream);
     else if (a.W <= 64 * 16) launch_rows<FX, FS, 64, 2>(a, stream);
     else if (a.W <= 256 * 8) launch_rows<FX, FS, 256, 1>(a, stream);
     else if (a.W <= 256 * 16) launch_rows<FX, FS, 256, 2>(a, stream);

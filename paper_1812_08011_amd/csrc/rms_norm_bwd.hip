@@ -41,14 +41,24 @@ __device__ __forceinline__ void put(const NormGradArgs& a, int64_t t, int64_t c,
     }
 }
 
-template <int FH, int FY, int FD, int T, int NV>
+// What a thread has loaded of a row.
+template <int FH, int FY, int FD, int NV>
+struct Loaded {
+    Eight<FH> h[NV];
+    Eight<FY> y[NV];
+    Eight<FD> r[NV];
+    float rstd;
+};
+
+// T threads of a row; AHEAD: the next row is on its way while one is worked on.
+template <int FH, int FY, int FD, int T, int NV, bool AHEAD>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGradArgs a) {
-    constexpr int kGroups = T < 256 ? 256 / T : 1;          // of a workgroup
-    __shared__ float red[2][T < 256 ? 1 : T / 64];
+    constexpr int kThreads = T < 256 ? 256 : T, kGroups = kThreads / T;
+    __shared__ float red[2][kThreads / 64];
     __shared__ float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? T * NV * 8 : 1];
     const int tid = threadIdx.x % T, sub = threadIdx.x / T;
     const int64_t t0 = ((int64_t)blockIdx.x * kGroups + sub) * a.share;
-    const int64_t t1 = t0 + a.share < a.T ? t0 + a.share : a.T;
+    const bool out = a.dx || a.dx8;
     float w[NV][8], dw[NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -60,53 +70,57 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGra
         }
         if (a.w && c < a.W) load_values8(a.w, a.w_format, c, a.W, w[v]);
     }
-    int turn = 0;
-    for (int64_t t = t0; t < t1; ++t) {
-        Eight<FH> eh[NV];
-        Eight<FY> ey[NV];
-        Eight<FD> er[NV];
-        const fmt_t<FH>* h = static_cast<const fmt_t<FH>*>(a.h) + t * a.h_ld;
-        const fmt_t<FY>* dy = static_cast<const fmt_t<FY>*>(a.dy) + t * a.dy_ld;
-        const fmt_t<FD>* dr = a.dr ? static_cast<const fmt_t<FD>*>(a.dr) + t * a.dr_ld : nullptr;
+    auto load = [&](int64_t t, Loaded<FH, FY, FD, NV>& x) {
+        // rows past the end, and columns: 0
+        x.rstd = t < a.T ? a.rstd[t] : 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int64_t c = (int64_t)(v * T + tid) * 8;
-            eh[v] = Eight<FH>{};
-            ey[v] = Eight<FY>{};
-            er[v] = Eight<FD>{};
-            if (c < a.W) {
-                eh[v] = load8<FH>(h, c, a.W);
-                ey[v] = load8<FY>(dy, c, a.W);
-                if (dr) er[v] = load8<FD>(dr, c, a.W);
+            x.h[v] = Eight<FH>{};
+            x.y[v] = Eight<FY>{};
+            x.r[v] = Eight<FD>{};
+            if (c < a.W && t < a.T) {
+                x.h[v] = load8<FH>(static_cast<const fmt_t<FH>*>(a.h) + t * a.h_ld, c, a.W);
+                x.y[v] = load8<FY>(static_cast<const fmt_t<FY>*>(a.dy) + t * a.dy_ld, c, a.W);
+                if (a.dr && out) x.r[v] = load8<FD>(static_cast<const fmt_t<FD>*>(a.dr) + t * a.dr_ld, c, a.W);
             }
         }
-        const float rstd = a.rstd[t];
+    };
+    Loaded<FH, FY, FD, NV> next;
+    if (AHEAD) load(t0, next);
+    for (int64_t i = 0; i < a.share; ++i) {                 // the same number for all groups
+        const int64_t t = t0 + i;
+        if (!AHEAD) load(t, next);
         float n[NV][8], g[NV][8], dot = 0.0f;
+        Eight<FD> r[NV];
+        const float rstd = next.rstd;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            values8<FH>(eh[v], n[v]);
-            values8<FY>(ey[v], g[v]);
+            values8<FH>(next.h[v], n[v]);
+            values8<FY>(next.y[v], g[v]);
+            r[v] = next.r[v];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                n[v][i] *= rstd;
-                dw[v][i] += g[v][i] * n[v][i];
-                g[v][i] *= w[v][i];
-                dot += g[v][i] * n[v][i];
+            for (int j = 0; j < 8; ++j) {
+                n[v][j] *= rstd;
+                dw[v][j] += g[v][j] * n[v][j];
+                g[v][j] *= w[v][j];
+                dot += g[v][j] * n[v][j];
             }
         }
-        const float m = row_reduce<T>(dot, red[turn], RowSum()) / (float)a.W;
-        turn ^= 1;
-        if (!a.dx && !a.dx8) continue;
+        if (AHEAD && i + 1 < a.share) load(t + 1, next);
+        if (!out) continue;
+        const float m = row_reduce<T>(dot, red[i & 1], RowSum()) / (float)a.W;
+        if (t >= a.T) continue;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int64_t c = (int64_t)(v * T + tid) * 8;
             if (c >= a.W) continue;
             float d[8];
-            values8<FD>(er[v], d);
+            values8<FD>(r[v], d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float own = rstd * (g[v][i] - n[v][i] * m);
-                d[i] = dr ? d[i] + own : own;
+            for (int j = 0; j < 8; ++j) {
+                const float own = rstd * (g[v][j] - n[v][j] * m);
+                d[j] = a.dr ? d[j] + own : own;
             }
             put<FD>(a, t, c, d);
         }
@@ -118,7 +132,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGra
 #pragma unroll
             for (int i = 0; i < 8; ++i) sums[sub][(v * T + tid) * 8 + i] = dw[v][i];
         __syncthreads();
-        for (int c = threadIdx.x; c < a.W; c += 256) {
+        for (int c = threadIdx.x; c < a.W; c += kThreads) {
             float s = sums[0][c];
 #pragma unroll
             for (int g = 1; g < kGroups; ++g) s += sums[g][c];
@@ -230,7 +244,8 @@ struct NormGradPlan {
     int64_t share, blocks;
 };
 NormGradPlan norm_grad_plan(int64_t T, int64_t W) {
-    const int64_t threads = W <= 64 * 16 ? 64 : W <= 256 * 16 ? 256 : 1024;
+    int64_t threads = 8;                                    // of a row: eight columns each
+    while (threads < 1024 && threads * 8 < W) threads *= 2;
     const int64_t groups = threads < 256 ? 256 / threads : 1;
     int64_t cus = device_cus();
     if (cus <= 0) cus = 256;
@@ -249,16 +264,19 @@ NormGradPlan norm_grad_plan(int64_t T, int64_t W) {
 
 template <int FH, int FY, int FD, int T, int NV>
 void launch_rows(const NormGradArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((rms_norm_bwd_kernel<FH, FY, FD, T, NV>), dim3((unsigned)a.blocks),
+    hipLaunchKernelGGL((rms_norm_bwd_kernel<FH, FY, FD, T, NV, NV == 1>), dim3((unsigned)a.blocks),
                        dim3(T < 256 ? 256 : T), 0, stream, a);
 }
 
 template <int FH, int FY, int FD>
 void launch(const NormGradArgs& a, hipStream_t stream) {
-    if (a.W <= 64 * 8) launch_rows<FH, FY, FD, 64, 1>(a, stream);
-    else if (a.W <= 64 * 16) launch_rows<FH, FY, FD, 64, 2>(a, stream);
+    if (a.W <= 8 * 8) launch_rows<FH, FY, FD, 8, 1>(a, stream);
+    else if (a.W <= 16 * 8) launch_rows<FH, FY, FD, 16, 1>(a, stream);
+    else if (a.W <= 32 * 8) launch_rows<FH, FY, FD, 32, 1>(a, stream);
+    else if (a.W <= 64 * 8) launch_rows<FH, FY, FD, 64, 1>(a, stream);
+    else if (a.W <= 128 * 8) launch_rows<FH, FY, FD, 128, 1>(a, stream);
     else if (a.W <= 256 * 8) launch_rows<FH, FY, FD, 256, 1>(a, stream);
-    else if (a.W <= 256 * 16) launch_rows<FH, FY, FD, 256, 2>(a, stream);
+    else if (a.W <= 512 * 8) launch_rows<FH, FY, FD, 512, 1>(a, stream);
     else if (a.W <= 1024 * 8) launch_rows<FH, FY, FD, 1024, 1>(a, stream);
     else if (a.W <= kWidest) launch_rows<FH, FY, FD, 1024, 2>(a, stream);
     else {

@@ -94,28 +94,74 @@ __device__ __forceinline__ void store_values8(void* row, int fmt, int64_t c, int
     else store_eight<FP8T_FMT_FP8>(static_cast<uint8_t*>(row) + c, n, x);
 }
 
-// A float as its nearest value in a stream's format.
+// Eight floats rounded to a stream's format: its codes, and x what they stand for.
 template <int FMT>
-__device__ __forceinline__ float through(float x) {
-    return FMT == FP8T_FMT_FP16 ? fp16_to_f32(f32_to_fp16_rn(x)) : x;
+__device__ __forceinline__ Eight<FMT> rounded8(float* x) {
+    Eight<FMT> e;
+    if constexpr (FMT == FP8T_FMT_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e.a[i] = x[i];
+            e.b[i] = x[4 + i];
+        }
+    } else {
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) top = maximum3_abs(top, x[i], x[i + 1]);
+        if (__builtin_expect(top < 0x1p31f, 1)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e.a[i] = fp16_pair(x[2 * i], x[2 * i + 1]);
+                const float2 p = fp16_finite_pair(e.a[i]);
+                x[2 * i] = p.x;
+                x[2 * i + 1] = p.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t lo = f32_to_fp16_rn(x[2 * i]), hi = f32_to_fp16_rn(x[2 * i + 1]);
+                e.a[i] = lo | (hi << 16);
+                x[2 * i] = fp16_to_f32(lo);
+                x[2 * i + 1] = fp16_to_f32(hi);
+            }
+        }
+    }
+    return e;
+}
+// n <= 8 stored elements (F32 or FP16) to p on.
+template <int FMT>
+__device__ __forceinline__ void store_stored8(fmt_t<FMT>* p, int n, const Eight<FMT>& e) {
+    if (n == 8) {
+        *reinterpret_cast<Eight<FMT>*>(p) = e;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= n) break;
+        if constexpr (FMT == FP8T_FMT_F32) p[i] = i < 4 ? e.a[i % 4] : e.b[i % 4];
+        else p[i] = (uint16_t)(e.a[i / 2] >> (16 * (i % 2)));
+    }
 }
 
 __device__ __forceinline__ int left8(int64_t c, int64_t W) {
     return W - c < 8 ? (int)(W - c) : 8;
 }
 
-// A reduction over the T threads of a row (T 64: a wave; else the workgroup),
-// every thread gets the same bits.  red: T / 64 floats, free before the call.
+// A reduction over the T threads of a row, T a power of two and rows beside each
+// other in the workgroup; every thread gets the same bits.  T up to 64 needs no
+// LDS; else red has a float for each wave of the workgroup, free before the
+// call, and all its threads call.
 template <int T, typename OP>
 __device__ __forceinline__ float row_reduce(float x, float* red, OP op) {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) x = op(x, __shfl_xor(x, d));
+    for (int d = (T < 64 ? T : 64) / 2; d; d >>= 1) x = op(x, __shfl_xor(x, d));
     if constexpr (T > 64) {
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
         __syncthreads();
-        x = red[0];
+        const float* mine = red + threadIdx.x / T * (T / 64);
+        x = mine[0];
 #pragma unroll
-        for (int i = 1; i < T / 64; ++i) x = op(x, red[i]);
+        for (int i = 1; i < T / 64; ++i) x = op(x, mine[i]);
     }
     return x;
 }

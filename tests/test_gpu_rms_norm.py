@@ -11,7 +11,7 @@ from tests.lm_util import check, value
 from tests.token_util import F8, F16, F32, TORCH, Wide, draw, gpu, replayed, rounded, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
-WIDTHS = [1, 7, 8, 9, 64, 511, 512, 513, 1000, 1024, 1025, 2048, 2049, 4096, 4099, 8192, 8200, 16384,
+WIDTHS = [1, 7, 8, 9, 64, 65, 128, 129, 200, 256, 257, 511, 512, 513, 1000, 1024, 1025, 2048, 2049, 4096, 4099, 8192, 8200, 16384,
           16385, 40003]
 
 
@@ -203,7 +203,7 @@ def test_gradient_widths_and_addresses(W):
         bwd(h, w, inverse_rms(h), dy, None, F16, pad=2, shift=1)
 
 
-@pytest.mark.parametrize("T,W", [(0, 40), (3, 40), (1023, 40), (5000, 9), (5003, 600), (1500, 2100),
+@pytest.mark.parametrize("T,W", [(0, 40), (3, 40), (1023, 40), (5000, 9), (3001, 100), (3001, 250), (5003, 600), (1500, 2100),
                                  (700, 5000), (300, 9000), (200, 17000)])
 def test_gradient_many_rows(T, W):
     rng = np.random.default_rng(69)
