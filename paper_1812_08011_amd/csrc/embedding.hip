@@ -32,13 +32,14 @@ struct EmbedArgs {
     int64_t T, V, W, t_ld, y_ld;
     float scale;
     int log_lanes;                     // lanes of a row: 1 << log_lanes, each with eight columns at a time
+    bool stream;                       // results past the caches
 };
 
 template <int FT, int FY>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
     constexpr int kRows = 4;
-    const int lanes = 1 << a.log_lanes, per = kThreads >> a.log_lanes;
-    const int64_t c0 = (int64_t)(threadIdx.x & (lanes - 1)) * 8;
+    constexpr bool kFours = FT == FP8T_FMT_F32 || FY == FP8T_FMT_F32;
+    const int lanes = 1 << a.log_lanes, per = kThreads >> a.log_lanes, lane = threadIdx.x & (lanes - 1);
     const int64_t step = (int64_t)gridDim.x * per * kRows;
     for (int64_t t0 = (int64_t)blockIdx.x * per * kRows + (threadIdx.x >> a.log_lanes); t0 < a.T; t0 += step) {
         int64_t tok[kRows];
@@ -47,7 +48,9 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
             const int64_t t = t0 + r * per;
             tok[r] = t < a.T ? a.tokens[t] : -1;
         }
-        for (int64_t c = c0; c < a.W; c += 8 * lanes) {
+        for (int64_t u = 0; u * 8 * lanes < a.W; ++u) {
+            const Cols<kFours> c(u, lane, lanes);
+            if (!c.any(a.W)) break;
             Eight<FT> e[kRows] = {};
 #pragma unroll
             for (int r = 0; r < kRows; ++r)
@@ -62,7 +65,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
                 const bool used = (uint64_t)tok[r] < (uint64_t)a.V;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = used ? x[i] * a.scale : 0.0f;
-                store_eight<FY>(static_cast<fmt_t<FY>*>(a.y) + t * a.y_ld + c, left8(c, a.W), x);
+                put8<FY>(static_cast<fmt_t<FY>*>(a.y) + t * a.y_ld, c, a.W, x, a.stream);
             }
         }
     }
@@ -104,6 +107,7 @@ struct GradArgs {
     int* start;                        // V + 1: a row's first sorted token
     int2* list;                        // T: (token, position), sorted
     float* parts;                      // pieces x 2 x W: sums of cut runs
+    bool stream;                       // results past the caches
 };
 
 __global__ __launch_bounds__(kIndexThreads) void embed_index_kernel(GradArgs a) {
@@ -212,16 +216,17 @@ __global__ __launch_bounds__(kIndexThreads) void embed_index_kernel(GradArgs a) 
     }
 }
 
-template <int FG>
-__device__ __forceinline__ void grad_out(const GradArgs& a, int64_t v, int64_t c, const float* sum) {
+template <int FG, bool FOURS>
+__device__ __forceinline__ void grad_out(const GradArgs& a, int64_t v, const Cols<FOURS>& c, const float* sum) {
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = sum[i] * a.scale;
-    store_eight<FG>(static_cast<fmt_t<FG>*>(a.g) + v * a.g_ld + c, left8(c, a.W), y);
+    put8<FG>(static_cast<fmt_t<FG>*>(a.g) + v * a.g_ld, c, a.W, y, a.stream);
 }
 
 template <int FE, int FG>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
+    constexpr bool kFours = FE == FP8T_FMT_F32 || FG == FP8T_FMT_F32;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (block >= a.piece_blocks) {
         // rows without a token: among kZeroRows a wave
@@ -234,15 +239,17 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
         while (todo) {
             const int64_t at = v0 + __ffsll((unsigned long long)todo) - 1;
             todo &= todo - 1;
-            for (int64_t c = lane * 8; c < a.W; c += 512)
-                store_eight<FG>(static_cast<fmt_t<FG>*>(a.g) + at * a.g_ld + c, left8(c, a.W), zero);
+            for (int64_t u = 0; u * 512 < a.W; ++u) {
+                const Cols<kFours> c(u, lane, 64);
+                if (c.any(a.W)) put8<FG>(static_cast<fmt_t<FG>*>(a.g) + at * a.g_ld, c, a.W, zero, a.stream);
+            }
         }
         return;
     }
     const int per = kThreads >> a.log_lanes, group = threadIdx.x >> a.log_lanes;
     const int lane = threadIdx.x & ((1 << a.log_lanes) - 1);
     const int64_t p = block / a.slabs;
-    const int64_t c = ((block % a.slabs << a.log_lanes) + lane) * 8;
+    const Cols<kFours> c(block % a.slabs, lane, 1 << a.log_lanes);
     const int n = a.start[a.V];
     if (p * a.piece >= n) return;
     // what a group leaves of cut runs: [0] of one that began before its share,
@@ -252,8 +259,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
     const int from = (int)p * a.piece + group * kShare, to = from + kShare < n ? from + kShare : n;
     if (lane == 0) left[0][group] = left[1][group] = -1;
     if (from < n) {
-        const fmt_t<FE>* e = static_cast<const fmt_t<FE>*>(a.e) + c;
-        const int64_t room = a.W - c;                       // <= 0: columns past the row's end
+        const fmt_t<FE>* e = static_cast<const fmt_t<FE>*>(a.e);
+        const bool mine = c.any(a.W);                       // not past the row's end
         const int head = a.list[from].x, tail = a.list[to - 1].x;
         const int head_begin = a.start[head], head_end = a.start[head + 1];
         const int tail_begin = a.start[tail], tail_end = a.start[tail + 1];
@@ -271,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
                 const int at = v == head && cut_head ? 0 : 1;
                 part[at][0][threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
                 part[at][1][threadIdx.x] = make_float4(sum[4], sum[5], sum[6], sum[7]);
-            } else if (room > 0) {
+            } else if (mine) {
                 grad_out<FG>(a, v, c, sum);
             }
         };
@@ -285,7 +292,7 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 tok[u] = next[u].x;
-                if (j + u < last && room > 0) x[u] = load8<FE>(e + (int64_t)next[u].y * a.e_ld, 0, room);
+                if (j + u < last && mine) x[u] = load8<FE>(e + (int64_t)next[u].y * a.e_ld, c, a.W);
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
@@ -310,14 +317,14 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
     __syncthreads();
     // the first group joins the parts of cut runs in their order; a run that
     // began before the piece or goes on behind it leaves a part of its own
-    if (group > 0 || c >= a.W) return;
+    if (group > 0 || !c.any(a.W)) return;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     int v = -1;
     bool inside = false;                                    // the run began in this piece
     auto done = [&](bool more) {
         if (v < 0) return;
         if (inside && !more) grad_out<FG>(a, v, c, sum);
-        else store_some<FP8T_FMT_F32>(a.parts + (p * 2 + inside) * a.W + c, left8(c, a.W), sum);
+        else put8<FP8T_FMT_F32>(a.parts + (p * 2 + inside) * a.W, c, a.W, sum, false);
     };
     for (int g = 0; g < per; ++g)
 #pragma unroll
@@ -351,9 +358,9 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(GradArgs a) {
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int64_t unit = block * per + (threadIdx.x >> a.log_lanes);
     const int64_t p = unit / a.slabs;
-    const int64_t c = ((unit % a.slabs) * lanes + (threadIdx.x & (lanes - 1))) * 8;
+    const Cols<true> c(unit % a.slabs, threadIdx.x & (lanes - 1), lanes);
     const int n = a.start[a.V];
-    if ((p + 1) * a.piece >= n || c >= a.W) return;
+    if ((p + 1) * a.piece >= n || !c.any(a.W)) return;
     const int v = a.list[(p + 1) * a.piece - 1].x, begin = a.start[v], end = a.start[v + 1];
     if (begin < p * a.piece || end <= (p + 1) * a.piece || end - begin <= kLong) return;
     const int64_t last = (end - 1) / a.piece;
@@ -459,6 +466,7 @@ extern "C" int embed_fwd(const int64_t* tokens, int64_t T, const void* table, in
     a.y_ld = y_ld;
     a.scale = scale;
     a.log_lanes = log_lanes(W, kThreads);
+    a.stream = T * W * bytes_of(y_format) > kStreamBytes;
     FP8T_BY_FORMATS(launch_fwd, table_format, y_format, a, stream)
     return launch_status();
 }
@@ -490,6 +498,7 @@ extern "C" int embed_bwd(const int64_t* tokens, int64_t T, const void* e, int e_
     a.e_ld = e_ld;
     a.g_ld = g_ld;
     a.scale = scale;
+    a.stream = V * W * bytes_of(g_format) > kStreamBytes;
     a.R = p.R;
     a.log_lanes = p.log_lanes;
     a.slabs = p.slabs;

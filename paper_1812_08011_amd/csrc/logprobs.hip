@@ -754,12 +754,14 @@ struct LogprobGradArgs {
     int64_t z_ld, g_ld, N;
     int V, m, chunks;                  // chunks of a row
     float tau, to2, scale;             // scale = grad_scale / tau
+    bool stream;                       // results past the caches
 };
 
 // HBM-bound and without sums over the row: a workgroup owns a chunk of one.
 template <int FZ, int FG>
 __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradArgs a) {
     constexpr int kUnits = 4;
+    constexpr bool kFours = FZ == FP8T_FMT_F32 || FG == FP8T_FMT_F32;
     extern __shared__ float given[];                        // [m] d_logp, tokens, their logits
     __shared__ float red[kGradThreads / 64];
     int* at = reinterpret_cast<int*>(given + a.m);
@@ -775,8 +777,8 @@ __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradAr
     Eight<FZ> e[kUnits];
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-        const int v = v0 + (u * kGradThreads + tid) * 8;
-        if (v < v1) e[u] = load_logits<FZ>(z, v, v1);
+        const Cols<kFours> c(u, tid, kGradThreads);
+        if (c.any(v1 - v0)) e[u] = load8<FZ>(z + v0, c, v1 - v0);
     }
     const float top = a.stats[2 * n], ls = a.stats[2 * n + 1];
     const float dh = a.d_entropy ? a.d_entropy[n] : 0.0f;
@@ -810,14 +812,14 @@ __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradAr
     };
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-        const int v = v0 + (u * kGradThreads + tid) * 8;
-        if (v >= v1) break;
+        const Cols<kFours> c(u, tid, kGradThreads);
+        if (!c.any(v1 - v0)) break;
         float x[8];
         Raw<FZ>::values(e[u], x);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             x[i] = some ? gradient(FZ == FP8T_FMT_F32 ? x[i] - m : __builtin_fmaf(x[i], Raw<FZ>::kUnit, -m)) : 0.0f;
-        store_eight<FG>(g + v, left8(v, v1), x);
+        put8<FG>(g + v0, c, v1 - v0, x, a.stream);
     }
     if (a.m == 0 || !some) return;
     // the given tokens of this chunk, each with the sum of its occurrences, by
@@ -928,6 +930,7 @@ extern "C" int token_logprobs_bwd(const void* z, int z_format, int64_t z_ld, con
     a.tau = tau;
     a.to2 = kLog2e / tau;
     a.scale = grad_scale / tau;
+    a.stream = N * V * bytes_of(g_format) > kStreamBytes;
     if (z_format == FP8T_FMT_F32) {
         if (g_format == FP8T_FMT_F32) launch_bwd<FP8T_FMT_F32, FP8T_FMT_F32>(a, stream);
         else if (g_format == FP8T_FMT_FP16) launch_bwd<FP8T_FMT_F32, FP8T_FMT_FP16>(a, stream);

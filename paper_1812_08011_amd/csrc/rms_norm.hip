@@ -23,6 +23,7 @@ struct NormArgs {
     int64_t x_ld, r_ld, h_ld, y_ld, T, W;
     int w_format, y_format;
     bool sum;                          // u is rounded to the stream's format
+    bool stream_h, stream_y;           // results past the caches
     float eps, y_scale;
 };
 
@@ -43,6 +44,8 @@ __device__ __forceinline__ float row_scale(float top, float y_scale) {
 
 template <int FX, int FS>
 struct NormRow {
+    static constexpr bool kFours = FX == FP8T_FMT_F32 || FS == FP8T_FMT_F32;
+    using C = Cols<kFours>;
     const NormArgs& a;
     const fmt_t<FX>* x;
     const fmt_t<FS>* r;
@@ -55,11 +58,11 @@ struct NormRow {
         div = a.x_row_scale ? a.x_row_scale[t] : 1.0f;
     }
     // u of elements c .. c + 7 from what was loaded; written to h
-    __device__ __forceinline__ void sum(const Eight<FX>& ex, const Eight<FS>& er, int64_t c, float* u) const {
+    __device__ __forceinline__ void sum(const Eight<FX>& ex, const Eight<FS>& er, const C& c, float* u) const {
         values8<FX>(ex, u);
         if (a.x_row_scale) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = c + i < a.W ? u[i] / div : 0.0f;
+            for (int i = 0; i < 8; ++i) u[i] = c.has(i, a.W) ? u[i] / div : 0.0f;
         }
         if (r) {
             float v[8];
@@ -69,10 +72,10 @@ struct NormRow {
         }
         if (a.sum) {
             const Eight<FS> e = rounded8<FS>(u);
-            if (h && c < a.W) store_stored8<FS>(h + c, left8(c, a.W), e);
+            if (h && c.any(a.W)) store8<FS>(h, c, a.W, e, a.stream_h);
         }
     }
-    __device__ __forceinline__ Eight<FS> residual(int64_t c) const {
+    __device__ __forceinline__ Eight<FS> residual(const C& c) const {
         return r ? load8<FS>(r, c, a.W) : Eight<FS>{};
     }
 };
@@ -86,6 +89,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
     const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + threadIdx.x / T;
     if (t >= a.T) return;                                   // all threads of a row
     const NormRow<FX, FS> row(a, t);
+    using C = typename NormRow<FX, FS>::C;
+    const int64_t units = (a.W + 8 * T - 1) / (8 * T);      // of a wide row
     float u[NV ? NV : 1][8], w[NV ? NV : 1][8];
     float ss = 0.0f;
     if constexpr (NV > 0) {
@@ -93,37 +98,39 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
         Eight<FS> er[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * T + tid) * 8;
+            const C c(v, tid, T);
             ex[v] = Eight<FX>{};
             er[v] = Eight<FS>{};
-            if (c < a.W) {
+            if (c.any(a.W)) {
                 ex[v] = load8<FX>(row.x, c, a.W);
                 er[v] = row.residual(c);
             }
         }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * T + tid) * 8;
+            const C c(v, tid, T);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[v][i] = 1.0f;
-            if (a.w && c < a.W) load_values8(a.w, a.w_format, c, a.W, w[v]);
+            if (a.w && c.any(a.W)) load_values8(a.w, a.w_format, c, a.W, w[v]);
         }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * T + tid) * 8;
+            const C c(v, tid, T);
             row.sum(ex[v], er[v], c, u[v]);                 // 0 past the row's end
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss += u[v][i] * u[v][i];
         }
     } else {
-        for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
+        for (int64_t v = 0; v < units; ++v) {
+            const C c(v, tid, T);
+            if (!c.any(a.W)) break;
             row.sum(load8<FX>(row.x, c, a.W), row.residual(c), c, u[0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss += u[0][i] * u[0][i];
         }
     }
     // u of a wide row once more: h may have taken r's or x's place
-    auto reload = [&](int64_t c, float* v) {
+    auto reload = [&](const C& c, float* v) {
         if (row.h) values8<FS>(load8<FS>(row.h, c, a.W), v);
         else row.sum(load8<FX>(row.x, c, a.W), row.residual(c), c, v);
     };
@@ -138,7 +145,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
 #pragma unroll
             for (int v = 0; v < NV; ++v) add(u[v]);
         } else {
-            for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
+            for (int64_t v = 0; v < units; ++v) {
+                const C c(v, tid, T);
+                if (!c.any(a.W)) break;
                 reload(c, u[0]);
                 add(u[0]);
             }
@@ -152,7 +161,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * wv[i];
     };
-    auto weights = [&](int64_t c, float* wv) {
+    auto weights = [&](const C& c, float* wv) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) wv[i] = 1.0f;
         if (a.w) load_values8(a.w, a.w_format, c, a.W, wv);
@@ -171,7 +180,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
 #pragma unroll
             for (int v = 0; v < NV; ++v) most(u[v]);
         } else {
-            for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
+            for (int64_t v = 0; v < units; ++v) {
+                const C c(v, tid, T);
+                if (!c.any(a.W)) break;
                 reload(c, u[0]);
                 weights(c, w[0]);
                 norm(u[0], w[0]);
@@ -184,19 +195,21 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
     }
     uint8_t* y = static_cast<uint8_t*>(a.y) +
                  t * a.y_ld * (a.y_format == FP8T_FMT_F32 ? 4 : a.y_format == FP8T_FMT_FP16 ? 2 : 1);
-    auto out = [&](int64_t c, float* v) {
+    auto out = [&](const C& c, float* v) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= scale;
-        store_values8(y, a.y_format, c, left8(c, a.W), v);
+        put_as8(y, a.y_format, c, a.W, v, a.stream_y);
     };
     if constexpr (NV > 0) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * T + tid) * 8;
-            if (c < a.W) out(c, u[v]);
+            const C c(v, tid, T);
+            if (c.any(a.W)) out(c, u[v]);
         }
     } else {
-        for (int64_t c = (int64_t)tid * 8; c < a.W; c += T * 8) {
+        for (int64_t v = 0; v < units; ++v) {
+            const C c(v, tid, T);
+            if (!c.any(a.W)) break;
             reload(c, u[0]);
             weights(c, w[0]);
             norm(u[0], w[0]);
@@ -265,6 +278,8 @@ extern "C" int rms_norm_fwd(const void* x, int x_format, int64_t x_ld, const flo
     a.w_format = w_format;
     a.y_format = y_format;
     a.sum = r || h;
+    a.stream_h = W <= kWidest && T * W * bytes_of(s_format) > kStreamBytes;   // wide rows are read again
+    a.stream_y = T * W * bytes_of(y_format) > kStreamBytes;
     a.eps = eps;
     a.y_scale = y_scale;
     const bool f32 = s_format == FP8T_FMT_F32;

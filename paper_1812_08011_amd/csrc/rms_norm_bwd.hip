@@ -28,18 +28,20 @@ struct NormGradArgs {
     int64_t share, blocks;             // rows of a group of T threads; workgroups
     int w_format;
     float dx8_scale;
+    bool stream, stream8;              // dx, dx8 past the caches
 };
 
-template <int FD>
-__device__ __forceinline__ void put(const NormGradArgs& a, int64_t t, int64_t c, float* d) {
-    const int n = left8(c, a.W);
-    if (a.dx) store_some<FD>(static_cast<fmt_t<FD>*>(a.dx) + t * a.dx_ld + c, n, d);
+template <int FD, bool FOURS>
+__device__ __forceinline__ void put(const NormGradArgs& a, int64_t t, const Cols<FOURS>& c, float* d) {
+    if (a.dx) put8<FD>(static_cast<fmt_t<FD>*>(a.dx) + t * a.dx_ld, c, a.W, d, a.stream);
     if (a.dx8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] *= a.dx8_scale;
-        store_eight<FP8T_FMT_FP8>(a.dx8 + t * a.dx8_ld + c, n, d);
+        put8<FP8T_FMT_FP8>(a.dx8 + t * a.dx8_ld, c, a.W, d, a.stream8);
     }
 }
+template <int FH, int FY, int FD>
+constexpr bool kFours = FH == FP8T_FMT_F32 || FY == FP8T_FMT_F32 || FD == FP8T_FMT_F32;
 
 // What a thread has loaded of a row.
 template <int FH, int FY, int FD, int NV>
@@ -54,6 +56,7 @@ struct Loaded {
 template <int FH, int FY, int FD, int T, int NV, bool AHEAD>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGradArgs a) {
     constexpr int kThreads = T < 256 ? 256 : T, kGroups = kThreads / T;
+    using C = Cols<kFours<FH, FY, FD>>;
     __shared__ float red[2][kThreads / 64];
     __shared__ float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? T * NV * 8 : 1];
     const int tid = threadIdx.x % T, sub = threadIdx.x / T;
@@ -62,24 +65,24 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGra
     float w[NV][8], dw[NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int64_t c = (int64_t)(v * T + tid) * 8;
+        const C c(v, tid, T);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             w[v][i] = 1.0f;
             dw[v][i] = 0.0f;
         }
-        if (a.w && c < a.W) load_values8(a.w, a.w_format, c, a.W, w[v]);
+        if (a.w && c.any(a.W)) load_values8(a.w, a.w_format, c, a.W, w[v]);
     }
     auto load = [&](int64_t t, Loaded<FH, FY, FD, NV>& x) {
         // rows past the end, and columns: 0
         x.rstd = t < a.T ? a.rstd[t] : 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * T + tid) * 8;
+            const C c(v, tid, T);
             x.h[v] = Eight<FH>{};
             x.y[v] = Eight<FY>{};
             x.r[v] = Eight<FD>{};
-            if (c < a.W && t < a.T) {
+            if (c.any(a.W) && t < a.T) {
                 x.h[v] = load8<FH>(static_cast<const fmt_t<FH>*>(a.h) + t * a.h_ld, c, a.W);
                 x.y[v] = load8<FY>(static_cast<const fmt_t<FY>*>(a.dy) + t * a.dy_ld, c, a.W);
                 if (a.dr && out) x.r[v] = load8<FD>(static_cast<const fmt_t<FD>*>(a.dr) + t * a.dr_ld, c, a.W);
@@ -113,8 +116,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGra
         if (t >= a.T) continue;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * T + tid) * 8;
-            if (c >= a.W) continue;
+            const C c(v, tid, T);
+            if (!c.any(a.W)) continue;
             float d[8];
             values8<FD>(r[v], d);
 #pragma unroll
@@ -130,7 +133,10 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGra
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sums[sub][(v * T + tid) * 8 + i] = dw[v][i];
+            for (int i = 0; i < 8; ++i) {
+                const C c(v, tid, T);
+                sums[sub][i < 4 ? c.a + i : c.b + i - 4] = dw[v][i];
+            }
         __syncthreads();
         for (int c = threadIdx.x; c < a.W; c += kThreads) {
             float s = sums[0][c];
@@ -141,9 +147,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGra
     } else {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * T + tid) * 8;
-            if (c < a.W)
-                store_some<FP8T_FMT_F32>(a.parts + (int64_t)blockIdx.x * a.W + c, left8(c, a.W), dw[v]);
+            const C c(v, tid, T);
+            if (c.any(a.W)) put8<FP8T_FMT_F32>(a.parts + (int64_t)blockIdx.x * a.W, c, a.W, dw[v], false);
         }
     }
 }
@@ -159,7 +164,9 @@ __global__ __launch_bounds__(1024) void rms_norm_bwd_wide_kernel(NormGradArgs a)
     const fmt_t<FD>* dr = a.dr ? static_cast<const fmt_t<FD>*>(a.dr) + t * a.dr_ld : nullptr;
     const float rstd = a.rstd[t];
     float n[8], g[8], w[8], dot = 0.0f;
-    auto load = [&](int64_t c) {
+    using C = Cols<kFours<FH, FY, FD>>;
+    const int64_t units = (a.W + 8191) / 8192;
+    auto load = [&](const C& c) {
         values8<FH>(load8<FH>(h, c, a.W), n);
         values8<FY>(load8<FY>(dy, c, a.W), g);
 #pragma unroll
@@ -171,13 +178,17 @@ __global__ __launch_bounds__(1024) void rms_norm_bwd_wide_kernel(NormGradArgs a)
             g[i] *= w[i];
         }
     };
-    for (int64_t c = (int64_t)threadIdx.x * 8; c < a.W; c += 8192) {
+    for (int64_t v = 0; v < units; ++v) {
+        const C c(v, threadIdx.x, 1024);
+        if (!c.any(a.W)) break;
         load(c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dot += g[i] * n[i];
     }
     const float m = row_reduce<1024>(dot, red, RowSum()) / (float)a.W;
-    for (int64_t c = (int64_t)threadIdx.x * 8; c < a.W; c += 8192) {
+    for (int64_t v = 0; v < units; ++v) {
+        const C c(v, threadIdx.x, 1024);
+        if (!c.any(a.W)) break;
         load(c);
         float d[8];
         if (dr) values8<FD>(load8<FD>(dr, c, a.W), d);
@@ -193,8 +204,8 @@ __global__ __launch_bounds__(1024) void rms_norm_bwd_wide_kernel(NormGradArgs a)
 // dw of wide rows: a thread owns eight columns and a range of rows.
 template <int FH, int FY>
 __global__ __launch_bounds__(kDwThreads) void rms_norm_dw_kernel(NormGradArgs a) {
-    const int64_t c = ((int64_t)blockIdx.x * kDwThreads + threadIdx.x) * 8;
-    if (c >= a.W) return;
+    const Cols<FH == FP8T_FMT_F32 || FY == FP8T_FMT_F32> c(blockIdx.x, threadIdx.x, kDwThreads);
+    if (!c.any(a.W)) return;
     const int64_t t0 = blockIdx.y * a.share, t1 = t0 + a.share < a.T ? t0 + a.share : a.T;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int64_t t = t0; t < t1; ++t) {
@@ -205,7 +216,7 @@ __global__ __launch_bounds__(kDwThreads) void rms_norm_dw_kernel(NormGradArgs a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += g[i] * (n[i] * rstd);
     }
-    store_some<FP8T_FMT_F32>(a.parts + blockIdx.y * a.W + c, left8(c, a.W), sum);
+    put8<FP8T_FMT_F32>(a.parts + blockIdx.y * a.W, c, a.W, sum, false);
 }
 
 // dw = the sum of the workgroups' rows: a lane owns a column, each wave a range
@@ -352,6 +363,8 @@ extern "C" int rms_norm_bwd(const void* h, int h_format, int64_t h_ld, const voi
     a.blocks = p.blocks;
     a.w_format = w_format;
     a.dx8_scale = dx8_scale;
+    a.stream = T * W * bytes_of(d_format) > kStreamBytes;
+    a.stream8 = T * W > kStreamBytes;
     if (T > 0) {
         const bool f32 = d_format == FP8T_FMT_F32;
         if (h_format == FP8T_FMT_F32) {

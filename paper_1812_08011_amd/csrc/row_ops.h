@@ -7,35 +7,115 @@
 
 namespace fp8t {
 
-// Elements c .. c + 7 of a row of W as they are stored, 0 past its end.
-template <int FMT>
-__device__ __forceinline__ Eight<FMT> load8(const fmt_t<FMT>* row, int64_t c, int64_t W) {
-    if (c + 8 <= W) return *reinterpret_cast<const Eight<FMT>*>(row + c);
-    Eight<FMT> e;
-    if constexpr (FMT == FP8T_FMT_F32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            e.a[i] = c + i < W ? row[c + i] : 0.0f;
-            e.b[i] = c + 4 + i < W ? row[c + 4 + i] : 0.0f;
-        }
-    } else if constexpr (FMT == FP8T_FMT_FP16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = c + 2 * i < W ? row[c + 2 * i] : 0;
-            const uint32_t hi = c + 2 * i + 1 < W ? row[c + 2 * i + 1] : 0;
-            e.a[i] = lo | (hi << 16);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t w = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c + 4 * i + j < W) w |= (uint32_t)row[c + 4 * i + j] << (8 * j);
-            e.a[i] = w;
-        }
+// The eight columns of a row that a thread holds: two fours, beside each other
+// or (FOURS) apart by the fours of the row's other threads.  Where floats are
+// stored they are apart, so that a wave's 16 bytes a lane are whole lines: 16384
+// x 2048 floats written in 42 us with eights, in 27 with fours (past the caches;
+// 36 through them).  Codes alone move as eights.
+template <bool FOURS>
+struct Cols {
+    int64_t a, b;
+    // unit u of thread tid of T
+    __device__ __forceinline__ Cols(int64_t u, int tid, int T) {
+        a = FOURS ? (u * 2 * T + tid) * 4 : (u * T + tid) * 8;
+        b = FOURS ? a + 4 * (int64_t)T : a + 4;
     }
+    __device__ __forceinline__ bool any(int64_t W) const { return a < W; }
+    __device__ __forceinline__ bool has(int i, int64_t W) const { return (i < 4 ? a + i : b + i - 4) < W; }
+};
+
+// Four consecutive elements at any address.
+template <int FMT>
+struct FourOf;
+template <>
+struct FourOf<FP8T_FMT_F32> { typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
+template <>
+struct FourOf<FP8T_FMT_FP16> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2))); };
+template <>
+struct FourOf<FP8T_FMT_FP8> { typedef uint32_t type __attribute__((aligned(1))); };
+
+// Four h (0 or 1) of eight stored elements.
+template <int FMT>
+__device__ __forceinline__ typename FourOf<FMT>::type four_of(const Eight<FMT>& e, int h) {
+    if constexpr (FMT == FP8T_FMT_F32) return h ? e.b : e.a;
+    else if constexpr (FMT == FP8T_FMT_FP16) return typename FourOf<FMT>::type{e.a[2 * h], e.a[2 * h + 1]};
+    else return e.a[h];
+}
+template <int FMT>
+__device__ __forceinline__ void set_four(Eight<FMT>& e, int h, const typename FourOf<FMT>::type& f) {
+    if constexpr (FMT == FP8T_FMT_F32) (h ? e.b : e.a) = f;
+    else if constexpr (FMT == FP8T_FMT_FP16) {
+        e.a[2 * h] = f[0];
+        e.a[2 * h + 1] = f[1];
+    } else e.a[h] = f;
+}
+// Element i of eight stored ones.
+template <int FMT>
+__device__ __forceinline__ fmt_t<FMT> element_of(const Eight<FMT>& e, int i) {
+    if constexpr (FMT == FP8T_FMT_F32) return i < 4 ? e.a[i % 4] : e.b[i % 4];
+    else if constexpr (FMT == FP8T_FMT_FP16) return (uint16_t)(e.a[i / 2] >> (16 * (i % 2)));
+    else return (uint8_t)(e.a[i / 4] >> (8 * (i % 4)));
+}
+template <int FMT>
+__device__ __forceinline__ void set_element(Eight<FMT>& e, int i, fmt_t<FMT> x) {
+    if constexpr (FMT == FP8T_FMT_F32) (i < 4 ? e.a : e.b)[i % 4] = x;
+    else if constexpr (FMT == FP8T_FMT_FP16) e.a[i / 2] |= (uint32_t)x << (16 * (i % 2));
+    else e.a[i / 4] |= (uint32_t)x << (8 * (i % 4));
+}
+
+// A row's elements as they are stored, 0 past its end.
+template <int FMT, bool FOURS>
+__device__ __forceinline__ Eight<FMT> load8(const fmt_t<FMT>* row, const Cols<FOURS>& c, int64_t W) {
+    if (c.b + 4 <= W) {
+        if constexpr (!FOURS) return *reinterpret_cast<const Eight<FMT>*>(row + c.a);
+        Eight<FMT> e;
+        set_four<FMT>(e, 0, *reinterpret_cast<const typename FourOf<FMT>::type*>(row + c.a));
+        set_four<FMT>(e, 1, *reinterpret_cast<const typename FourOf<FMT>::type*>(row + c.b));
+        return e;
+    }
+    Eight<FMT> e = {};
+    if (FOURS && c.a + 4 <= W) {                            // a row's last fours
+        set_four<FMT>(e, 0, *reinterpret_cast<const typename FourOf<FMT>::type*>(row + c.a));
+#pragma unroll
+        for (int i = 4; i < 8; ++i)
+            if (c.b + i - 4 < W) set_element<FMT>(e, i, row[c.b + i - 4]);
+        return e;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c.has(i, W)) set_element<FMT>(e, i, row[i < 4 ? c.a + i : c.b + i - 4]);
     return e;
+}
+
+// Results past what the caches hold are stored past them (`stream`): what they
+// push out there may be wanted, they will not be found there.
+constexpr int64_t kStreamBytes = 32 << 20;
+template <typename V>
+__device__ __forceinline__ void put_vector(V* p, const V& v, bool stream) {
+    if (stream) {
+        asm volatile("; past the caches");                  // or the two stores become one plain one
+        __builtin_nontemporal_store(v, p);
+        asm volatile("; past the caches");
+    } else {
+        *p = v;
+    }
+}
+template <int FMT, bool FOURS>
+__device__ __forceinline__ void store8(fmt_t<FMT>* row, const Cols<FOURS>& c, int64_t W, const Eight<FMT>& e,
+                                       bool stream) {
+    using Four = typename FourOf<FMT>::type;
+    if (c.b + 4 <= W) {
+        if constexpr (FOURS || FMT == FP8T_FMT_F32) {
+            put_vector(reinterpret_cast<Four*>(row + c.a), four_of<FMT>(e, 0), stream);
+            put_vector(reinterpret_cast<Four*>(row + c.b), four_of<FMT>(e, 1), stream);
+        } else {
+            put_vector(reinterpret_cast<decltype(e.a)*>(row + c.a), e.a, stream);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c.has(i, W)) row[i < 4 ? c.a + i : c.b + i - 4] = element_of<FMT>(e, i);
 }
 
 template <int FMT>
@@ -58,45 +138,17 @@ __device__ __forceinline__ void values8(const Eight<FMT>& e, float* x) {
 }
 
 // Eight values of a row in a format that is known at run time only (uniform).
-__device__ __forceinline__ void load_values8(const void* row, int fmt, int64_t c, int64_t W, float* x) {
+template <bool FOURS>
+__device__ __forceinline__ void load_values8(const void* row, int fmt, const Cols<FOURS>& c, int64_t W, float* x) {
     if (fmt == FP8T_FMT_F32)
         values8<FP8T_FMT_F32>(load8<FP8T_FMT_F32>(static_cast<const float*>(row), c, W), x);
     else
         values8<FP8T_FMT_FP16>(load8<FP8T_FMT_FP16>(static_cast<const uint16_t*>(row), c, W), x);
 }
 
-// n <= 8 results to p on; eight FP8 results that need no saturation and are no
-// NaN, as nearly always, in four instructions.
+// Eight floats as a format stores them.
 template <int FMT>
-__device__ __forceinline__ void store_eight(fmt_t<FMT>* p, int n, const float* x) {
-    if constexpr (FMT == FP8T_FMT_FP8) {
-        float top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) top = maximum3_abs(top, x[i], x[i + 1]);
-        if (__builtin_expect(n == 8 && top <= 57344.0f, 1)) {
-            Eight<FMT> e;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t w = __builtin_amdgcn_cvt_pk_bf8_f32(x[4 * i], x[4 * i + 1], 0, false);
-                e.a[i] = __builtin_amdgcn_cvt_pk_bf8_f32(x[4 * i + 2], x[4 * i + 3], w, true);
-            }
-            *reinterpret_cast<Eight<FMT>*>(p) = e;
-            return;
-        }
-    }
-    store_some<FMT>(p, n, x);
-}
-
-// n <= 8 results (n > 0) to elements c .. of a row.
-__device__ __forceinline__ void store_values8(void* row, int fmt, int64_t c, int n, const float* x) {
-    if (fmt == FP8T_FMT_F32) store_some<FP8T_FMT_F32>(static_cast<float*>(row) + c, n, x);
-    else if (fmt == FP8T_FMT_FP16) store_some<FP8T_FMT_FP16>(static_cast<uint16_t*>(row) + c, n, x);
-    else store_eight<FP8T_FMT_FP8>(static_cast<uint8_t*>(row) + c, n, x);
-}
-
-// Eight floats rounded to a stream's format: its codes, and x what they stand for.
-template <int FMT>
-__device__ __forceinline__ Eight<FMT> rounded8(float* x) {
+__device__ __forceinline__ Eight<FMT> codes8(const float* x) {
     Eight<FMT> e;
     if constexpr (FMT == FP8T_FMT_F32) {
 #pragma unroll
@@ -105,46 +157,56 @@ __device__ __forceinline__ Eight<FMT> rounded8(float* x) {
             e.b[i] = x[4 + i];
         }
     } else {
+        // results that need no saturation and are no NaN, as nearly always, take
+        // four instructions (FP8), or no overflow's (FP16)
         float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) top = maximum3_abs(top, x[i], x[i + 1]);
-        if (__builtin_expect(top < 0x1p31f, 1)) {
+        if constexpr (FMT == FP8T_FMT_FP16) {
+            if (__builtin_expect(top < 0x1p31f, 1)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                e.a[i] = fp16_pair(x[2 * i], x[2 * i + 1]);
-                const float2 p = fp16_finite_pair(e.a[i]);
-                x[2 * i] = p.x;
-                x[2 * i + 1] = p.y;
+                for (int i = 0; i < 4; ++i) e.a[i] = fp16_pair(x[2 * i], x[2 * i + 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    e.a[i] = (uint32_t)f32_to_fp16_rn(x[2 * i]) | ((uint32_t)f32_to_fp16_rn(x[2 * i + 1]) << 16);
+            }
+        } else if (__builtin_expect(top <= 57344.0f, 1)) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t w = __builtin_amdgcn_cvt_pk_bf8_f32(x[4 * i], x[4 * i + 1], 0, false);
+                e.a[i] = __builtin_amdgcn_cvt_pk_bf8_f32(x[4 * i + 2], x[4 * i + 3], w, true);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t lo = f32_to_fp16_rn(x[2 * i]), hi = f32_to_fp16_rn(x[2 * i + 1]);
-                e.a[i] = lo | (hi << 16);
-                x[2 * i] = fp16_to_f32(lo);
-                x[2 * i + 1] = fp16_to_f32(hi);
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t lo = f32x2_to_fp8x2<false>(x[4 * i], x[4 * i + 1], 0u);
+                e.a[i] = f32x2_to_fp8x2<true>(x[4 * i + 2], x[4 * i + 3], lo);
             }
         }
     }
     return e;
 }
-// n <= 8 stored elements (F32 or FP16) to p on.
-template <int FMT>
-__device__ __forceinline__ void store_stored8(fmt_t<FMT>* p, int n, const Eight<FMT>& e) {
-    if (n == 8) {
-        *reinterpret_cast<Eight<FMT>*>(p) = e;
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i >= n) break;
-        if constexpr (FMT == FP8T_FMT_F32) p[i] = i < 4 ? e.a[i % 4] : e.b[i % 4];
-        else p[i] = (uint16_t)(e.a[i / 2] >> (16 * (i % 2)));
-    }
+template <int FMT, bool FOURS>
+__device__ __forceinline__ void put8(fmt_t<FMT>* row, const Cols<FOURS>& c, int64_t W, const float* x, bool stream) {
+    store8<FMT>(row, c, W, codes8<FMT>(x), stream);
 }
+// The same in a format that is known at run time only (uniform).
+template <bool FOURS>
+__device__ __forceinline__ void put_as8(void* row, int fmt, const Cols<FOURS>& c, int64_t W, const float* x,
+                                        bool stream) {
+    if (fmt == FP8T_FMT_F32) put8<FP8T_FMT_F32>(static_cast<float*>(row), c, W, x, stream);
+    else if (fmt == FP8T_FMT_FP16) put8<FP8T_FMT_FP16>(static_cast<uint16_t*>(row), c, W, x, stream);
+    else put8<FP8T_FMT_FP8>(static_cast<uint8_t*>(row), c, W, x, stream);
+}
+inline int64_t bytes_of(int fmt) { return fmt == FP8T_FMT_F32 ? 4 : fmt == FP8T_FMT_FP16 ? 2 : 1; }
 
-__device__ __forceinline__ int left8(int64_t c, int64_t W) {
-    return W - c < 8 ? (int)(W - c) : 8;
+// Eight floats rounded to F32 or FP16: what is stored, and x what that stands for.
+template <int FMT>
+__device__ __forceinline__ Eight<FMT> rounded8(float* x) {
+    const Eight<FMT> e = codes8<FMT>(x);
+    if constexpr (FMT != FP8T_FMT_F32) values8<FMT>(e, x);
+    return e;
 }
 
 // A reduction over the T threads of a row, T a power of two and rows beside each
