@@ -27,8 +27,10 @@
 extern "C" {
 #endif
 
-/* Largest vocabulary of embed_bwd. */
-#define FP8T_EMBED_MAX_V (1 << 24)
+/* Largest vocabulary of embed_bwd, token_logprobs and token_logprobs_bwd. */
+#define FP8T_MAX_VOCAB (1 << 24)
+/* Widest row of rms_norm_fwd and rms_norm_bwd. */
+#define FP8T_MAX_NORM_W (1 << 20)
 /* Most alternatives token_logprobs gives. */
 #define FP8T_MAX_TOP 128
 
@@ -55,7 +57,7 @@ int embed_fwd(const int64_t* tokens, int64_t T, const void* table, int table_for
  * e: T x W in e_format; g: V x W in g_format; both F32, FP16 or FP8.
  * workspace: at least embed_bwd_workspace_size bytes, 16-byte aligned.
  * Errors: FP8T_EINVAL (negative size, T or W above 2^31 - 4097, V above
- * FP8T_EMBED_MAX_V, unknown format, a stride below W, NULL pointer for
+ * FP8T_MAX_VOCAB, unknown format, a stride below W, NULL pointer for
  * non-empty data, a workspace that is not 16-byte aligned); FP8T_EWORKSPACE
  * (workspace_bytes below the query); FP8T_EHIP.
  */
@@ -81,18 +83,19 @@ size_t embed_bwd_workspace_size(int64_t T, int64_t V, int64_t W);
  * y_row_scale[t], so that the row's largest result is y_scale.  A product with
  * y in place of n c, given to the next norm as x with that y_row_scale as its
  * x_row_scale, is divided by it again.
+ * Inf and NaN follow IEEE arithmetic within their row (a row with an Inf has
+ * rstd 0) and leave the other rows alone.
  *
  * x: T x W in x_format (F32 or FP16); r, h: T x W in s_format (F32 or FP16); w:
  * W contiguous in w_format (F32 or FP16); y: T x W in y_format (F32, FP16 or
  * FP8); x_row_scale, y_row_scale, rstd: T floats.  r, w, x_row_scale and the
  * results h, y, y_row_scale, rstd are optional (NULL), one of h, y and rstd is
  * not.  h may be r or x itself (same format and stride); other results must
- * not overlap an operand.  A row that holds an Inf or NaN is not finite itself
- * and leaves the others alone.
- * Errors: FP8T_EINVAL (negative size, T or W above 2^31 - 4097, unknown
- * format, a stride below W, eps not from 2^-100 to 2^100, NULL pointer for
- * non-empty data, no result, y_row_scale without y or with a y_scale that is not
- * positive and finite); FP8T_EHIP.
+ * not overlap an operand.
+ * Errors: FP8T_EINVAL (negative size, T above 2^31 - 4097, W above
+ * FP8T_MAX_NORM_W, unknown format, a stride below W, eps not from 2^-100 to
+ * 2^100, NULL pointer for non-empty data, no result, y_row_scale without y or
+ * with a y_scale that is not positive and finite); FP8T_EHIP.
  */
 int rms_norm_fwd(const void* x, int x_format, int64_t x_ld, const float* x_row_scale,
                  const void* r, int64_t r_ld, const void* w, int w_format, int64_t T, int64_t W,
@@ -154,9 +157,9 @@ size_t rms_norm_bwd_workspace_size(int64_t T, int64_t W);
  * workspace: token_logprobs_workspace_size bytes for the fastest plan, or none
  * (workspace_bytes == 0, then a plan that needs none); it holds the partial
  * results of parts of rows that several workgroups share.
- * Errors: FP8T_EINVAL (negative size, N above 2^31 - 4097, V above 2^31 - 131073, V = 0
- * with N > 0, m > 4096, k > FP8T_MAX_TOP, tau not from 2^-30 to 2^30, unknown
- * format, a stride below V, NULL pointer for non-empty data, no result, NULL
+ * Errors: FP8T_EINVAL (negative size, N above 2^31 - 4097, V above
+ * FP8T_MAX_VOCAB, V = 0 with N > 0, m > 4096, k > FP8T_MAX_TOP, tau not from
+ * 2^-30 to 2^30, unknown format, a stride below V, NULL pointer for non-empty data, no result, NULL
  * workspace with workspace_bytes > 0, or one that is not 16-byte aligned where
  * it is used); FP8T_EWORKSPACE (0 < workspace_bytes < the query); FP8T_EHIP.
  */

@@ -17,7 +17,7 @@ SRC_F32, SRC_FP16 = 0, 1
 EXACT, FAST = 0, 1
 FMT_F32, FMT_FP16, FMT_FP8, FMT_HALF = 0, 1, 2, 3
 ATTN_MAX_D = 128
-MAX_TOP, EMBED_MAX_V = 128, 1 << 24
+MAX_TOP, MAX_VOCAB, MAX_NORM_W = 128, 1 << 24, 1 << 20
 
 _lib = None
 

@@ -425,7 +425,7 @@ void launch_bwd(GradArgs a, hipStream_t stream) {
 }
 
 bool grad_sizes_ok(int64_t T, int64_t V, int64_t W) {
-    return T >= 0 && V >= 0 && W >= 0 && T <= kMaxGemmDim && W <= kMaxGemmDim && V <= FP8T_EMBED_MAX_V;
+    return T >= 0 && V >= 0 && W >= 0 && T <= kMaxGemmDim && W <= kMaxGemmDim && V <= FP8T_MAX_VOCAB;
 }
 
 // fn<FX, FY>(a, stream) for formats known at run time.

@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kMaxGiven = 4096;
 constexpr int64_t kAcross = 1 << 20;           // rows along a grid's first dimension
-constexpr int64_t kMaxV = INT32_MAX - 131072;  // a thread's next positions stay in 32 bits
+constexpr int64_t kMaxV = FP8T_MAX_VOCAB;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -270,6 +270,7 @@ __device__ __forceinline__ void add_logits(Soft& x, const float (&y)[N][8], floa
     all *= kUnit;
     if (all > x.m) move_to(x, all, to2);
     const float m = x.m == -INFINITY ? 0.0f : x.m;
+    float s = 0.0f, t = 0.0f;                               // of these alone: shorter chains of additions
 #pragma unroll
     for (int u = 0; u < N; ++u)
 #pragma unroll
@@ -277,9 +278,11 @@ __device__ __forceinline__ void add_logits(Soft& x, const float (&y)[N][8], floa
             // the distance first, exact or rounded once
             const float d = (FZ == FP8T_FMT_F32 ? y[u][i] - m : __builtin_fmaf(y[u][i], kUnit, -m)) * to2;
             const float p = __builtin_amdgcn_exp2f(d);
-            x.s += p;
-            x.t = __builtin_fmaf(fmaxf(d, floor2), p, x.t);  // d = -Inf adds 0
+            s += p;
+            t = __builtin_fmaf(fmaxf(d, floor2), p, t);      // d = -Inf adds 0
         }
+    x.s += s;
+    x.t += t;
 }
 
 // The largest of eight neighbouring lanes, in all of them.
@@ -309,8 +312,7 @@ struct Blocks {
         n = (((tiles - 1) >> shift) + 1) * in_tile;
     }
     // The first element of eight number u of block i, from the part's start; it
-    // may lie behind the part's end, by less than a tenth of its length (blocks of
-    // several tiles: at least 17 times their tiles are there), below 2^32.
+    // may lie behind the part's end.
     __device__ __forceinline__ uint32_t element(int i, int u, int T) const {
         const uint32_t tile = (i / in_tile << shift) + (fine ? 0 : u >> 3), at = i % in_tile;
         return tile * T * 8 + (fine ? at * 8 : at * 64 + (u & 7) * 8);

@@ -251,7 +251,7 @@ extern "C" int rms_norm_fwd(const void* x, int x_format, int64_t x_ld, const flo
                             int64_t W, float eps, void* h, int s_format, int64_t h_ld, void* y,
                             int y_format, int64_t y_ld, float y_scale, float* y_row_scale,
                             float* rstd, hipStream_t stream) {
-    if (T < 0 || W < 0 || T > kMaxGemmDim || W > kMaxGemmDim || !float_or_16(x_format) ||
+    if (T < 0 || W < 0 || T > kMaxGemmDim || W > FP8T_MAX_NORM_W || !float_or_16(x_format) ||
         !float_or_16(s_format) || !float_or_16(w_format) || !storage_format(y_format) ||
         !(eps >= 0x1p-100f) || !(eps <= 0x1p100f))
         return FP8T_EINVAL;

@@ -52,10 +52,15 @@ struct Loaded {
     float rstd;
 };
 
+// Threads of a workgroup: several rows' where they are short, so that there are
+// fewer rows of partial sums.
+template <int T>
+constexpr int kRowThreads = T < 512 ? 512 : T;
+
 // T threads of a row; AHEAD: the next row is on its way while one is worked on.
 template <int FH, int FY, int FD, int T, int NV, bool AHEAD>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_bwd_kernel(NormGradArgs a) {
-    constexpr int kThreads = T < 256 ? 256 : T, kGroups = kThreads / T;
+__global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradArgs a) {
+    constexpr int kThreads = kRowThreads<T>, kGroups = kThreads / T;
     using C = Cols<kFours<FH, FY, FD>>;
     __shared__ float red[2][kThreads / 64];
     __shared__ float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? T * NV * 8 : 1];
@@ -257,7 +262,7 @@ struct NormGradPlan {
 NormGradPlan norm_grad_plan(int64_t T, int64_t W) {
     int64_t threads = 8;                                    // of a row: eight columns each
     while (threads < 1024 && threads * 8 < W) threads *= 2;
-    const int64_t groups = threads < 256 ? 256 / threads : 1;
+    const int64_t groups = threads < 512 ? 512 / threads : 1;
     int64_t cus = device_cus();
     if (cus <= 0) cus = 256;
     // as many as run at a time, but two rows for each group at least
@@ -276,7 +281,7 @@ NormGradPlan norm_grad_plan(int64_t T, int64_t W) {
 template <int FH, int FY, int FD, int T, int NV>
 void launch_rows(const NormGradArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((rms_norm_bwd_kernel<FH, FY, FD, T, NV, NV == 1>), dim3((unsigned)a.blocks),
-                       dim3(T < 256 ? 256 : T), 0, stream, a);
+                       dim3(kRowThreads<T>), 0, stream, a);
 }
 
 template <int FH, int FY, int FD>
@@ -313,7 +318,7 @@ void launch_dy(const NormGradArgs& a, int dy_format, hipStream_t stream) {
 }
 
 bool norm_sizes_ok(int64_t T, int64_t W) {
-    return T >= 0 && W >= 0 && T <= kMaxGemmDim && W <= kMaxGemmDim;
+    return T >= 0 && W >= 0 && T <= kMaxGemmDim && W <= FP8T_MAX_NORM_W;
 }
 
 }  // namespace

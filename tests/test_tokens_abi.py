@@ -32,7 +32,8 @@ def test_declared_and_exported(lib):
     for name in names:
         assert hasattr(lib, name) and callable(getattr(fp8t, name)), name
     assert re.search(r"FP8T_MAX_TOP\s+%d\b" % fp8t.MAX_TOP, open(HEADER).read())
-    assert fp8t.EMBED_MAX_V == 1 << 24 and "FP8T_EMBED_MAX_V (1 << 24)" in open(HEADER).read()
+    assert fp8t.MAX_VOCAB == 1 << 24 and "FP8T_MAX_VOCAB (1 << 24)" in open(HEADER).read()
+    assert fp8t.MAX_NORM_W == 1 << 20 and "FP8T_MAX_NORM_W (1 << 20)" in open(HEADER).read()
 
 
 def caller(f, **defaults):
@@ -71,6 +72,7 @@ def test_rms_norm_fwd_rejects(lib):
                   eps=1e-5, h=FAKE, sf=0, hld=8, y=FAKE, yf=2, yld=8, ys=1.0, yrs=None, rstd=FAKE)
     nan, inf = float("nan"), float("inf")
     for bad in (dict(T=-1), dict(W=-1), dict(T=BIG), dict(W=BIG, xld=BIG, rld=BIG, hld=BIG, yld=BIG),
+                dict(W=2 ** 20 + 1, xld=BIG, rld=BIG, hld=BIG, yld=BIG),
                 dict(xf=2), dict(sf=2), dict(wf=2), dict(yf=3), dict(xld=7), dict(rld=7), dict(hld=7),
                 dict(yld=7), dict(x=None), dict(eps=0.0), dict(eps=-1e-5), dict(eps=nan), dict(eps=inf),
                 dict(eps=1e-38), dict(h=None, y=None, rstd=None), dict(y=None, yrs=FAKE),
@@ -85,6 +87,7 @@ def test_rms_norm_bwd_rejects(lib):
                   dr=FAKE, drld=8, T=3, W=8, dx=FAKE, df=0, dxld=8, dx8=FAKE, dx8ld=8, s8=1.0, dw=FAKE,
                   dwf=0, ws=FAKE, wsb=1 << 20)
     for bad in (dict(T=-1), dict(W=-1), dict(T=BIG), dict(W=BIG, hld=BIG, dyld=BIG, drld=BIG, dxld=BIG, dx8ld=BIG),
+                dict(W=2 ** 20 + 1, hld=BIG, dyld=BIG, drld=BIG, dxld=BIG, dx8ld=BIG),
                 dict(hf=2), dict(wf=2), dict(dyf=3), dict(df=2), dict(dwf=2), dict(hld=7), dict(dyld=7),
                 dict(drld=7), dict(dxld=7), dict(dx8ld=7), dict(h=None), dict(dy=None), dict(rstd=None),
                 dict(dx=None, dx8=None, dw=None), dict(ws=FAKE + 4), dict(ws=None)):
@@ -96,6 +99,7 @@ def test_rms_norm_bwd_rejects(lib):
 
 
 LOGITS_BAD = (dict(N=-1), dict(V=-1), dict(V=0), dict(m=-1), dict(m=4097), dict(N=BIG), dict(V=BIG, zld=BIG),
+              dict(V=2 ** 24 + 1, zld=BIG),
               dict(zf=2), dict(zld=49), dict(z=None), dict(tau=0.0), dict(tau=-1.0),
               dict(tau=float("nan")), dict(tau=float("inf")), dict(idx=None))
 
