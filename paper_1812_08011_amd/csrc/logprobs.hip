@@ -49,12 +49,11 @@ struct LogprobArgs {
 struct Soft {
     float m, s, t;
 };
-// The sums of x relative to the larger m.
+// The sums of x relative to m, its largest or larger.  Nothing there (-Inf) stays
+// nothing, a NaN stays.
 __device__ __forceinline__ void move_to(Soft& x, float m, float to2) {
-    if (x.m == m) return;
-    const float d = (x.m - m) * to2;                        // negative; -Inf: nothing was there
-    const float f = exp2f(d);
-    x.t = f > 0.0f ? f * (x.t + d * x.s) : 0.0f * x.s;      // 0, or a NaN kept
+    const float d = x.m == m ? 0.0f : fmaxf((x.m - m) * to2, -1000.0f), f = __builtin_amdgcn_exp2f(d);
+    x.t = f * __builtin_fmaf(d, x.s, x.t);
     x.s *= f;
     x.m = m;
 }
@@ -65,6 +64,20 @@ __device__ __forceinline__ Soft join(Soft a, Soft b, float to2) {
     a.s += b.s;
     a.t += b.t;
     return a;
+}
+// The sums of a wave's lanes, in all of them: the largest first, so that each
+// lane's sums move once.
+__device__ __forceinline__ Soft wave_join(Soft x, float to2) {
+    float m = x.m;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    move_to(x, m, to2);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        x.s += __shfl_xor(x.s, d);
+        x.t += __shfl_xor(x.t, d);
+    }
+    return x;
 }
 
 // Order of a float as a whole number: -0 is 0, NaN is above +Inf.
@@ -299,22 +312,23 @@ __device__ __forceinline__ float max_of_8_lanes(float x) {
 // 8 or 64 elements; blocks of 64 of 1 << shift tiles (0, or 2 and more) may be
 // one.  At most `most` of them.
 struct Blocks {
-    int in_tile, units, shift, n;      // blocks of a tile; eights of a block; all blocks
+    int log_in_tile, log_units, shift, n;   // blocks of a tile; eights of a block; all blocks
     bool fine;
     __device__ __forceinline__ Blocks(int length, int T, int most) {
-        const int tiles = (length + T * 8 - 1) / (T * 8);
+        const int tiles = (length + T * 8 - 1) / (T * 8), log_T = 31 - __clz(T);
         fine = tiles <= most / T;
-        in_tile = fine ? T : T / 8;
+        log_in_tile = fine ? log_T : log_T - 3;
         shift = 0;
-        if (!fine && tiles > most / in_tile)
-            for (shift = 2; ((tiles - 1) >> shift) + 1 > most / in_tile;) ++shift;
-        units = (fine ? 1 : 8) << shift;
-        n = (((tiles - 1) >> shift) + 1) * in_tile;
+        if (!fine && tiles > most >> log_in_tile)
+            for (shift = 2; ((tiles - 1) >> shift) + 1 > most >> log_in_tile;) ++shift;
+        log_units = (fine ? 0 : 3) + shift;
+        n = (((tiles - 1) >> shift) + 1) << log_in_tile;
     }
     // The first element of eight number u of block i, from the part's start; it
     // may lie behind the part's end.
     __device__ __forceinline__ uint32_t element(int i, int u, int T) const {
-        const uint32_t tile = (i / in_tile << shift) + (fine ? 0 : u >> 3), at = i % in_tile;
+        const uint32_t tile = (i >> log_in_tile << shift) + (fine ? 0 : u >> 3);
+        const uint32_t at = i & ((1 << log_in_tile) - 1);
         return tile * T * 8 + (fine ? at * 8 : at * 64 + (u & 7) * 8);
     }
 };
@@ -424,11 +438,7 @@ __device__ __forceinline__ void finish_top(const LogprobArgs& a, S& s, int64_t n
 // The sums of all threads.  red: T / 64 of them, free before the call.
 template <int T>
 __device__ __forceinline__ Soft block_join(Soft x, Soft* red, float to2) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        Soft y = {__shfl_xor(x.m, d), __shfl_xor(x.s, d), __shfl_xor(x.t, d)};
-        x = join(x, y, to2);
-    }
+    x = wave_join(x, to2);
     if constexpr (T > 64) {
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
         __syncthreads();
@@ -598,7 +608,7 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
     for (int i = tid; i < blocks.n; i += T)
         if (odd || order_of(most[i]) >= bound) chosen[atomicAdd(&reached, 1)] = (uint16_t)i;
     __syncthreads();
-    const int items = reached * blocks.units;
+    const int items = reached << blocks.log_units;
     // below every value where there are fewer groups than k (a NaN's bits then)
     const float least = value_of_order(bound);
     constexpr int kItems = 4;
@@ -607,10 +617,10 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
         int at[kItems];
 #pragma unroll
         for (int u = 0; u < kItems; ++u) {
-            const int item = i + u * T, who = item / blocks.units;
+            const int item = i + u * T, who = item >> blocks.log_units;
             at[u] = v1;
             if (item < items) {
-                const uint32_t v = v0 + blocks.element(chosen[who], item - who * blocks.units, T);
+                const uint32_t v = v0 + blocks.element(chosen[who], item - (who << blocks.log_units), T);
                 if (v < (uint32_t)v1) at[u] = (int)v;
             }
             if (at[u] < v1) e[u] = load_logits<FZ>(z, at[u], v1);
@@ -650,10 +660,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobArgs 
     // every wave joins the parts' sums: lane i has part i's
     const int lane = tid & 63;
     const float4 own = lane < a.parts ? sums[lane] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
-    Soft x = {own.x, own.y, own.z};
-#pragma unroll
-    for (int d = 32; d; d >>= 1)
-        x = join(x, Soft{__shfl_xor(x.m, d), __shfl_xor(x.s, d), __shfl_xor(x.t, d)}, a.to2);
+    const Soft x = wave_join(Soft{own.x, own.y, own.z}, a.to2);
     row_results<FZ, kJoinThreads>(a, n, z, x, given);
     if (k == 0) return;
     __syncthreads();
