@@ -11,8 +11,7 @@
 //             its rows (that is where its part of the sorted list begins), then
 //             every wave places its own tokens in order.
 //   sum    -- a workgroup takes a piece of the sorted tokens, each of its groups
-//             of lanes the runs (equal tokens) that begin in a share of
-//             kShare tokens.  A run of more than kLong is cut at the shares'
+//             of lanes the runs (equal tokens) that begin in its share.  A run of more than kLong is cut at the shares'
 //             borders: the parts' sums meet in LDS, in order, and those of runs
 //             that leave the piece go to the workspace.  Other workgroups write
 //             the rows that no token names.
@@ -89,7 +88,8 @@ void launch_fwd(const EmbedArgs& a, hipStream_t stream) {
 
 constexpr int kIndexThreads = 1024, kWaves = kIndexThreads / 64, kMaxRows = 512;
 constexpr int kSeen = 192;             // tokens of its rows that a wave of the index kernel keeps
-constexpr int kShare = 16, kLong = 32; // sorted tokens per group of lanes; the longest run that is not cut
+constexpr int kMinShare = 4, kShare = 16;   // sorted tokens of a group of lanes
+constexpr int kLong = 32;              // the longest run that is not cut
 constexpr int kZeroRows = 16;          // rows that a wave looks at for those without a token
 static_assert(kLong >= kShare, "a run longer than kLong passes a border of its share");
 
@@ -102,7 +102,7 @@ struct GradArgs {
     int R;                             // vocabulary rows per index workgroup
     int log_lanes;                     // lanes of a row of errors, eight columns each
     int slabs;                         // column slabs of 8 << log_lanes
-    int piece;                         // sorted tokens of a workgroup: its groups' shares
+    int share, piece;                  // sorted tokens of a group of lanes, of a workgroup
     int64_t pieces, piece_blocks, zero_blocks;
     int* start;                        // V + 1: a row's first sorted token
     int2* list;                        // T: (token, position), sorted
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
     // [1] of one that begins there (whole workgroups' worth: 256 x 8 floats each)
     __shared__ float4 part[2][2][kThreads];
     __shared__ int left[2][kThreads];                       // their tokens, -1: none
-    const int from = (int)p * a.piece + group * kShare, to = from + kShare < n ? from + kShare : n;
+    const int from = (int)p * a.piece + group * a.share, to = from + a.share < n ? from + a.share : n;
     if (lane == 0) left[0][group] = left[1][group] = -1;
     if (from < n) {
         const fmt_t<FE>* e = static_cast<const fmt_t<FE>*>(a.e);
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(GradArgs a) {
 }
 
 struct GradPlan {
-    int R, log_lanes, slabs, piece;
+    int R, log_lanes, slabs, share, piece;
     int64_t pieces;
     size_t list, parts, bytes;         // offsets into the workspace: start, list, parts
 };
@@ -395,7 +395,11 @@ GradPlan grad_plan(int64_t T, int64_t V, int64_t W) {
     p.R = (int)(r < 16 ? 16 : r > kMaxRows ? kMaxRows : r);
     p.log_lanes = log_lanes(W, 64);
     p.slabs = (int)((W + (8 << p.log_lanes) - 1) / (8 << p.log_lanes));
-    p.piece = kShare * (kThreads >> p.log_lanes);
+    // small shares where few tokens would leave CUs idle: 257 tokens of 256 columns
+    // 13 us with 16, 10 with 4
+    const int64_t waves = (T * p.slabs << p.log_lanes) / 64;   // of one token each
+    p.share = (int)(waves / 2048 < kMinShare ? kMinShare : waves / 2048 > kShare ? kShare : waves / 2048);
+    p.piece = p.share * (kThreads >> p.log_lanes);
     p.pieces = (T + p.piece - 1) / p.piece;
     auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };
     p.list = up(sizeof(int) * (size_t)(V + 1));
@@ -502,6 +506,7 @@ extern "C" int embed_bwd(const int64_t* tokens, int64_t T, const void* e, int e_
     a.R = p.R;
     a.log_lanes = p.log_lanes;
     a.slabs = p.slabs;
+    a.share = p.share;
     a.piece = p.piece;
     a.pieces = p.pieces;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
