@@ -21,22 +21,27 @@ struct NormArgs {
     float* y_row_scale;
     float* rstd;
     int64_t x_ld, r_ld, h_ld, y_ld, T, W;
+    double inv_W;
     int w_format, y_format;
     bool sum;                          // u is rounded to the stream's format
     bool stream_h, stream_y;           // results past the caches
     float eps, y_scale;
 };
 
+// 1 / sqrt(x): a float's, and a step of Newton's method on it in double precision.
+__device__ __forceinline__ double inverse_sqrt(double x) {
+    const double r = (double)(1.0f / sqrtf((float)x));
+    return r == 0.0 ? 0.0 : r * (1.5 - 0.5 * x * r * r);
+}
 // 1 / sqrt(mean + eps) of a row whose squares add up to `ss`; the squares of
 // finite floats can pass FP32's largest: then `again` gives their sum times
-// 2^-160.  eps >= 2^-100 hides what squares lose below 2^-126.
+// 2^-160.  eps >= 2^-100 hides what squares lose below 2^-126.  An Inf in the row
+// gives 0.
 template <typename AGAIN>
-__device__ __forceinline__ float inverse_rms(float ss, int64_t W, float eps, AGAIN again) {
-    if (__builtin_expect(ss == INFINITY, 0)) {
-        const float s = again() / (float)W + (eps * 0x1p-80f) * 0x1p-80f;
-        return 0x1p-80f / sqrtf(s);                         // Inf in the row: 0
-    }
-    return 1.0f / sqrtf(ss / (float)W + eps);
+__device__ __forceinline__ double inverse_rms(double ss, double inv_W, float eps, AGAIN again) {
+    if (__builtin_expect(!(ss < 1e38), 0))
+        return 0x1p-80 * inverse_sqrt(again() * inv_W + (double)eps * 0x1p-160);
+    return inverse_sqrt(ss * inv_W + (double)eps);
 }
 __device__ __forceinline__ float row_scale(float top, float y_scale) {
     return top > 0.0f && top < INFINITY ? fminf(y_scale / top, 0x1p126f) : 1.0f;
@@ -84,7 +89,8 @@ struct NormRow {
 template <int FX, int FS, int T, int NV>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a) {
     constexpr int kRows = T < 256 ? 256 / T : 1;            // rows of a workgroup
-    __shared__ float red[2][T < 256 ? 1 : T / 64];
+    __shared__ double sums[2][T < 256 ? 1 : T / 64];
+    __shared__ float red[T < 256 ? 1 : T / 64];
     const int tid = threadIdx.x % T;
     const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + threadIdx.x / T;
     if (t >= a.T) return;                                   // all threads of a row
@@ -134,8 +140,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
         if (row.h) values8<FS>(load8<FS>(row.h, c, a.W), v);
         else row.sum(load8<FX>(row.x, c, a.W), row.residual(c), c, v);
     };
-    ss = row_reduce<T>(ss, red[0], RowSum());
-    const float rstd = inverse_rms(ss, a.W, a.eps, [&]() {
+    const double r = inverse_rms(row_reduce<T>((double)ss, sums[0], RowSum()), a.inv_W, a.eps, [&]() {
         float s = 0.0f;
         auto add = [&](const float* v) {
 #pragma unroll
@@ -152,14 +157,19 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
                 add(u[0]);
             }
         }
-        return row_reduce<T>(s, red[1], RowSum());
+        return row_reduce<T>((double)s, sums[1], RowSum());
     });
+    // in two floats, so that n is rounded once
+    const float rstd = (float)r, rest = (float)(r - (double)rstd);
     if (a.rstd && tid == 0) a.rstd[t] = rstd;
     if (!a.y) return;
     float scale = a.y_scale;
     auto norm = [&](float* v, const float* wv) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * wv[i];
+        for (int i = 0; i < 8; ++i) {
+            const float n = v[i] * rstd, e = __builtin_fmaf(v[i], rest, __builtin_fmaf(v[i], rstd, -n));
+            v[i] = __builtin_fmaf(n, wv[i], e * wv[i]);
+        }
     };
     auto weights = [&](const C& c, float* wv) {
 #pragma unroll
@@ -189,8 +199,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
                 most(u[0]);
             }
         }
-        if constexpr (T > 64) __syncthreads();              // red[1] may be in use
-        scale = row_scale(row_reduce<T>(top, red[1], RowMax()), a.y_scale);
+        scale = row_scale(row_reduce<T>(top, red, RowMax()), a.y_scale);
         if (tid == 0) a.y_row_scale[t] = scale;
     }
     uint8_t* y = static_cast<uint8_t*>(a.y) +
@@ -275,6 +284,7 @@ extern "C" int rms_norm_fwd(const void* x, int x_format, int64_t x_ld, const flo
     a.y_ld = y_ld;
     a.T = T;
     a.W = W;
+    a.inv_W = 1.0 / (double)W;
     a.w_format = w_format;
     a.y_format = y_format;
     a.sum = r || h;

@@ -211,16 +211,16 @@ __device__ __forceinline__ Eight<FMT> rounded8(float* x) {
 
 // A reduction over the T threads of a row, T a power of two and rows beside each
 // other in the workgroup; every thread gets the same bits.  T up to 64 needs no
-// LDS; else red has a float for each wave of the workgroup, free before the
+// LDS; else red has a number for each wave of the workgroup, free before the
 // call, and all its threads call.
-template <int T, typename OP>
-__device__ __forceinline__ float row_reduce(float x, float* red, OP op) {
+template <int T, typename X, typename OP>
+__device__ __forceinline__ X row_reduce(X x, X* red, OP op) {
 #pragma unroll
     for (int d = (T < 64 ? T : 64) / 2; d; d >>= 1) x = op(x, __shfl_xor(x, d));
     if constexpr (T > 64) {
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
         __syncthreads();
-        const float* mine = red + threadIdx.x / T * (T / 64);
+        const X* mine = red + threadIdx.x / T * (T / 64);
         x = mine[0];
 #pragma unroll
         for (int i = 1; i < T / 64; ++i) x = op(x, mine[i]);
@@ -228,7 +228,8 @@ __device__ __forceinline__ float row_reduce(float x, float* red, OP op) {
     return x;
 }
 struct RowSum {
-    __device__ float operator()(float a, float b) const { return a + b; }
+    template <typename X>
+    __device__ X operator()(X a, X b) const { return a + b; }
 };
 // NaN wins.
 struct RowMax {
