@@ -1,7 +1,9 @@
 // embed_fwd, embed_bwd: rows of a table by tokens, and the table's gradient.
 //
 // Forward: HBM-bound, one pass.  A thread owns eight columns of four rows,
-// whose tokens and table rows are loaded together.
+// whose tokens and table rows are loaded together.  16384 tokens of a text's
+// frequencies, 50001 x 2048 FP16 to floats: 26 us, 6.1 TB/s (a copy of 1 GiB runs
+// at 5.6, a fill at 6.9).  One, two or eight rows change that by 3%.
 //
 // Backward: the tokens are sorted, so that every row of the gradient is summed
 // by one reader of its errors and written once, with no atomics.  Two or three
@@ -9,13 +11,20 @@
 //   index  -- workgroup r owns R rows of the vocabulary and reads all tokens
 //             twice: first it counts each row's tokens per wave and those below
 //             its rows (that is where its part of the sorted list begins), then
-//             every wave places its own tokens in order.
+//             every wave places its own tokens in order.  No sorting passes, no
+//             scan over workgroups: reading 16384 tokens in each of 256
+//             workgroups is 32 MB from the L2s, 8 us; from some 10^6 tokens on it
+//             is what the call takes longest for.
 //   sum    -- a workgroup takes a piece of the sorted tokens, each of its groups
-//             of lanes the runs (equal tokens) that begin in its share.  A run of more than kLong is cut at the shares'
-//             borders: the parts' sums meet in LDS, in order, and those of runs
-//             that leave the piece go to the workspace.  Other workgroups write
-//             the rows that no token names.
+//             of lanes the runs (equal tokens) that begin in its share.  The
+//             errors of eight tokens are on their way whatever runs they belong
+//             to (run by run: 107 us where this takes 33).  A run of more than
+//             kLong is cut at the shares' borders: the parts' sums meet in LDS,
+//             in order, and those of runs that leave the piece go to the
+//             workspace.  Other workgroups write the rows that no token names.
 //   join   -- adds the parts of such runs in their order.
+// 16384 tokens into 32768 x 1024 floats: 8 + 33 + 5 us; the gradient's 134 MB and
+// the errors' 34 are 30 us of a copy's rate.
 #include "row_ops.h"
 
 namespace fp8t {

@@ -1,6 +1,6 @@
 // token_logprobs: log probabilities of given tokens, entropy, likeliest tokens.
 //
-// HBM-bound: a row's logits are read once from memory.  Each thread keeps, of
+// A row's logits are read once from memory.  Each thread keeps, of
 // its own elements, the largest x, the sum of 2^d and the sum of d 2^d with d
 // = (x - largest) log2(e) / tau; the workgroup joins them.  The entropy is
 // ln S - (sum of d e^d) / S, both terms of one sign each, so that nothing
@@ -17,6 +17,14 @@
 //
 // Where rows are few, several workgroups share one, each with the k largest of
 // its part, and a second kernel joins them.
+//
+// 4096 x 32768 FP16: 55 us without alternatives, 4.9 TB/s; 78 with 20 of them, 85
+// with 64 (73 at the clock of a cool card): a row's sums, bound, second reading
+// and ranking follow each other, and the vector ALUs, busy for two thirds of the
+// time with 11 instructions a logit and 5000 a row, are what other rows share.  Floats,
+// twice the bytes: 93, 101 and 107 us.  One row of 50001 floats, 20 alternatives: 9
+// us and 5 for the join.
+//
 #include <type_traits>
 
 #include "row_ops.h"
@@ -766,7 +774,9 @@ struct LogprobGradArgs {
     bool stream;                       // results past the caches
 };
 
-// HBM-bound and without sums over the row: a workgroup owns a chunk of one.
+// HBM-bound and without sums over the row: a workgroup owns a chunk of one.  4096
+// x 32768 FP16 to FP8: 76 us, 5.3 TB/s; 777 x 50001 floats, three given tokens: 63
+// us, 4.9 TB/s (a copy of 1 GiB runs at 5.6).
 template <int FZ, int FG>
 __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradArgs a) {
     constexpr int kUnits = 4;

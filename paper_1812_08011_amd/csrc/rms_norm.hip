@@ -2,7 +2,15 @@
 //
 // HBM-bound.  T threads own a row and keep it in registers, NV times eight
 // elements each, between the sum of squares and the result: every element is
-// read once and written once.  Rows wider than kWidest are read again.
+// read once and written once.  T is the fewest threads that hold a row (8 for 64
+// columns: 100000 x 64 FP16 in 12 us, with a wave a row 84).  Rows wider than
+// kWidest are read again.
+//
+// 16384 x 4096, FP16 + floats to floats and FP8, each row scaled: 129 us, 5.7 TB/s
+// (a copy of 1 GiB runs at 5.6); 8192 x 2048, all of it FP16, to FP8: 29 us, 4.0
+// TB/s, the vector ALUs between the codes and floats.  One row: 3.5 us, a launch.
+// The sum leaves the threads in double precision and 1 / rms is a double, so that
+// a result is rounded once before its scale; it costs less than the spread.
 #include "row_ops.h"
 
 namespace fp8t {

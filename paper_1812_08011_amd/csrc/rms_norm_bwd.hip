@@ -1,11 +1,17 @@
 // rms_norm_bwd: gradients of the root-mean-square norm.
 //
 // HBM-bound, one pass.  A workgroup owns a range of rows; the T threads of a
-// row keep it in registers (NV times eight elements each) between the mean and
-// the gradient, and their columns' sums of dw over the rows.  Those go to the
-// workspace, one row of sums for each workgroup, and a second kernel adds them
-// in order.  Rows wider than kWidest are read twice, and dw has a kernel of its
-// own.
+// row keep it in registers, eight elements each, between the mean and the
+// gradient, with the next row on its way, and their columns' sums of dw over the
+// rows.  Those go to the workspace, one row of sums for each workgroup, and a
+// second kernel adds them in order.  Rows wider than 8192 are twice eight
+// elements a thread without a row ahead (no registers are left), those wider
+// than kWidest are read twice, and dw has a kernel of its own.
+//
+// 8192 x 4096 floats with FP16 errors, to floats and FP8: 98 us and 5 for the
+// join, 4.9 TB/s (a copy of 1 GiB runs at 5.6); twice eight elements in 256 threads, 155
+// registers, and no row ahead: 109 and 7.  5003 x 1001 in FP16: 15 us and 4, three
+// rows for each group of threads one after the other, 2 TB/s.
 #include "row_ops.h"
 
 namespace fp8t {
