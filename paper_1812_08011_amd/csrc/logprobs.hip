@@ -272,24 +272,38 @@ struct Raw {
         }
     }
 };
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+// The largest of three in one instruction (fmaxf of values from bits takes three),
+// a NaN left out.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// Constants of the loops over logits.  In vector registers: instructions that
+// read scalar ones issue at half rate.
+struct Consts {
+    float to2, unit;
+    __device__ __forceinline__ Consts(float to2_, float unit_)
+        : to2(__uint_as_float(in_vgpr(__float_as_uint(to2_)))),
+          unit(__uint_as_float(in_vgpr(__float_as_uint(unit_)))) {}
+};
+constexpr float kFloor2 = -160.0f;     // below it powers are 0
 
 // N times eight logits more: y is what Raw gives; top: the largest of each eight,
 // of the same unit.
 template <int FZ, int N>
-__device__ __forceinline__ void add_logits(Soft& x, const float (&y)[N][8], float (&top)[N], float to2,
-                                           float floor2) {
-    constexpr float kUnit = Raw<FZ>::kUnit;
+__device__ __forceinline__ void add_logits(Soft& x, const float (&y)[N][8], float (&top)[N], const Consts& k) {
     float all = -INFINITY;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-        top[u] = fmaxf(y[u][0], y[u][1]);
-#pragma unroll
-        for (int i = 2; i < 8; i += 2) top[u] = max3(top[u], y[u][i], y[u][i + 1]);
+        top[u] = max3(y[u][0], y[u][1], y[u][2]);
+        top[u] = max3(top[u], y[u][3], y[u][4]);
+        top[u] = max3(top[u], y[u][5], y[u][6]);
+        top[u] = max3(top[u], y[u][7], y[u][7]);
         all = fmaxf(all, top[u]);
     }
-    all *= kUnit;
-    if (all > x.m) move_to(x, all, to2);
+    all *= k.unit;
+    if (all > x.m) move_to(x, all, k.to2);
     const float m = x.m == -INFINITY ? 0.0f : x.m;
     float s = 0.0f, t = 0.0f;                               // of these alone: shorter chains of additions
 #pragma unroll
@@ -297,10 +311,10 @@ __device__ __forceinline__ void add_logits(Soft& x, const float (&y)[N][8], floa
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             // the distance first, exact or rounded once
-            const float d = (FZ == FP8T_FMT_F32 ? y[u][i] - m : __builtin_fmaf(y[u][i], kUnit, -m)) * to2;
+            const float d = (FZ == FP8T_FMT_F32 ? y[u][i] - m : __builtin_fmaf(y[u][i], k.unit, -m)) * k.to2;
             const float p = __builtin_amdgcn_exp2f(d);
             s += p;
-            t = __builtin_fmaf(fmaxf(d, floor2), p, t);      // d = -Inf adds 0
+            t = __builtin_fmaf(fmaxf(d, kFloor2), p, t);     // d = -Inf adds 0
         }
     x.s += s;
     x.t += t;
@@ -472,8 +486,7 @@ __global__ __launch_bounds__(64) void logprob_short_kernel(LogprobArgs a) {
     const fmt_t<FZ>* z = static_cast<const fmt_t<FZ>*>(a.z) + n * a.z_ld;
     const int v0 = SPLIT ? blockIdx.z * a.per : 0;
     const int v1 = SPLIT && v0 + a.per < a.V ? v0 + a.per : a.V;
-    const float to2 = __uint_as_float(in_vgpr(__float_as_uint(a.to2)));
-    const float floor2 = __uint_as_float(in_vgpr(__float_as_uint(-160.0f)));
+    const Consts k(a.to2, Raw<FZ>::kUnit);
     Eight<FZ> e[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -487,7 +500,7 @@ __global__ __launch_bounds__(64) void logprob_short_kernel(LogprobArgs a) {
         if (v0 + u * kTile < v1) {                          // the same for all
             float y[1][8], most[1];
             Raw<FZ>::values(e[u], y[0]);
-            add_logits<FZ, 1>(x, y, most, to2, floor2);
+            add_logits<FZ, 1>(x, y, most, k);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 half[h] = max3(fmaxf(y[0][4 * h], y[0][4 * h + 1]), y[0][4 * h + 2], y[0][4 * h + 3]) * Raw<FZ>::kUnit;
@@ -500,7 +513,7 @@ __global__ __launch_bounds__(64) void logprob_short_kernel(LogprobArgs a) {
     }
     const bool odd = x.s != x.s;                            // a NaN, or +Inf, among this thread's
     if (tid == 0) s.count = 0;
-    x = block_join<T>(x, nullptr, to2);
+    x = block_join<T>(x, nullptr, a.to2);
     if (!SPLIT) row_results<FZ, T>(a, n, z, x, given);
     else if (tid == 0) a.part_sums[n * a.parts + blockIdx.z] = make_float4(x.m, x.s, x.t, 0.0f);
     if (a.k == 0) return;
@@ -537,9 +550,7 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
     const fmt_t<FZ>* z = static_cast<const fmt_t<FZ>*>(a.z) + n * a.z_ld;
     const int v0 = SPLIT ? blockIdx.z * a.per : 0;
     const int v1 = SPLIT && v0 + a.per < a.V ? v0 + a.per : a.V;
-    // in vector registers: instructions that read scalar ones issue at half rate
-    const float to2 = __uint_as_float(in_vgpr(__float_as_uint(a.to2)));
-    const float floor2 = __uint_as_float(in_vgpr(__float_as_uint(-160.0f)));
+    const Consts k(a.to2, Raw<FZ>::kUnit);
     const Given given = SPLIT ? Given{false, 0.0f} : load_given<FZ>(a, n, z, tid);
     Soft x = {-INFINITY, 0.0f, 0.0f};
     constexpr int kAhead = 2, kTile = T * 8;              // kAhead divides four, the least tiles of a block of several
@@ -569,7 +580,7 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) e[u] = *reinterpret_cast<const Eight<FZ>*>(at + u * kTile);
             }
-            add_logits<FZ, kAhead>(x, y, top, to2, floor2);
+            add_logits<FZ, kAhead>(x, y, top, k);
             if (a.k == 0) continue;
             if (blocks.fine) {
 #pragma unroll
@@ -595,13 +606,13 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
         float y[1][8], top[1];
         const int v = v0 + tile * kTile + tid * 8;
         Raw<FZ>::values(load_logits<FZ>(z, v, v1), y[0]);
-        add_logits<FZ, 1>(x, y, top, to2, floor2);
+        add_logits<FZ, 1>(x, y, top, k);
         if (a.k == 0) continue;
         if (blocks.fine) most[tile * T + tid] = top[0] * kUnit;
         else joined(tile, max_of_8_lanes(top[0]) * kUnit);
     }
     if (tid == 0) s.count = reached = 0;
-    x = block_join<T>(x, red, to2);
+    x = block_join<T>(x, red, a.to2);
     if (!SPLIT) row_results<FZ, T>(a, n, z, x, given);
     else if (tid == 0) a.part_sums[n * a.parts + blockIdx.z] = make_float4(x.m, x.s, x.t, 0.0f);
     if (a.k == 0) return;
@@ -823,12 +834,21 @@ __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradAr
     // in base 2: the row's factors are taken once, and no power of a sum
     const float inv = a.scale * exp2f(-ls * kLog2e);
     auto vgpr = [](float x) { return __uint_as_float(in_vgpr(__float_as_uint(x))); };
-    const float c0 = vgpr(-inv * (sum + dh * (H - ls))), c1 = vgpr(-inv * dh * kLn2);
-    const float to2 = vgpr(a.to2), floor2 = vgpr(-160.0f), m = vgpr(top);
+    const float c0 = vgpr(-inv * (sum + dh * (H - ls))), c1 = vgpr(-inv * dh * kLn2), m = vgpr(top);
+    const Consts k(a.to2, Raw<FZ>::kUnit);
     auto gradient = [&](float distance) {
-        const float d = distance * to2;
-        return __builtin_amdgcn_exp2f(d) * __builtin_fmaf(c1, fmaxf(d, floor2), c0);
+        const float d = distance * k.to2;
+        return __builtin_amdgcn_exp2f(d) * __builtin_fmaf(c1, fmaxf(d, kFloor2), c0);
     };
+    if (!some) {
+        const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const Cols<kFours> c(u, tid, kGradThreads);
+            if (c.any(v1 - v0)) put8<FG>(g + v0, c, v1 - v0, none, a.stream);
+        }
+        return;
+    }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
         const Cols<kFours> c(u, tid, kGradThreads);
@@ -837,10 +857,10 @@ __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradAr
         Raw<FZ>::values(e[u], x);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            x[i] = some ? gradient(FZ == FP8T_FMT_F32 ? x[i] - m : __builtin_fmaf(x[i], Raw<FZ>::kUnit, -m)) : 0.0f;
+            x[i] = gradient(FZ == FP8T_FMT_F32 ? x[i] - m : __builtin_fmaf(x[i], k.unit, -m));
         put8<FG>(g + v0, c, v1 - v0, x, a.stream);
     }
-    if (a.m == 0 || !some) return;
+    if (a.m == 0) return;
     // the given tokens of this chunk, each with the sum of its occurrences, by
     // the first of them -- after the others, above
     __syncthreads();
