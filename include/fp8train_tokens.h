@@ -14,9 +14,9 @@
  * whose order could change them); a workspace, where it is optional, chooses
  * the order of sums.  Nothing in a workspace is kept from one call for the
  * next; calls that may overlap need workspaces of their own.  Sums and
- * statistics are FP32; every result is rounded once, from FP32, to its storage
- * format: Q below (FP8: nearest even, saturating at 57344; FP16: nearest even;
- * F32: as is).
+ * statistics are FP32 or better; every result is rounded once, from FP32, to
+ * its storage format: Q below (FP8: nearest even, saturating at 57344; FP16:
+ * nearest even; F32: as is).
  */
 #ifndef FP8TRAIN_TOKENS_H
 #define FP8TRAIN_TOKENS_H
@@ -159,9 +159,9 @@ size_t rms_norm_bwd_workspace_size(int64_t T, int64_t W);
  * results of parts of rows that several workgroups share.
  * Errors: FP8T_EINVAL (negative size, N above 2^31 - 4097, V above
  * FP8T_MAX_VOCAB, V = 0 with N > 0, m > 4096, k > FP8T_MAX_TOP, tau not from
- * 2^-30 to 2^30, unknown format, a stride below V, NULL pointer for non-empty data, no result, NULL
- * workspace with workspace_bytes > 0, or one that is not 16-byte aligned where
- * it is used); FP8T_EWORKSPACE (0 < workspace_bytes < the query); FP8T_EHIP.
+ * 2^-30 to 2^30, unknown format, a stride below V, NULL pointer for non-empty
+ * data, no result, NULL workspace with workspace_bytes > 0, or one that is not
+ * 16-byte aligned where it is used); FP8T_EWORKSPACE (0 < workspace_bytes < the query); FP8T_EHIP.
  */
 int token_logprobs(const void* z, int z_format, int64_t z_ld, const int64_t* idx, int64_t m,
                    int64_t N, int64_t V, float tau, float* logp, float* entropy, float* stats,

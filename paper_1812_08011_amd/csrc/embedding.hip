@@ -21,7 +21,9 @@
 //             to (run by run: 107 us where this takes 33).  A run of more than
 //             kLong is cut at the shares' borders: the parts' sums meet in LDS,
 //             in order, and those of runs that leave the piece go to the
-//             workspace.  Other workgroups write the rows that no token names.
+//             workspace.  Sums are doubles (a frequent token's errors cancel; the
+//             vector ALUs are idle).  Other workgroups write the rows that no
+//             token names.
 //   join   -- adds the parts of such runs in their order.
 // 16384 tokens into 32768 x 1024 floats: 8 + 33 + 5 us; the gradient's 134 MB and
 // the errors' 34 are 30 us of a copy's rate.
@@ -111,11 +113,12 @@ struct GradArgs {
     int R;                             // vocabulary rows per index workgroup
     int log_lanes;                     // lanes of a row of errors, eight columns each
     int slabs;                         // column slabs of 8 << log_lanes
+    int log_columns, join_slabs;       // columns of a group of threads of the join, its column slabs
     int share, piece;                  // sorted tokens of a group of lanes, of a workgroup
     int64_t pieces, piece_blocks, zero_blocks;
     int* start;                        // V + 1: a row's first sorted token
     int2* list;                        // T: (token, position), sorted
-    float* parts;                      // pieces x 2 x W: sums of cut runs
+    double* parts;                     // pieces x 2 x W: sums of cut runs
     bool stream;                       // results past the caches
 };
 
@@ -226,11 +229,20 @@ __global__ __launch_bounds__(kIndexThreads) void embed_index_kernel(GradArgs a) 
 }
 
 template <int FG, bool FOURS>
-__device__ __forceinline__ void grad_out(const GradArgs& a, int64_t v, const Cols<FOURS>& c, const float* sum) {
+__device__ __forceinline__ void grad_out(const GradArgs& a, int64_t v, const Cols<FOURS>& c, const double* sum) {
     float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = sum[i] * a.scale;
+    for (int i = 0; i < 8; ++i) y[i] = (float)(sum[i] * (double)a.scale);
     put8<FG>(static_cast<fmt_t<FG>*>(a.g) + v * a.g_ld, c, a.W, y, a.stream);
+}
+
+// A cut run's part, in the workspace.
+template <bool FOURS>
+__device__ __forceinline__ void put_sums(const GradArgs& a, int64_t part, const Cols<FOURS>& c, const double* sum) {
+    double* to = a.parts + part * a.W;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c.has(i, a.W)) to[i < 4 ? c.a + i : c.b + i - 4] = sum[i];
 }
 
 template <int FE, int FG>
@@ -262,8 +274,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
     const int n = a.start[a.V];
     if (p * a.piece >= n) return;
     // what a group leaves of cut runs: [0] of one that began before its share,
-    // [1] of one that begins there (whole workgroups' worth: 256 x 8 floats each)
-    __shared__ float4 part[2][2][kThreads];
+    // [1] of one that begins there: eight sums of each thread
+    __shared__ double2 part[2][4][kThreads];
     __shared__ int left[2][kThreads];                       // their tokens, -1: none
     const int from = (int)p * a.piece + group * a.share, to = from + a.share < n ? from + a.share : n;
     if (lane == 0) left[0][group] = left[1][group] = -1;
@@ -280,13 +292,13 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
         if (tail_begin >= i && !cut_tail && tail_end > to) last = tail_end;
         if (lane == 0 && cut_head) left[0][group] = head;
         if (lane == 0 && cut_tail) left[1][group] = tail;
-        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        double sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         int v = i < last ? a.list[i].x : -1;
         auto flush = [&]() {
             if ((v == head && cut_head) || (v == tail && cut_tail)) {
                 const int at = v == head && cut_head ? 0 : 1;
-                part[at][0][threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-                part[at][1][threadIdx.x] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) part[at][k][threadIdx.x] = make_double2(sum[2 * k], sum[2 * k + 1]);
             } else if (mine) {
                 grad_out<FG>(a, v, c, sum);
             }
@@ -313,12 +325,12 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
                     flush();
                     v = tok[u];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+                    for (int k = 0; k < 8; ++k) sum[k] = 0.0;
                 }
                 float w[8];
                 values8<FE>(x[u], w);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) sum[k] += w[k];
+                for (int k = 0; k < 8; ++k) sum[k] += (double)w[k];
             }
         }
         if (i < last) flush();
@@ -327,13 +339,13 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
     // the first group joins the parts of cut runs in their order; a run that
     // began before the piece or goes on behind it leaves a part of its own
     if (group > 0 || !c.any(a.W)) return;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    double sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     int v = -1;
     bool inside = false;                                    // the run began in this piece
     auto done = [&](bool more) {
         if (v < 0) return;
         if (inside && !more) grad_out<FG>(a, v, c, sum);
-        else put8<FP8T_FMT_F32>(a.parts + (p * 2 + inside) * a.W, c, a.W, sum, false);
+        else put_sums(a, p * 2 + inside, c, sum);
     };
     for (int g = 0; g < per; ++g)
 #pragma unroll
@@ -344,52 +356,40 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(GradArgs a) {
                 v = left[at][g];
                 inside = at == 1;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+                for (int k = 0; k < 8; ++k) sum[k] = 0.0;
             }
-            const int from_lane = (g << a.log_lanes) + lane;
-            const float4 lo = part[at][0][from_lane], hi = part[at][1][from_lane];
-            sum[0] += lo.x;
-            sum[1] += lo.y;
-            sum[2] += lo.z;
-            sum[3] += lo.w;
-            sum[4] += hi.x;
-            sum[5] += hi.y;
-            sum[6] += hi.z;
-            sum[7] += hi.w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const double2 x = part[at][k][(g << a.log_lanes) + lane];
+                sum[2 * k] += x.x;
+                sum[2 * k + 1] += x.y;
+            }
         }
     done(v >= 0 && a.start[v + 1] > (p + 1) * a.piece);
 }
 
-// The cut run that begins in piece p and goes on behind it, if one does.
+// The cut run that begins in piece p and goes on behind it, if one does: a thread
+// owns a column.
 template <int FG>
 __global__ __launch_bounds__(kThreads) void embed_join_kernel(GradArgs a) {
-    const int lanes = 1 << a.log_lanes, per = kThreads >> a.log_lanes;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int64_t unit = block * per + (threadIdx.x >> a.log_lanes);
-    const int64_t p = unit / a.slabs;
-    const Cols<true> c(unit % a.slabs, threadIdx.x & (lanes - 1), lanes);
+    const int64_t p = block / a.join_slabs * (kThreads >> a.log_columns) + (threadIdx.x >> a.log_columns);
+    const int64_t c = (block % a.join_slabs << a.log_columns) + (threadIdx.x & ((1 << a.log_columns) - 1));
     const int n = a.start[a.V];
-    if ((p + 1) * a.piece >= n || !c.any(a.W)) return;
+    if ((p + 1) * a.piece >= n || c >= a.W) return;
     const int v = a.list[(p + 1) * a.piece - 1].x, begin = a.start[v], end = a.start[v + 1];
     if (begin < p * a.piece || end <= (p + 1) * a.piece || end - begin <= kLong) return;
     const int64_t last = (end - 1) / a.piece;
-    float sum[8];
-    values8<FP8T_FMT_F32>(load8<FP8T_FMT_F32>(a.parts + (p * 2 + 1) * a.W, c, a.W), sum);
-    constexpr int kAhead = 8;
+    double sum = a.parts[(p * 2 + 1) * a.W + c];
+    constexpr int kAhead = 16;
     for (int64_t q = p + 1; q <= last; q += kAhead) {
-        Eight<FP8T_FMT_F32> x[kAhead] = {};
+        double x[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (q + u <= last) x[u] = load8<FP8T_FMT_F32>(a.parts + (q + u) * 2 * a.W, c, a.W);
+        for (int u = 0; u < kAhead; ++u) x[u] = q + u <= last ? a.parts[(q + u) * 2 * a.W + c] : 0.0;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            float y[8];
-            values8<FP8T_FMT_F32>(x[u], y);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += y[k];
-        }
+        for (int u = 0; u < kAhead; ++u) sum += x[u];
     }
-    grad_out<FG>(a, v, c, sum);
+    static_cast<fmt_t<FG>*>(a.g)[v * a.g_ld + c] = fmt_code<FG>((float)(sum * (double)a.scale));
 }
 
 struct GradPlan {
@@ -413,7 +413,7 @@ GradPlan grad_plan(int64_t T, int64_t V, int64_t W) {
     auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };
     p.list = up(sizeof(int) * (size_t)(V + 1));
     p.parts = p.list + up(sizeof(int2) * (size_t)T);
-    p.bytes = p.parts + (p.pieces > 1 ? sizeof(float) * 2 * (size_t)W * (size_t)p.pieces : 0);
+    p.bytes = p.parts + (p.pieces > 1 ? sizeof(double) * 2 * (size_t)W * (size_t)p.pieces : 0);
     return p;
 }
 
@@ -431,9 +431,12 @@ void launch_bwd(GradArgs a, hipStream_t stream) {
     a.zero_blocks = (a.V + kThreads / 64 * kZeroRows - 1) / (kThreads / 64 * kZeroRows);
     hipLaunchKernelGGL((embed_sum_kernel<FE, FG>), grid_of(a.piece_blocks + a.zero_blocks), dim3(kThreads), 0, stream, a);
     if (a.pieces > 1) {
-        const int64_t per = kThreads >> a.log_lanes;
-        hipLaunchKernelGGL((embed_join_kernel<FG>), grid_of((a.piece_blocks + per - 1) / per), dim3(kThreads), 0,
-                           stream, a);
+        a.log_columns = 0;
+        while ((1 << a.log_columns) < kThreads && (1 << a.log_columns) < a.W) ++a.log_columns;
+        a.join_slabs = (int)((a.W + (1 << a.log_columns) - 1) >> a.log_columns);
+        const int64_t per = kThreads >> a.log_columns;
+        hipLaunchKernelGGL((embed_join_kernel<FG>), grid_of((a.pieces + per - 1) / per * a.join_slabs),
+                           dim3(kThreads), 0, stream, a);
     }
 }
 
@@ -521,7 +524,7 @@ extern "C" int embed_bwd(const int64_t* tokens, int64_t T, const void* e, int e_
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     a.start = reinterpret_cast<int*>(ws);
     a.list = reinterpret_cast<int2*>(ws + p.list);
-    a.parts = reinterpret_cast<float*>(ws + p.parts);
+    a.parts = reinterpret_cast<double*>(ws + p.parts);
     FP8T_BY_FORMATS(launch_bwd, e_format, g_format, a, stream)
     return launch_status();
 }
