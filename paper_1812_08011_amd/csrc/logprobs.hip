@@ -18,15 +18,13 @@
 // Where rows are few, several workgroups share one, each with the k largest of
 // its part, and a second kernel joins them.
 //
-// 4096 x 32768 FP16: 55 us without alternatives, 4.9 TB/s; 78 with 20 of them, 85
-// with 64 (73 at the clock of a cool card): a row's sums, bound, second reading
-// and ranking follow each other, and the vector ALUs, busy for two thirds of the
-// time with 11 instructions a logit and 5000 a row, are what other rows share.  Floats,
-// twice the bytes: 93, 101 and 107 us.  One row of 50001 floats, 20 alternatives: 9
-// us and 5 for the join.
+// 4096 x 32768 FP16: 54 us without alternatives, 4.9 TB/s; 71 with 20 of them, 81
+// with 64 (72 on a card that has not been at work): a row's sums, bound, second
+// reading and ranking follow each other and hide behind other rows only, and they
+// are 1000 vector instructions a row with one alternative, 3000 with 64, beside 12
+// a logit, the vector ALUs' share of the stream.  Floats, twice the bytes: 92, 100
+// and 105 us.  One row of 50001 floats, 20 alternatives: 9 us and 5 for the join.
 //
-#include <type_traits>
-
 #include "row_ops.h"
 
 namespace fp8t {
@@ -320,14 +318,18 @@ __device__ __forceinline__ void add_logits(Soft& x, const float (&y)[N][8], floa
     x.t += t;
 }
 
-// The largest of eight neighbouring lanes, in all of them.
+// The largest of eight neighbouring lanes, in all of them: an instruction a step
+// (three from builtins), two states after the one that wrote what other lanes
+// read.
 __device__ __forceinline__ float max_of_8_lanes(float x) {
-    auto other = [](float v, auto ctrl) {
-        return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xF, 0xF, true));
-    };
-    x = fmaxf(x, other(x, std::integral_constant<int, 0xB1>()));    // lanes 1 0 3 2
-    x = fmaxf(x, other(x, std::integral_constant<int, 0x4E>()));    // lanes 2 3 0 1
-    return fmaxf(x, other(x, std::integral_constant<int, 0x141>()));  // mirrored in eight
+    float r;
+    asm("s_nop 1\n\tv_max_f32_dpp %0, %1, %1 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+        "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+        "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_half_mirror row_mask:0xf bank_mask:0xf\n\t"
+        "s_nop 1"
+        : "=&v"(r)
+        : "v"(x));
+    return r;
 }
 
 // Where a row's blocks lie: tiles of T x 8 elements, of each `in_tile` blocks of
@@ -629,7 +631,7 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
     __syncthreads();
     const int items = reached << blocks.log_units;
     // below every value where there are fewer groups than k (a NaN's bits then)
-    const float least = value_of_order(bound);
+    const float least = value_of_order(bound) * (1.0f / kUnit);   // rounded, it keeps the order
     constexpr int kItems = 4;
     for (int i = tid; i < items; i += T * kItems) {
         Eight<FZ> e[kItems];
@@ -648,12 +650,12 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
         for (int u = 0; u < kItems; ++u) {
             if (at[u] >= v1) continue;
             float y[8];
-            values8<FZ>(e[u], y);
+            Raw<FZ>::values(e[u], y);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (!(y[j] < least) && at[u] + j < v1) {
                     const int to = atomicAdd(&s.count, 1);  // the order is made below
-                    if (to < kRoom) s.keys[to] = key_of(order_of(y[j]), at[u] + j);
+                    if (to < kRoom) s.keys[to] = key_of(order_of(y[j] * kUnit), at[u] + j);
                 }
         }
     }
@@ -746,9 +748,9 @@ template <int FZ>
 void launch(const LogprobArgs& a, hipStream_t stream) {
     // The fewest threads whose sums are not the longer part of a row's time: each
     // row waits for its sums, its bound and its few elements again, and more rows
-    // at a time hide that.  k 20, T 128, 256 and 512: 8192 x 8192 FP16 51, 59 and
-    // 105 us; 4096 x 32768 75, 69 and 75; 512 x 131072 59, 36 and 36 (with k 64 75,
-    // 44 and 38).
+    // at a time hide that.  k 20, T 128, 256 and 512, measured side by side: 8192 x
+    // 8192 FP16 51, 59 and 105 us; 4096 x 32768 75, 69 and 75; 512 x 131072 59, 36
+    // and 36 (with k 64 75, 44 and 38).
     const int length = a.parts > 1 ? a.per : a.V;
     if (length <= kShort) {
         if (a.parts > 1)
@@ -786,8 +788,8 @@ struct LogprobGradArgs {
 };
 
 // HBM-bound and without sums over the row: a workgroup owns a chunk of one.  4096
-// x 32768 FP16 to FP8: 76 us, 5.3 TB/s; 777 x 50001 floats, three given tokens: 63
-// us, 4.9 TB/s (a copy of 1 GiB runs at 5.6).
+// x 32768 FP16 to FP8: 73 us, 5.5 TB/s; 777 x 50001 floats, three given tokens: 60
+// us, 5.2 TB/s (a copy of 1 GiB runs at 5.6).
 template <int FZ, int FG>
 __global__ __launch_bounds__(kGradThreads) void logprob_bwd_kernel(LogprobGradArgs a) {
     constexpr int kUnits = 4;
