@@ -4,14 +4,18 @@
 // row keep it in registers, eight elements each, between the mean and the
 // gradient, with the next row on its way, and their columns' sums of dw over the
 // rows.  Those go to the workspace, one row of sums for each workgroup, and a
-// second kernel adds them in order.  Rows wider than 8192 are twice eight
+// second kernel adds them in order.  These sums are doubles, a
+// workgroup's stored as floats: the conversion and the add hide behind the stream
+// (1 us of the 16 below).  Rows wider than 8192 are twice eight
 // elements a thread without a row ahead (no registers are left), those wider
 // than kWidest are read twice, and dw has a kernel of its own.
 //
 // 8192 x 4096 floats with FP16 errors, to floats and FP8: 98 us and 5 for the
 // join, 4.9 TB/s (a copy of 1 GiB runs at 5.6); twice eight elements in 256 threads, 155
-// registers, and no row ahead: 109 and 7.  5003 x 1001 in FP16: 15 us and 4, three
+// registers, and no row ahead: 109 and 7.  5003 x 1001 in FP16: 16 us and 5, three
 // rows for each group of threads one after the other, 2 TB/s.
+#include <type_traits>
+
 #include "row_ops.h"
 
 namespace fp8t {
@@ -68,19 +72,23 @@ template <int FH, int FY, int FD, int T, int NV, bool AHEAD>
 __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradArgs a) {
     constexpr int kThreads = kRowThreads<T>, kGroups = kThreads / T;
     using C = Cols<kFours<FH, FY, FD>>;
+    // doubles of twice eight columns would spill 50 bytes a thread; in floats a sum
+    // over R rows is off by (R + 2) 2^-24 of the sum of magnitudes at most
+    using Sum = std::conditional_t<NV == 1, double, float>;
     __shared__ float red[2][kThreads / 64];
-    __shared__ float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? T * NV * 8 : 1];
+    __shared__ double sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? T * NV * 8 : 1];
     const int tid = threadIdx.x % T, sub = threadIdx.x / T;
     const int64_t t0 = ((int64_t)blockIdx.x * kGroups + sub) * a.share;
     const bool out = a.dx || a.dx8;
-    float w[NV][8], dw[NV][8];
+    float w[NV][8];
+    Sum dw[NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const C c(v, tid, T);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             w[v][i] = 1.0f;
-            dw[v][i] = 0.0f;
+            dw[v][i] = 0;
         }
         if (a.w && c.any(a.W)) load_values8(a.w, a.w_format, c, a.W, w[v]);
     }
@@ -150,16 +158,19 @@ __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradAr
             }
         __syncthreads();
         for (int c = threadIdx.x; c < a.W; c += kThreads) {
-            float s = sums[0][c];
+            double s = sums[0][c];
 #pragma unroll
             for (int g = 1; g < kGroups; ++g) s += sums[g][c];
-            a.parts[(int64_t)blockIdx.x * a.W + c] = s;
+            a.parts[(int64_t)blockIdx.x * a.W + c] = (float)s;
         }
     } else {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const C c(v, tid, T);
-            if (c.any(a.W)) put8<FP8T_FMT_F32>(a.parts + (int64_t)blockIdx.x * a.W, c, a.W, dw[v], false);
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = (float)dw[v][i];
+            if (c.any(a.W)) put8<FP8T_FMT_F32>(a.parts + (int64_t)blockIdx.x * a.W, c, a.W, d, false);
         }
     }
 }
@@ -218,7 +229,7 @@ __global__ __launch_bounds__(kDwThreads) void rms_norm_dw_kernel(NormGradArgs a)
     const Cols<FH == FP8T_FMT_F32 || FY == FP8T_FMT_F32> c(blockIdx.x, threadIdx.x, kDwThreads);
     if (!c.any(a.W)) return;
     const int64_t t0 = blockIdx.y * a.share, t1 = t0 + a.share < a.T ? t0 + a.share : a.T;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    double sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int64_t t = t0; t < t1; ++t) {
         float n[8], g[8];
         values8<FH>(load8<FH>(static_cast<const fmt_t<FH>*>(a.h) + t * a.h_ld, c, a.W), n);
@@ -227,7 +238,10 @@ __global__ __launch_bounds__(kDwThreads) void rms_norm_dw_kernel(NormGradArgs a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += g[i] * (n[i] * rstd);
     }
-    put8<FP8T_FMT_F32>(a.parts + blockIdx.y * a.W, c, a.W, sum, false);
+    float d[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] = (float)sum[i];
+    put8<FP8T_FMT_F32>(a.parts + blockIdx.y * a.W, c, a.W, d, false);
 }
 
 // dw = the sum of the workgroups' rows: a lane owns a column, each wave a range
@@ -235,20 +249,20 @@ __global__ __launch_bounds__(kDwThreads) void rms_norm_dw_kernel(NormGradArgs a)
 __global__ __launch_bounds__(kJoinThreads) void rms_norm_join_kernel(const float* parts, int64_t blocks,
                                                                      int64_t W, void* dw, int dw_format) {
     constexpr int kWaves = kJoinThreads / 64;
-    __shared__ float sums[kWaves][64];
+    __shared__ double sums[kWaves][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane;
     const int64_t share = (blocks + kWaves - 1) / kWaves;
     const int64_t g0 = wave * share, g1 = g0 + share < blocks ? g0 + share : blocks;
-    float sum = 0.0f;
+    double sum = 0.0;
     if (c < W) {
         constexpr int kAhead = 16;
         for (int64_t g = g0; g < g1; g += kAhead) {
-            float x[kAhead];
+            float x[kAhead];                // the last row again past the end: no branches between
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) x[u] = g + u < g1 ? parts[(g + u) * W + c] : 0.0f;
+            for (int u = 0; u < kAhead; ++u) x[u] = parts[(g + u < g1 ? g + u : g1 - 1) * W + c];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) sum += x[u];
+            for (int u = 0; u < kAhead; ++u) sum += g + u < g1 ? x[u] : 0.0f;
         }
     }
     sums[wave][lane] = sum;
@@ -257,8 +271,8 @@ __global__ __launch_bounds__(kJoinThreads) void rms_norm_join_kernel(const float
     sum = sums[0][lane];
 #pragma unroll
     for (int i = 1; i < kWaves; ++i) sum += sums[i][lane];
-    if (dw_format == FP8T_FMT_F32) static_cast<float*>(dw)[c] = sum;
-    else static_cast<uint16_t*>(dw)[c] = f32_to_fp16_rn(sum);
+    if (dw_format == FP8T_FMT_F32) static_cast<float*>(dw)[c] = (float)sum;
+    else static_cast<uint16_t*>(dw)[c] = f32_to_fp16_rn((float)sum);
 }
 
 // Rows of a group of T threads, and workgroups (rows of partial sums).
