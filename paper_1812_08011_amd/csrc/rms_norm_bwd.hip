@@ -4,14 +4,14 @@
 // row keep it in registers, eight elements each, between the mean and the
 // gradient, with the next row on its way, and their columns' sums of dw over the
 // rows.  Those go to the workspace, one row of sums for each workgroup, and a
-// second kernel adds them in order.  These sums are doubles, a
-// workgroup's stored as floats: the conversion and the add hide behind the stream
-// (1 us of the 16 below).  Rows wider than 8192 are twice eight
-// elements a thread without a row ahead (no registers are left), those wider
-// than kWidest are read twice, and dw has a kernel of its own.
+// second kernel adds them in order.  The sums are doubles, a workgroup's stored as
+// floats: the conversion and the add hide behind the stream (1 us of the 16 below).
+// Rows wider than 8192 are twice eight elements a thread without a row ahead (no
+// registers are left), those wider than kWidest are read twice, and dw has a
+// kernel of its own.
 //
 // 8192 x 4096 floats with FP16 errors, to floats and FP8: 98 us and 5 for the
-// join, 4.9 TB/s (a copy of 1 GiB runs at 5.6); twice eight elements in 256 threads, 155
+// join, 5.1 TB/s (a copy of 1 GiB runs at 5.6); twice eight elements in 256 threads, 155
 // registers, and no row ahead: 109 and 7.  5003 x 1001 in FP16: 16 us and 5, three
 // rows for each group of threads one after the other, 2 TB/s.
 #include <type_traits>
