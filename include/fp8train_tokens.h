@@ -74,12 +74,12 @@ size_t embed_bwd_workspace_size(int64_t T, int64_t V, int64_t W);
  *   x'   = value(x[t, :]), or RN32(value(x[t, :]) / x_row_scale[t])
  *   u    = value(Q(RN32(x' + value(r[t, :])))), Q to s_format, written to h
  *   rstd = 1 / sqrt(mean(u^2) + eps)
- *   n    = u rstd value(w)                        (w NULL: 1)
+ *   n    = RN32(RN32(u rstd) value(w))            (w NULL: 1)
  *   y    = Q(RN32(n * c))
  * With neither r nor h, u = x' (not rounded); with h alone, u = value(Q(x')).
  * The norm is of the sum as it is stored, which is what rms_norm_bwd reads.
- * c = y_scale; with y_row_scale the row's own scale: c = y_scale / max |n|, at
- * most 2^126 (1 where that maximum is 0, infinite or NaN), written to
+ * c = y_scale; with y_row_scale the row's own scale: c = RN32(y_scale / max |n|),
+ * at most 2^126 (1 where that maximum is 0, infinite or NaN), written to
  * y_row_scale[t], so that the row's largest result is y_scale.  A product with
  * y in place of n c, given to the next norm as x with that y_row_scale as its
  * x_row_scale, is divided by it again.

@@ -9,8 +9,9 @@
 // 16384 x 4096, FP16 + floats to floats and FP8, each row scaled: 129 us, 5.7 TB/s
 // (a copy of 1 GiB runs at 5.6); 8192 x 2048, all of it FP16, to FP8: 29 us, 4.0
 // TB/s, the vector ALUs between the codes and floats.  One row: 3.5 us, a launch.
-// The sum leaves the threads in double precision and 1 / rms is a double, so that
-// a result is rounded once before its scale; it costs less than the spread.
+// The sum leaves the threads in double precision and 1 / rms is a double; n is the
+// floats' two products after it, as a program with rstd in hand forms it, Inf and
+// NaN included.
 #include "row_ops.h"
 
 namespace fp8t {
@@ -167,17 +168,13 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
         }
         return row_reduce<T>((double)s, sums[1], RowSum());
     });
-    // in two floats, so that n is rounded once
-    const float rstd = (float)r, rest = (float)(r - (double)rstd);
+    const float rstd = (float)r;
     if (a.rstd && tid == 0) a.rstd[t] = rstd;
     if (!a.y) return;
     float scale = a.y_scale;
     auto norm = [&](float* v, const float* wv) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float n = v[i] * rstd, e = __builtin_fmaf(v[i], rest, __builtin_fmaf(v[i], rstd, -n));
-            v[i] = __builtin_fmaf(n, wv[i], e * wv[i]);
-        }
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * wv[i];
     };
     auto weights = [&](const C& c, float* wv) {
 #pragma unroll
