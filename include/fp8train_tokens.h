@@ -73,7 +73,7 @@ size_t embed_bwd_workspace_size(int64_t T, int64_t V, int64_t W);
  * rms_norm_fwd -- a residual sum and its root-mean-square norm.  For row t:
  *   x'   = value(x[t, :]), or RN32(value(x[t, :]) / x_row_scale[t])
  *   u    = value(Q(RN32(x' + value(r[t, :])))), Q to s_format, written to h
- *   rstd = 1 / sqrt(mean(u^2) + eps)
+ *   rstd = RN32(1 / sqrt(mean(u^2) + eps)), formed in doubles
  *   n    = RN32(RN32(u rstd) value(w))            (w NULL: 1)
  *   y    = Q(RN32(n * c))
  * With neither r nor h, u = x' (not rounded); with h alone, u = value(Q(x')).

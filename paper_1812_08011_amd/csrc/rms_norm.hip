@@ -9,9 +9,9 @@
 // 16384 x 4096, FP16 + floats to floats and FP8, each row scaled: 129 us, 5.7 TB/s
 // (a copy of 1 GiB runs at 5.6); 8192 x 2048, all of it FP16, to FP8: 29 us, 4.0
 // TB/s, the vector ALUs between the codes and floats.  One row: 3.5 us, a launch.
-// The sum leaves the threads in double precision and 1 / rms is a double; n is the
-// floats' two products after it, as a program with rstd in hand forms it, Inf and
-// NaN included.
+// The squares (exact), their sum and 1 / rms are doubles, so that rstd is rounded
+// once; n is the floats' two products after it, as a program with rstd in hand
+// forms it, Inf and NaN included.
 #include "row_ops.h"
 
 namespace fp8t {
@@ -37,20 +37,15 @@ struct NormArgs {
     float eps, y_scale;
 };
 
-// 1 / sqrt(x): a float's, and a step of Newton's method on it in double precision.
+// 1 / sqrt(x), x > 0, to 2^-51 of itself: the hardware's estimate and two steps of
+// Newton's method (r += r e / 2, e = 1 - x r^2), which square its error each.  An
+// Inf gives 0.
 __device__ __forceinline__ double inverse_sqrt(double x) {
-    const double r = (double)(1.0f / sqrtf((float)x));
-    return r == 0.0 ? 0.0 : r * (1.5 - 0.5 * x * r * r);
-}
-// 1 / sqrt(mean + eps) of a row whose squares add up to `ss`; the squares of
-// finite floats can pass FP32's largest: then `again` gives their sum times
-// 2^-160.  eps >= 2^-100 hides what squares lose below 2^-126.  An Inf in the row
-// gives 0.
-template <typename AGAIN>
-__device__ __forceinline__ double inverse_rms(double ss, double inv_W, float eps, AGAIN again) {
-    if (__builtin_expect(!(ss < 1e38), 0))
-        return 0x1p-80 * inverse_sqrt(again() * inv_W + (double)eps * 0x1p-160);
-    return inverse_sqrt(ss * inv_W + (double)eps);
+    double r = __builtin_amdgcn_rsq(x);
+    if (r == 0.0) return r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = __builtin_fma(0.5 * r, __builtin_fma(-x * r, r, 1.0), r);
+    return r;
 }
 __device__ __forceinline__ float row_scale(float top, float y_scale) {
     return top > 0.0f && top < INFINITY ? fminf(y_scale / top, 0x1p126f) : 1.0f;
@@ -98,7 +93,7 @@ struct NormRow {
 template <int FX, int FS, int T, int NV>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a) {
     constexpr int kRows = T < 256 ? 256 / T : 1;            // rows of a workgroup
-    __shared__ double sums[2][T < 256 ? 1 : T / 64];
+    __shared__ double sums[T < 256 ? 1 : T / 64];
     __shared__ float red[T < 256 ? 1 : T / 64];
     const int tid = threadIdx.x % T;
     const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + threadIdx.x / T;
@@ -107,7 +102,11 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
     using C = typename NormRow<FX, FS>::C;
     const int64_t units = (a.W + 8 * T - 1) / (8 * T);      // of a wide row
     float u[NV ? NV : 1][8], w[NV ? NV : 1][8];
-    float ss = 0.0f;
+    double ss = 0.0;                                        // squares of floats are exact, and finite
+    auto square = [&](const float* v) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)v[i], (double)v[i], ss);
+    };
     if constexpr (NV > 0) {
         Eight<FX> ex[NV];
         Eight<FS> er[NV];
@@ -132,16 +131,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
         for (int v = 0; v < NV; ++v) {
             const C c(v, tid, T);
             row.sum(ex[v], er[v], c, u[v]);                 // 0 past the row's end
-#pragma unroll
-            for (int i = 0; i < 8; ++i) ss += u[v][i] * u[v][i];
+            square(u[v]);
         }
     } else {
         for (int64_t v = 0; v < units; ++v) {
             const C c(v, tid, T);
             if (!c.any(a.W)) break;
             row.sum(load8<FX>(row.x, c, a.W), row.residual(c), c, u[0]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) ss += u[0][i] * u[0][i];
+            square(u[0]);
         }
     }
     // u of a wide row once more: h may have taken r's or x's place
@@ -149,26 +146,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a)
         if (row.h) values8<FS>(load8<FS>(row.h, c, a.W), v);
         else row.sum(load8<FX>(row.x, c, a.W), row.residual(c), c, v);
     };
-    const double r = inverse_rms(row_reduce<T>((double)ss, sums[0], RowSum()), a.inv_W, a.eps, [&]() {
-        float s = 0.0f;
-        auto add = [&](const float* v) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += (v[i] * 0x1p-80f) * (v[i] * 0x1p-80f);
-        };
-        if constexpr (NV > 0) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) add(u[v]);
-        } else {
-            for (int64_t v = 0; v < units; ++v) {
-                const C c(v, tid, T);
-                if (!c.any(a.W)) break;
-                reload(c, u[0]);
-                add(u[0]);
-            }
-        }
-        return row_reduce<T>((double)s, sums[1], RowSum());
-    });
-    const float rstd = (float)r;
+    const float rstd = (float)inverse_sqrt(row_reduce<T>(ss, sums, RowSum()) * a.inv_W + (double)a.eps);
     if (a.rstd && tid == 0) a.rstd[t] = rstd;
     if (!a.y) return;
     float scale = a.y_scale;

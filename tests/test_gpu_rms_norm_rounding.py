@@ -78,3 +78,22 @@ def test_weights_that_are_not_finite(W, ty):
                 same(got, rounded(n, y))
                 if rows:
                     assert (c == 1.0).all() and np.array_equal(c, want)
+
+
+@pytest.mark.parametrize("W", WIDTHS + [300007])
+def test_rstd_is_rounded_once(W):
+    """Squares, their mean and 1 / rms are doubles: a sum of W terms is off by W
+    2^-53 of itself, 2^-34 at the widest here, rstd by half of that and its last
+    steps' 2^-50; then it is rounded to a float."""
+    rng = np.random.default_rng(122)
+    x = draw(rng, (5, W), F32)
+    x[1] *= F32(1e30)                                          # squares past FP32's range
+    x[2] *= F32(2.0 ** 62)
+    x[3] = np.exp(rng.uniform(-60, 60, W)).astype(F32)
+    x[4] *= F32(1e-30)
+    for ty, data in ((F32, x), (F16, draw(rng, (40, W), F16, 2.0))):
+        for eps in (1e-5, 2.0 ** -100):
+            h, y, rstd, _ = run(data, None, None, F32, False, eps=eps)
+            want = 1.0 / np.sqrt((value(h) ** 2).mean(1) + float(F32(eps)))
+            assert (abs(rstd - want) <= want * (2.0 ** -24 + 2.0 ** -35 + 2.0 ** -50) + 2.0 ** -150).all(), \
+                (abs(rstd / want - 1) * 2 ** 24).max()
