@@ -6,16 +6,14 @@
 // rows.  Those go to the workspace, one row of sums for each workgroup, and a
 // second kernel adds them in order.  The sums are doubles, a workgroup's stored as
 // floats: the conversion and the add hide behind the stream (1 us of the 16 below).
-// Rows wider than 8192 are twice eight elements a thread without a row ahead (no
-// registers are left), those wider than kWidest are read twice, and dw has a
-// kernel of its own.
+// Rows wider than 8192 are twice eight elements a thread without a row ahead and
+// with the sums in LDS (no registers are left), those wider than kWidest are read
+// twice, and dw has a kernel of its own.
 //
 // 8192 x 4096 floats with FP16 errors, to floats and FP8: 98 us and 5 for the
 // join, 5.1 TB/s (a copy of 1 GiB runs at 5.6); twice eight elements in 256 threads, 155
 // registers, and no row ahead: 109 and 7.  5003 x 1001 in FP16: 16 us and 5, three
 // rows for each group of threads one after the other, 2 TB/s.
-#include <type_traits>
-
 #include "row_ops.h"
 
 namespace fp8t {
@@ -72,23 +70,27 @@ template <int FH, int FY, int FD, int T, int NV, bool AHEAD>
 __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradArgs a) {
     constexpr int kThreads = kRowThreads<T>, kGroups = kThreads / T;
     using C = Cols<kFours<FH, FY, FD>>;
-    // doubles of twice eight columns would spill 50 bytes a thread; in floats a sum
-    // over R rows is off by (R + 2) 2^-24 of the sum of magnitudes at most
-    using Sum = std::conditional_t<NV == 1, double, float>;
+    // doubles of twice eight columns would spill 50 bytes a thread: they lie in LDS,
+    // 128 of its 160 KB (a workgroup of 1024 threads has a CU's registers anyway),
+    // each thread's beside the next one's.  2048 x 16384 floats with FP16 errors 110
+    // us, with float sums in registers 112; 2048 x 9000 of FP16, FP8 and FP16 66 and 64
+    constexpr bool kInLds = NV > 1;
+    __shared__ double wide[kInLds ? NV * 8 : 1][kInLds ? T : 1];
     __shared__ float red[2][kThreads / 64];
     __shared__ double sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? T * NV * 8 : 1];
     const int tid = threadIdx.x % T, sub = threadIdx.x / T;
     const int64_t t0 = ((int64_t)blockIdx.x * kGroups + sub) * a.share;
     const bool out = a.dx || a.dx8;
     float w[NV][8];
-    Sum dw[NV][8];
+    double dw[kInLds ? 1 : NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const C c(v, tid, T);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             w[v][i] = 1.0f;
-            dw[v][i] = 0;
+            if constexpr (kInLds) wide[v * 8 + i][tid] = 0.0;
+            else dw[v][i] = 0.0;
         }
         if (a.w && c.any(a.W)) load_values8(a.w, a.w_format, c, a.W, w[v]);
     }
@@ -121,10 +123,14 @@ __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradAr
             values8<FH>(next.h[v], n[v]);
             values8<FY>(next.y[v], g[v]);
             r[v] = next.r[v];
+            if (kInLds && a.parts && C(v, tid, T).any(a.W)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) wide[v * 8 + j][tid] += g[v][j] * (n[v][j] * rstd);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 n[v][j] *= rstd;
-                dw[v][j] += g[v][j] * n[v][j];
+                if constexpr (!kInLds) dw[v][j] += g[v][j] * n[v][j];
                 g[v][j] *= w[v][j];
                 dot += g[v][j] * n[v][j];
             }
@@ -169,7 +175,10 @@ __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradAr
             const C c(v, tid, T);
             float d[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = (float)dw[v][i];
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (kInLds) d[i] = (float)wide[v * 8 + i][tid];
+                else d[i] = (float)dw[v][i];
+            }
             if (c.any(a.W)) put8<FP8T_FMT_F32>(a.parts + (int64_t)blockIdx.x * a.W, c, a.W, d, false);
         }
     }
