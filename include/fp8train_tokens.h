@@ -111,8 +111,9 @@ int rms_norm_fwd(const void* x, int x_format, int64_t x_ld, const float* x_row_s
  *   d  = value(dr) + rstd (value(w) value(dy) - value(h) rstd m)
  *   dx = Q(d) in d_format,  dx8 = Q(RN32(d * dx8_scale)) in FP8
  *   dw = Q(sum over t of value(dy) value(h) rstd) in dw_format
- * d is the error of x' and of r alike.  The scales of y are constants: dy is
- * the error of n c times c.
+ * The products are FP32, m's sum and dw's are doubles (parts of dw's, the rows
+ * of a workgroup, are stored as floats).  d is the error of x' and of r alike.
+ * The scales of y are constants: dy is the error of n c times c.
  * h: h_format F32 or FP16; w: F32, FP16 or NULL; rstd: T floats; dy: F32, FP16
  * or FP8; dr, dx: d_format F32 or FP16, dx may be dr itself (same stride); dw:
  * W contiguous, F32 or FP16 (all +0 with T = 0).  dx, dx8 and dw are optional

@@ -4,8 +4,8 @@
 // row keep it in registers, eight elements each, between the mean and the
 // gradient, with the next row on its way, and their columns' sums of dw over the
 // rows.  Those go to the workspace, one row of sums for each workgroup, and a
-// second kernel adds them in order.  The sums are doubles, a workgroup's stored as
-// floats: the conversion and the add hide behind the stream (1 us of the 16 below).
+// second kernel adds them in order.  The sums and the mean's are doubles of float
+// products, a workgroup's dw is stored as floats: the conversion and the add hide behind the stream (1 us of the 16 below).
 // Rows wider than 8192 are twice eight elements a thread without a row ahead and
 // with the sums in LDS (no registers are left), those wider than kWidest are read
 // twice, and dw has a kernel of its own.
@@ -34,6 +34,7 @@ struct NormGradArgs {
     float* parts;                      // workgroups x W (null: no dw)
     int64_t h_ld, dy_ld, dr_ld, dx_ld, dx8_ld, T, W;
     int64_t share, blocks;             // rows of a group of T threads; workgroups
+    double inv_W;
     int w_format;
     float dx8_scale;
     bool stream, stream8;              // dx, dx8 past the caches
@@ -47,6 +48,11 @@ __device__ __forceinline__ void put(const NormGradArgs& a, int64_t t, const Cols
         for (int i = 0; i < 8; ++i) d[i] *= a.dx8_scale;
         put8<FP8T_FMT_FP8>(a.dx8 + t * a.dx8_ld, c, a.W, d, a.stream8);
     }
+}
+// Eight terms, two by two: a chain of additions is three long.
+template <typename F>
+__device__ __forceinline__ double sum8(F term) {
+    return ((term(0) + term(1)) + (term(2) + term(3))) + ((term(4) + term(5)) + (term(6) + term(7)));
 }
 template <int FH, int FY, int FD>
 constexpr bool kFours = FH == FP8T_FMT_F32 || FY == FP8T_FMT_F32 || FD == FP8T_FMT_F32;
@@ -76,7 +82,7 @@ __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradAr
     // us, with float sums in registers 112; 2048 x 9000 of FP16, FP8 and FP16 66 and 64
     constexpr bool kInLds = NV > 1;
     __shared__ double wide[kInLds ? NV * 8 : 1][kInLds ? T : 1];
-    __shared__ float red[2][kThreads / 64];
+    __shared__ double red[2][kThreads / 64];
     __shared__ double sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? T * NV * 8 : 1];
     const int tid = threadIdx.x % T, sub = threadIdx.x / T;
     const int64_t t0 = ((int64_t)blockIdx.x * kGroups + sub) * a.share;
@@ -115,7 +121,8 @@ __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradAr
     for (int64_t i = 0; i < a.share; ++i) {                 // the same number for all groups
         const int64_t t = t0 + i;
         if (!AHEAD) load(t, next);
-        float n[NV][8], g[NV][8], dot = 0.0f;
+        float n[NV][8], g[NV][8];
+        double dot = 0.0;
         Eight<FD> r[NV];
         const float rstd = next.rstd;
 #pragma unroll
@@ -132,12 +139,12 @@ __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradAr
                 n[v][j] *= rstd;
                 if constexpr (!kInLds) dw[v][j] += g[v][j] * n[v][j];
                 g[v][j] *= w[v][j];
-                dot += g[v][j] * n[v][j];
             }
+            dot += sum8([&](int j) { return (double)(g[v][j] * n[v][j]); });
         }
         if (AHEAD && i + 1 < a.share) load(t + 1, next);
         if (!out) continue;
-        const float m = row_reduce<T>(dot, red[i & 1], RowSum()) / (float)a.W;
+        const float m = (float)(row_reduce<T>(dot, red[i & 1], RowSum()) * a.inv_W);
         if (t >= a.T) continue;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -187,14 +194,15 @@ __global__ __launch_bounds__(kRowThreads<T>) void rms_norm_bwd_kernel(NormGradAr
 // Wide rows: one row per workgroup, read twice.
 template <int FH, int FY, int FD>
 __global__ __launch_bounds__(1024) void rms_norm_bwd_wide_kernel(NormGradArgs a) {
-    __shared__ float red[16];
+    __shared__ double red[16];
     const int64_t t = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (t >= a.T) return;
     const fmt_t<FH>* h = static_cast<const fmt_t<FH>*>(a.h) + t * a.h_ld;
     const fmt_t<FY>* dy = static_cast<const fmt_t<FY>*>(a.dy) + t * a.dy_ld;
     const fmt_t<FD>* dr = a.dr ? static_cast<const fmt_t<FD>*>(a.dr) + t * a.dr_ld : nullptr;
     const float rstd = a.rstd[t];
-    float n[8], g[8], w[8], dot = 0.0f;
+    float n[8], g[8], w[8];
+    double dot = 0.0;
     using C = Cols<kFours<FH, FY, FD>>;
     const int64_t units = (a.W + 8191) / 8192;
     auto load = [&](const C& c) {
@@ -213,10 +221,9 @@ __global__ __launch_bounds__(1024) void rms_norm_bwd_wide_kernel(NormGradArgs a)
         const C c(v, threadIdx.x, 1024);
         if (!c.any(a.W)) break;
         load(c);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dot += g[i] * n[i];
+        dot += sum8([&](int i) { return (double)(g[i] * n[i]); });
     }
-    const float m = row_reduce<1024>(dot, red, RowSum()) / (float)a.W;
+    const float m = (float)(row_reduce<1024>(dot, red, RowSum()) / (double)a.W);
     for (int64_t v = 0; v < units; ++v) {
         const C c(v, threadIdx.x, 1024);
         if (!c.any(a.W)) break;
@@ -393,6 +400,7 @@ extern "C" int rms_norm_bwd(const void* h, int h_format, int64_t h_ld, const voi
     a.dx8_ld = dx8_ld;
     a.T = T;
     a.W = W;
+    a.inv_W = 1.0 / (double)W;
     a.share = p.share;
     a.blocks = p.blocks;
     a.w_format = w_format;

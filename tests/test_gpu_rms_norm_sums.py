@@ -37,3 +37,37 @@ def test_weight_gradient_keeps_small_terms(T, W):
         fp8t.rms_norm_bwd(hd, None, torch.ones(T, device=DEV), dev(np.full((T, W), dy, ty)), None, dx, None, 1.0, again,
                           workspace(n), n)
         assert np.array_equal(host(again), host(dw))
+
+
+@pytest.mark.parametrize("W", [7, 64, 100, 200, 500, 1000, 2048, 4096, 8192, 8200, 16384, 20003])
+def test_row_mean_keeps_small_terms(W):
+    """Four rows whose small products stand beside +2^24 and -2^24, and random ones.
+    From a mean rounded once the gradient follows in float products: bit for bit in
+    random rows.  In the first ones an addition of doubles next to 2^24 loses 2^-29,
+    so that two orders' means are 2^-28 apart before they are rounded (2^-24 of
+    themselves each) and n m, g - n m and the residual's sum by their roundings; a
+    float there loses 1 with every addition."""
+    rng = np.random.default_rng(131)
+    T = 12
+    h, dy, dr = draw(rng, (T, W), F32), draw(rng, (T, W), F16), draw(rng, (T, W), F32)
+    w, rstd = draw(rng, W, F32), np.exp(rng.standard_normal(T)).astype(F32)
+    h[:4], rstd[:4] = rng.integers(-31, 32, (4, W)) / F32(64), 1
+    for row in range(4):
+        at = rng.permutation(W)[:2]
+        h[row, at] = 2.0 ** 24, -2.0 ** 24
+        w[at], dy[row, at] = 1, 31 << 9
+    for r in (None, dr):
+        say(f"rms_norm_bwd {T}x{W} mean, residual {r is not None}")
+        dx, dx8 = torch.empty((T, W), device=DEV), torch.empty((T, W), dtype=torch.uint8, device=DEV)
+        fp8t.rms_norm_bwd(dev(h), dev(w), dev(rstd), dev(dy), None if r is None else dev(r), dx, dx8, 4.0)
+        n, g = h * rstd[:, None], value(dy).astype(F32) * w
+        m = ((g * n).astype(np.float64).sum(1) / W).astype(F32)
+        own = rstd[:, None] * (g - n * m[:, None])
+        d = own if r is None else r + own
+        got = host(dx)
+        assert np.array_equal(got[4:], d[4:])
+        f = lambda a: abs(a[:4].astype(np.float64))
+        nm = f(n) * f(m[:, None])
+        lim = f(n) * 2.0 ** -28 + 2.0 ** -23 * (3 * nm + f(g) + f(d))
+        assert (f(got - d.astype(np.float64)) <= lim).all(), np.argwhere(f(got - d.astype(np.float64)) > lim)[:5]
+        assert np.array_equal(host(dx8), rounded(got, F8, 4.0))
