@@ -146,8 +146,9 @@ size_t rms_norm_bwd_workspace_size(int64_t T, int64_t W);
  *     is above +Inf); past the vocabulary's end -1 and -Inf.
  * Powers are taken of a logit's distance from the row's largest; below 2^-126
  * they are 0.  A row whose largest logit is +Inf or -Inf (every token masked),
- * or that holds a NaN, has NaN log probabilities and entropy; masked tokens
- * (-Inf) of other rows have a log probability of -Inf.
+ * or that holds a NaN, has NaN log probabilities, entropy and ln S, and M is
+ * +Inf, -Inf or NaN; masked tokens (-Inf) of other rows have a log probability
+ * of -Inf.
  * The top entries are what distill_loss takes of a teacher (top_idx as idx,
  * top_logp as t), the statistics what token_logprobs_bwd takes.
  *

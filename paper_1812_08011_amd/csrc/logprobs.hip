@@ -51,10 +51,12 @@ struct LogprobArgs {
     uint64_t* part_top;                // N x parts x k
 };
 
-// Largest element, sum of 2^d, sum of d 2^d.
+// Largest element (kTop for +Inf, whose distance from it is +Inf then), sum of 2^d,
+// sum of d 2^d.  So s is +Inf with an element of +Inf, NaN with a NaN alone.
 struct Soft {
     float m, s, t;
 };
+constexpr float kTop = 0x1.fffffep127f;        // FP32's largest
 // The sums of x relative to m, its largest or larger.  Nothing there (-Inf) stays
 // nothing, a NaN stays.
 __device__ __forceinline__ void move_to(Soft& x, float m, float to2) {
@@ -300,7 +302,7 @@ __device__ __forceinline__ void add_logits(Soft& x, const float (&y)[N][8], floa
         top[u] = max3(top[u], y[u][7], y[u][7]);
         all = fmaxf(all, top[u]);
     }
-    all *= k.unit;
+    all = fminf(all * k.unit, kTop);
     if (all > x.m) move_to(x, all, k.to2);
     const float m = x.m == -INFINITY ? 0.0f : x.m;
     float s = 0.0f, t = 0.0f;                               // of these alone: shorter chains of additions
@@ -359,8 +361,11 @@ struct Blocks {
 
 // What a row's sums are once joined: ln S and the entropy.
 __device__ __forceinline__ float log_sum(const Soft& x) {
-    // the largest is +Inf, NaN, or nothing was above -Inf
-    return x.m == -INFINITY || x.m == INFINITY ? NAN : log2f(x.s) * kLn2;
+    // +Inf or a NaN is there, or nothing is above -Inf
+    return x.m == -INFINITY || !(x.s < INFINITY) ? NAN : log2f(x.s) * kLn2;
+}
+__device__ __forceinline__ float largest(const Soft& x) {
+    return x.s < INFINITY ? x.m : x.s;
 }
 
 // A given token's logit, on its way since the kernel's start.
@@ -386,7 +391,7 @@ __device__ __forceinline__ void row_results(const LogprobArgs& a, int64_t n, con
     const float ls = log_sum(x);
     if (threadIdx.x == 0) {
         if (a.stats) {
-            a.stats[2 * n] = x.s != x.s ? NAN : x.m;
+            a.stats[2 * n] = largest(x);
             a.stats[2 * n + 1] = ls;
         }
         if (a.entropy) a.entropy[n] = ls - kLn2 * (x.t / x.s);
@@ -513,7 +518,7 @@ __global__ __launch_bounds__(64) void logprob_short_kernel(LogprobArgs a) {
             s.group[(U + u) * T + tid] = order_of(half[1]);
         }
     }
-    const bool odd = x.s != x.s;                            // a NaN, or +Inf, among this thread's
+    const bool odd = x.s != x.s;                            // a NaN among this thread's
     if (tid == 0) s.count = 0;
     x = block_join<T>(x, nullptr, a.to2);
     if (!SPLIT) row_results<FZ, T>(a, n, z, x, given);
@@ -624,7 +629,7 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
         s.group[g] = order_of(top);
     }
     const uint32_t bound = find_bound<T>(s, a.k);
-    // the blocks that reach the bound; all of them where a NaN, or +Inf, is about
+    // the blocks that reach the bound; all of them where a NaN, which maxima leave out, is about
     const bool odd = x.s != x.s;
     for (int i = tid; i < blocks.n; i += T)
         if (odd || order_of(most[i]) >= bound) chosen[atomicAdd(&reached, 1)] = (uint16_t)i;
