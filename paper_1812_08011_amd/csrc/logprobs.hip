@@ -368,6 +368,14 @@ __device__ __forceinline__ float largest(const Soft& x) {
     return x.s < INFINITY ? x.m : x.s;
 }
 
+// A log probability; a distance that passes FP32's range may not after the division.
+__device__ __forceinline__ float log_probability(float z, const Soft& x, float tau, float ls) {
+    const float d = z - x.m;
+    if (__builtin_expect(d == -INFINITY && z > -INFINITY, 0))
+        return (float)(((double)z - (double)x.m) / (double)tau - (double)ls);
+    return d / tau - ls;
+}
+
 // A given token's logit, on its way since the kernel's start.
 struct Given {
     bool used;
@@ -399,7 +407,7 @@ __device__ __forceinline__ void row_results(const LogprobArgs& a, int64_t n, con
     if (a.logp)
         for (int i = threadIdx.x; i < a.m; i += T) {
             const Given g = i == (int)threadIdx.x ? first : load_given<FZ>(a, n, z, i);
-            a.logp[n * a.m + i] = g.used ? (g.z - x.m) / a.tau - ls : 0.0f;
+            a.logp[n * a.m + i] = g.used ? log_probability(g.z, x, a.tau, ls) : 0.0f;
         }
 }
 
@@ -414,7 +422,7 @@ __device__ __forceinline__ void top_result(const LogprobArgs& a, int64_t n, int 
     if (a.top_logp) {
         const uint32_t o = (uint32_t)(key >> 32);
         const float v = o == 0xFFFFFFFFu ? NAN : value_of_order(o);
-        a.top_logp[at] = key ? (v - x.m) / a.tau - log_sum(x) : -INFINITY;
+        a.top_logp[at] = key ? log_probability(v, x, a.tau, log_sum(x)) : -INFINITY;
     }
 }
 

@@ -42,3 +42,28 @@ def test_largest_logit_of_rows_that_are_not_finite(ty, V, k):
             check("ln S", got[:, 1], want["stats"][rows, 1], want["stats_err"][rows, 1])
             if k:
                 assert np.array_equal(host(top_idx), want["top_idx"][rows])
+
+
+@pytest.mark.parametrize("tau", [2.0, 4.0, 1e9])
+@pytest.mark.parametrize("V", [5, 100, 3000, 70001])
+def test_distances_past_the_range_of_floats(V, tau):
+    """z - M beyond FP32's range, its quotient by tau within it: log probabilities
+    of given tokens and of the likeliest ones are finite."""
+    rng = np.random.default_rng(141)
+    z = draw(rng, (4, V), F32)
+    z[0], z[0, V // 2] = -3.2e38, 3.2e38
+    z[1] = rng.uniform(-3.3e38, 3.3e38, V).astype(F32)
+    z[2, 0], z[2, V - 1] = -3e38, 3e38
+    idx = np.stack([rng.integers(0, V, 3) for _ in range(4)])
+    idx[:, 0], idx[:, 1] = 0, V - 1
+    want = ot.logprobs(value(z), idx, float(F32(tau)), 4)
+    assert np.isfinite(want["logp"]).all()
+    for rows in (slice(0, 4), slice(0, 1), slice(1, 2)):
+        zd = dev(z[rows])
+        for n in sorted({0, fp8t.token_logprobs_workspace_size(zd, 4)}):
+            say(f"token_logprobs distances {rows} of {V} tau={tau} workspace={n}")
+            nan = lambda *s: torch.full(s, np.nan, device=DEV)
+            out = dict(logp=nan(len(zd), 3), entropy=nan(len(zd)), top_logp=nan(len(zd), 4))
+            fp8t.token_logprobs(zd, dev(idx[rows]), tau, **out, workspace=workspace(n), workspace_bytes=n)
+            for x in out:
+                check(x, host(out[x]), want[x][rows], want[x + "_err"][rows])
