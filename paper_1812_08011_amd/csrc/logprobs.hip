@@ -486,12 +486,12 @@ __device__ __forceinline__ Soft block_join(Soft x, Soft* red, float to2) {
     return x;
 }
 
-// Rows, or parts, of 2048 elements at most: one wave keeps them in registers, and
-// nothing is read again.  A group is half the eight elements of a load, so that
-// there are as many as alternatives but for the shortest rows, whose elements
-// all have room.
+// Rows of 2048 elements at most, which no workgroups share: one wave keeps them in
+// registers, and nothing is read again.  A group is half the eight elements of a
+// load, so that there are as many as alternatives but for the shortest rows, whose
+// elements all have room.
 constexpr int kShort = 2048;
-template <int FZ, bool SPLIT>
+template <int FZ>
 __global__ __launch_bounds__(64) void logprob_short_kernel(LogprobArgs a) {
     constexpr int T = 64, U = kShort / (T * 8), kTile = T * 8, kRoom = 512, kGroups = 2 * T * U;
     __shared__ Selection<kRoom, kGroups> s;
@@ -499,20 +499,18 @@ __global__ __launch_bounds__(64) void logprob_short_kernel(LogprobArgs a) {
     if (n >= a.N) return;
     const int tid = threadIdx.x;
     const fmt_t<FZ>* z = static_cast<const fmt_t<FZ>*>(a.z) + n * a.z_ld;
-    const int v0 = SPLIT ? blockIdx.z * a.per : 0;
-    const int v1 = SPLIT && v0 + a.per < a.V ? v0 + a.per : a.V;
     const Consts k(a.to2, Raw<FZ>::kUnit);
     Eight<FZ> e[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (v0 + u * kTile < v1) e[u] = load_logits<FZ>(z, v0 + u * kTile + tid * 8, v1);
-    const Given given = SPLIT ? Given{false, 0.0f} : load_given<FZ>(a, n, z, tid);
+        if (u * kTile < a.V) e[u] = load_logits<FZ>(z, u * kTile + tid * 8, a.V);
+    const Given given = load_given<FZ>(a, n, z, tid);
     Soft x = {-INFINITY, 0.0f, 0.0f};
     float top[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         float half[2] = {-INFINITY, -INFINITY};
-        if (v0 + u * kTile < v1) {                          // the same for all
+        if (u * kTile < a.V) {                              // the same for all
             float y[1][8], most[1];
             Raw<FZ>::values(e[u], y[0]);
             add_logits<FZ, 1>(x, y, most, k);
@@ -529,26 +527,25 @@ __global__ __launch_bounds__(64) void logprob_short_kernel(LogprobArgs a) {
     const bool odd = x.s != x.s;                            // a NaN among this thread's
     if (tid == 0) s.count = 0;
     x = block_join<T>(x, nullptr, a.to2);
-    if (!SPLIT) row_results<FZ, T>(a, n, z, x, given);
-    else if (tid == 0) a.part_sums[n * a.parts + blockIdx.z] = make_float4(x.m, x.s, x.t, 0.0f);
+    row_results<FZ, T>(a, n, z, x, given);
     if (a.k == 0) return;
     const uint32_t bound = find_bound<T>(s, a.k);
     // below every value where there are fewer groups than k (a NaN's bits then)
     const float least = value_of_order(bound);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int v = v0 + u * kTile + tid * 8;
-        if (v >= v1 || (!odd && top[u] < least)) continue;
+        const int v = u * kTile + tid * 8;
+        if (v >= a.V || (!odd && top[u] < least)) continue;
         float y[8];
         values8<FZ>(e[u], y);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (!(y[j] < least) && v + j < v1) {
+            if (!(y[j] < least) && v + j < a.V) {
                 const int to = atomicAdd(&s.count, 1);      // the order is made below
                 if (to < kRoom) s.keys[to] = key_of(order_of(y[j]), v + j);
             }
     }
-    finish_top<FZ, T, SPLIT>(a, s, n, z, v0, v1, bound, x);
+    finish_top<FZ, T, false>(a, s, n, z, 0, a.V, bound, x);
 }
 
 template <int FZ, int T, bool SPLIT>
@@ -731,7 +728,8 @@ LogprobPlan logprob_plan(int64_t N, int64_t V, int64_t k) {
     LogprobPlan p;
     int64_t cus = device_cus();
     if (cus <= 0) cus = 256;
-    // parts of 4096 elements at least, as many as fill the chip once
+    // parts of 4096 elements at least (the last one may have fewer), as many as fill
+    // the chip once
     int64_t parts = N > 0 ? cus / N : 1;
     if (parts > V / 4096) parts = V / 4096;
     if (parts > 32) parts = 32;
@@ -766,10 +764,7 @@ void launch(const LogprobArgs& a, hipStream_t stream) {
     // and 36 (with k 64 75, 44 and 38).
     const int length = a.parts > 1 ? a.per : a.V;
     if (length <= kShort) {
-        if (a.parts > 1)
-            hipLaunchKernelGGL((logprob_short_kernel<FZ, true>), grid_of(a.N, a.parts), dim3(64), 0, stream, a);
-        else
-            hipLaunchKernelGGL((logprob_short_kernel<FZ, false>), grid_of(a.N, 1), dim3(64), 0, stream, a);
+        hipLaunchKernelGGL(logprob_short_kernel<FZ>, grid_of(a.N, 1), dim3(64), 0, stream, a);
     } else if (length <= 8192) {
         launch_rows<FZ, 128>(a, stream);
     } else if (length <= 65536) {
