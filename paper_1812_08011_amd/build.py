@@ -32,7 +32,8 @@ def compile_flags():
         "-ffp-contract=off",
         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
         "-I", INCLUDE, "-I", CSRC,
-        "-Wall", "-Wno-unused-function",
+        # a vector type whose alignment a template dropped would be stored as aligned
+        "-Wall", "-Wno-unused-function", "-Werror=align-mismatch",
     ]
 
 

@@ -33,6 +33,13 @@ template <>
 struct FourOf<FP8T_FMT_FP16> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2))); };
 template <>
 struct FourOf<FP8T_FMT_FP8> { typedef uint32_t type __attribute__((aligned(1))); };
+// Eight codes that are one vector.
+template <int FMT>
+struct AllOf;
+template <>
+struct AllOf<FP8T_FMT_FP16> { typedef Eight<FP8T_FMT_FP16>::v4 type; };
+template <>
+struct AllOf<FP8T_FMT_FP8> { typedef Eight<FP8T_FMT_FP8>::v2 type; };
 
 // Four h (0 or 1) of eight stored elements.
 template <int FMT>
@@ -90,8 +97,10 @@ __device__ __forceinline__ Eight<FMT> load8(const fmt_t<FMT>* row, const Cols<FO
 // Results past what the caches hold are stored past them (`stream`): what they
 // push out there may be wanted, they will not be found there.
 constexpr int64_t kStreamBytes = 32 << 20;
-template <typename V>
-__device__ __forceinline__ void put_vector(V* p, const V& v, bool stream) {
+// OF::type: a vector type, whose alignment (a template's own argument would lose it)
+// is one element's.
+template <typename OF>
+__device__ __forceinline__ void put_vector(typename OF::type* p, const typename OF::type& v, bool stream) {
     if (stream) {
         asm volatile("; past the caches");                  // or the two stores become one plain one
         __builtin_nontemporal_store(v, p);
@@ -106,10 +115,10 @@ __device__ __forceinline__ void store8(fmt_t<FMT>* row, const Cols<FOURS>& c, in
     using Four = typename FourOf<FMT>::type;
     if (c.b + 4 <= W) {
         if constexpr (FOURS || FMT == FP8T_FMT_F32) {
-            put_vector(reinterpret_cast<Four*>(row + c.a), four_of<FMT>(e, 0), stream);
-            put_vector(reinterpret_cast<Four*>(row + c.b), four_of<FMT>(e, 1), stream);
+            put_vector<FourOf<FMT>>(reinterpret_cast<Four*>(row + c.a), four_of<FMT>(e, 0), stream);
+            put_vector<FourOf<FMT>>(reinterpret_cast<Four*>(row + c.b), four_of<FMT>(e, 1), stream);
         } else {
-            put_vector(reinterpret_cast<decltype(e.a)*>(row + c.a), e.a, stream);
+            put_vector<AllOf<FMT>>(reinterpret_cast<typename AllOf<FMT>::type*>(row + c.a), e.a, stream);
         }
         return;
     }
