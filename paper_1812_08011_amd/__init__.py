@@ -148,8 +148,11 @@ def _ptr(t):
 def _stream(stream):
     if stream is None:
         import torch
-        # the address alone: 0.3 us, a stream object 2.7
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        # the address alone, where this torch gives it: 0.3 us, a stream object 2.7
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            return torch.cuda.current_stream().cuda_stream
+        return raw(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
