@@ -53,8 +53,9 @@ int embed_fwd(const int64_t* tokens, int64_t T, const void* table, int table_for
  * for every v in [0, V): a row that no token names is +0.  Errors of tokens
  * outside [0, V) are not read.  The tokens are sorted on the device, and a
  * row's sum is taken in the order of t, in pieces that the sorted order alone
- * decides.
- * e: T x W in e_format; g: V x W in g_format; both F32, FP16 or FP8.
+ * decides, in doubles.
+ * e: T x W in e_format; g: V x W in g_format; both F32, FP16 or FP8; g must not
+ * overlap e.
  * workspace: at least embed_bwd_workspace_size bytes, 16-byte aligned.
  * Errors: FP8T_EINVAL (negative size, T or W above 2^31 - 4097, V above
  * FP8T_MAX_VOCAB, unknown format, a stride below W, NULL pointer for
@@ -117,7 +118,7 @@ int rms_norm_fwd(const void* x, int x_format, int64_t x_ld, const float* x_row_s
  * h: h_format F32 or FP16; w: F32, FP16 or NULL; rstd: T floats; dy: F32, FP16
  * or FP8; dr, dx: d_format F32 or FP16, dx may be dr itself (same stride); dw:
  * W contiguous, F32 or FP16 (all +0 with T = 0).  dx, dx8 and dw are optional
- * (NULL), one is not.
+ * (NULL), one is not; but for dx in dr's place they must not overlap an operand.
  * workspace: with dw at least rms_norm_bwd_workspace_size bytes, 16-byte
  * aligned (partial sums of dw); without dw none is used.
  * Errors: FP8T_EINVAL (as rms_norm_fwd, and for a workspace that is not 16-byte

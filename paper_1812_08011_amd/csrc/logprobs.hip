@@ -18,13 +18,12 @@
 // Where rows are few, several workgroups share one, each with the k largest of
 // its part, and a second kernel joins them.
 //
-// 4096 x 32768 FP16: 54 us without alternatives, 4.9 TB/s; 71 with 20 of them, 81
-// with 64 (72 on a card that has not been at work): a row's sums, bound, second
+// 4096 x 32768 FP16, calls one after the other on two inputs in turn: 54 us without
+// alternatives, 4.9 TB/s; 64 with 20 of them, 72 with 64: a row's sums, bound, second
 // reading and ranking follow each other and hide behind other rows only, and they
 // are 1000 vector instructions a row with one alternative, 3000 with 64, beside 12
-// a logit, the vector ALUs' share of the stream.  Floats, twice the bytes: 92, 100
+// a logit, the vector ALUs' share of the stream.  Floats, twice the bytes: 92, 99
 // and 105 us.  One row of 50001 floats, 20 alternatives: 9 us and 5 for the join.
-//
 #include "row_ops.h"
 
 namespace fp8t {
@@ -759,9 +758,9 @@ template <int FZ>
 void launch(const LogprobArgs& a, hipStream_t stream) {
     // The fewest threads whose sums are not the longer part of a row's time: each
     // row waits for its sums, its bound and its few elements again, and more rows
-    // at a time hide that.  k 20, T 128, 256 and 512, measured side by side: 8192 x
-    // 8192 FP16 51, 59 and 105 us; 4096 x 32768 75, 69 and 75; 512 x 131072 59, 36
-    // and 36 (with k 64 75, 44 and 38).
+    // at a time hide that.  FP16, k 20, T 128, 256 and 512, in turn: 8192 x 8192 46,
+    // 45 and 69 us; 4096 x 32768 74, 64 and 64 (with k 64 86, 72 and 75); 1024 x
+    // 65536 35, 31 and 32; 512 x 131072 61, 35 and 32 (with k 64 75, 43 and 34).
     const int length = a.parts > 1 ? a.per : a.V;
     if (length <= kShort) {
         hipLaunchKernelGGL(logprob_short_kernel<FZ>, grid_of(a.N, 1), dim3(64), 0, stream, a);

@@ -3,12 +3,16 @@
 // HBM-bound.  T threads own a row and keep it in registers, NV times eight
 // elements each, between the sum of squares and the result: every element is
 // read once and written once.  T is the fewest threads that hold a row (8 for 64
-// columns: 100000 x 64 FP16 in 12 us, with a wave a row 84).  Rows wider than
+// columns: 100000 x 64 FP16 in 11 us, with a wave a row 84).  Rows wider than
 // kWidest are read again.
 //
 // 16384 x 4096, FP16 + floats to floats and FP8, each row scaled: 129 us, 5.7 TB/s
-// (a copy of 1 GiB runs at 5.6); 8192 x 2048, all of it FP16, to FP8: 29 us, 4.0
-// TB/s, the vector ALUs between the codes and floats.  One row: 3.5 us, a launch.
+// (a copy of 1 GiB runs at 5.6); 8192 x 2048, all of it FP16, to FP8: 27 us, 4.3
+// TB/s, the vector ALUs, between the codes and floats, 72% busy.  Rows of x divided
+// by their scale: 4 us of the first, 1 of the second.  2048 x 20000, FP16 + floats to
+// floats and FP8: 113 us where a copy's rate is 81, the sum's row read again; 134
+// with rows scaled, and again; 2048 x 16384 in registers 70 of 66.  One row: 3.8 us,
+// a launch.
 // The squares (exact), their sum and 1 / rms are doubles, so that rstd is rounded
 // once; n is the floats' two products after it, as a program with rstd in hand
 // forms it, Inf and NaN included.

@@ -5,7 +5,8 @@
 // gradient, with the next row on its way, and their columns' sums of dw over the
 // rows.  Those go to the workspace, one row of sums for each workgroup, and a
 // second kernel adds them in order.  The sums and the mean's are doubles of float
-// products, a workgroup's dw is stored as floats: the conversion and the add hide behind the stream (1 us of the 16 below).
+// products, a workgroup's dw is stored as floats: the conversions and additions hide
+// behind the stream (1 us of the 16 below).
 // Rows wider than 8192 are twice eight elements a thread without a row ahead and
 // with the sums in LDS (no registers are left), those wider than kWidest are read
 // twice, and dw has a kernel of its own.
@@ -13,7 +14,8 @@
 // 8192 x 4096 floats with FP16 errors, to floats and FP8: 98 us and 5 for the
 // join, 5.1 TB/s (a copy of 1 GiB runs at 5.6); twice eight elements in 256 threads, 155
 // registers, and no row ahead: 109 and 7.  5003 x 1001 in FP16: 16 us and 5, three
-// rows for each group of threads one after the other, 2 TB/s.
+// rows for each group of threads one after the other, 2 TB/s.  2048 x 16384: 109 us
+// where a copy's rate is 91; 2048 x 20000: 136 and 56 for dw, of 111.
 #include "row_ops.h"
 
 namespace fp8t {
@@ -301,7 +303,10 @@ NormGradPlan norm_grad_plan(int64_t T, int64_t W) {
     const int64_t groups = threads < 512 ? 512 / threads : 1;
     int64_t cus = device_cus();
     if (cus <= 0) cus = 256;
-    // as many as run at a time, but two rows for each group at least
+    // as many as run at a time, but two rows for each group at least.  Wide rows' dw
+    // has a workgroup for 2048 columns besides: ranges of rows 32, 64, 128 and 256, in
+    // turn, 2048 x 20000 93, 64, 58 and 58 us, 512 x 100000 79, 77, 78 and 85, 512 x
+    // 300000 214, 222, 235 and 287 (more partial sums)
     int64_t most = W > kWidest ? 64 : cus * 1024 / (threads * groups) * groups;
     const int64_t pairs = (T + 1) / 2;
     if (most > pairs) most = pairs;
